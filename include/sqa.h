@@ -16,6 +16,9 @@
  *   sqa_prefill_scores_lse, sqa_residual_add_importance, sqa_decode_plan (what a
  *   decode call would launch), sqa_kept_idx_sorted, and for K/V kept in 16-row
  *   blocks (sqa_layer_cache.block_table) the host free list sqa_block_pool_*.
+ *   Between a model's projections and these calls: sqa_qk_norm_rope, and for prompts
+ *   that come in chunks (or drafts of a few tokens) sqa_chunk_append,
+ *   sqa_chunk_attention and sqa_chunk_scores.
  *
  * Conventions
  *   - "DEVICE" pointers are HIP device memory owned by the caller and borrowed
@@ -423,6 +426,89 @@ sqa_status sqa_read_device_status(const void* workspace, void* stream, int32_t* 
  *   out : DEVICE int32 [B][Hkv][layer->capacity]; with packed units (unit_offset)
  *         laid out like pos: unit u's entries start at out[unit_offset[u]] */
 sqa_status sqa_kept_idx_sorted(const sqa_layer_cache* layer, int B, int Hkv, int32_t* out, void* stream);
+
+/* ---- queries and keys as a projection leaves them, and chunks of a prompt ----
+ * What lies between a model's projections and the calls above.  A chunk is T tokens of each of B sequences, at
+ * consecutive positions new_pos, new_pos + 1, ...: T = 1 is a decode step, a few are a draft to be verified, hundreds
+ * or thousands a piece of a prompt or all of it.  With opts:
+ *   prompt_len  [B]: how many of the T are tokens, 0..T; rows behind them are padding: neither read nor written
+ *   new_pos_seq [B]: position of the sequence's first new token (new_pos is then ignored); < 0: it takes no part
+ *   budget_seq  [B] (one layer): the sequence's budget, 1 .. layer->budget (sqa_chunk_append)
+ *   status      receives the error code of a sequence or unit that the kernel left out (below); never cleared
+ * opts->order is not used.  Any Hq that is a multiple of Hkv; D is 64 or 128.
+ */
+typedef struct sqa_token_rows {   /* HOST; heads of tokens as they lie in a projection's output */
+  const void* data;               /* DEVICE, 16-byte aligned: element d of head h of token t of sequence b is
+                                     data[b*seq_stride + t*row_stride + h*D + d]                     */
+  int64_t seq_stride, row_stride; /* in elements, not negative, multiples of 16 bytes (ignored where B or T is 1): q, k
+                                     and v may be parts of one packed tensor, or a slice of a longer prompt */
+} sqa_token_rows;
+
+typedef struct sqa_head_prep {    /* HOST; what is done to each head of queries and keys, in this order */
+  const void* q_weight;           /* DEVICE [D], the call's dtype, or NULL: x <- x / sqrt(mean(x^2) + eps) * weight */
+  const void* k_weight;           /* the same for keys                                               */
+  const float* rope;              /* DEVICE [n_pos][rot_dim] or NULL, 16-byte aligned: row p holds rot_dim/2 cosines and then
+                                     rot_dim/2 sines of position p's angles: (a, b) <- (a cos - b sin, b cos + a sin) */
+  float eps;                      /* >= 0                                                            */
+  int32_t n_pos, rot_dim;         /* the leading rot_dim elements of a head are rotated; a multiple of 16, at most D */
+  int32_t interleaved;            /* pairs (a, b): 0 = elements (i, i + rot_dim/2), 1 = elements (2i, 2i + 1) */
+} sqa_head_prep;
+
+/* Norm, rotation and layout of queries and keys in one pass: what sqa_prefill_scores, sqa_prefill_compress (keys),
+ * sqa_chunk_attention and sqa_decode_step (T = 1) take.  All arithmetic in fp32, rounded once.
+ *   q, k         : HOST structs; either may be NULL (with its output)
+ *   prep         : HOST; NULL = layout only
+ *   q_out, k_out : DEVICE [B][Hq][T][D], [B][Hkv][T][D]; must not overlap any input
+ * A sequence that has tokens at positions >= n_pos is left out: status SQA_ERR_SHAPE. */
+sqa_status sqa_qk_norm_rope(const sqa_token_rows* q, const sqa_token_rows* k, sqa_dtype dt,
+                            int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
+                            void* q_out, void* k_out, void* stream, const sqa_batch_opts* opts);
+
+/* Appends a chunk to one layer's cache (Eq. 2-3 for T tokens; nothing is evicted): the token at position p goes to slot p
+ * of each of its sequence's units, its key normalised and rotated on the way, its value as it is, its score 0.
+ * Sets unit_state to {new_pos + tokens, 0, -2, 0}: what lay behind is dropped, so a draft that was rejected
+ * is taken back by the next append at a smaller new_pos.
+ *   q, q_out : the chunk's queries, prepared by the same launch as in sqa_qk_norm_rope; or both NULL
+ *   k, v     : HOST structs
+ *   layer    : HOST struct with DEVICE pointers, any of the three layouts; score_acc may be NULL.  Units as
+ *              sqa_prefill_compress or decode leave them, or empty ones ({0, 0, -2, 0})
+ * A unit takes a chunk while it still holds every token of its sequence (slot = position, as it is until the
+ * first eviction).  One that does not is left untouched, and so is one with too few tokens, status SQA_ERR_STATE; one
+ * whose budget or slots would be exceeded: SQA_ERR_CAPACITY; a budget_seq entry out of range: SQA_ERR_BUDGET;
+ * a block number outside the pools, or positions >= n_pos: SQA_ERR_SHAPE.  The queries are written all the same (but for the last). */
+sqa_status sqa_chunk_append(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt,
+                            int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
+                            void* q_out, const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts);
+
+/* Scratch of the two calls below for chunks of up to T tokens: work on few rows is shared out over the slots and joined.
+ * DEVICE, 256-byte aligned, zero-filled once before its first use (sqa_decode_workspace_init) and not shared with other calls
+ * than these; calls that share one must not overlap in time.  0 for arguments that those calls refuse. */
+size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int Hq, int Hkv, int D);
+
+/* Causal attention of a chunk over all that the cache holds up to each of its tokens (the chunk has been appended):
+ *   out[b][t][h] = sum_{j <= new_pos + t} softmax_j(q . K_j / sqrt(D)) V_j
+ *   q   : DEVICE [B][Hq][T][D], dtype dt
+ *   out : DEVICE [B][T][Hq][D], dtype dt (what an output projection takes)
+ *   lse : DEVICE float [B][Hq][T] or NULL: ln sum_{j <= new_pos + t} exp(q . K_j / sqrt(D)), the row_lse of
+ *         sqa_prefill_scores_lse and sqa_chunk_scores
+ * The softmax is in fp32; in bf16 the probabilities are rounded to bf16 for the product with V, as in sqa_decode_step on the
+ * matrix cores.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
+ * A unit that does not hold the chunk at its slots (see sqa_chunk_append) gets rows of zeros and lse -inf, status
+ * SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  Results are the same from run to run. */
+sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                               const sqa_layer_cache* layer, void* out, float* lse,
+                               void* workspace, size_t ws_bytes, void* stream, const sqa_batch_opts* opts);
+
+/* H2O's accumulated attention for a chunk (Sec. 5.1 "Heavy-Hitter"): adds to each slot's score what the chunk gives it,
+ *   score_acc[j] += sum over the g query heads of the unit and the chunk's tokens t with new_pos + t >= j of
+ *                   exp(q . K_j / sqrt(D) - lse[b][h][t])
+ * After the last chunk of a prompt score_acc is what sqa_prefill_scores gives for the whole prompt (to rounding), and K, V and
+ * score_acc of a dense layer are the inputs of sqa_prefill_compress (P = capacity, opts->prompt_len).
+ *   q, lse : as for sqa_chunk_attention; layer->score_acc required.  A wrong lse gives wrong scores, not an error
+ * A unit that does not hold the chunk is left untouched, status as above.  Results are the same from run to run. */
+sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D,
+                            int32_t new_pos, const sqa_layer_cache* layer,
+                            void* workspace, size_t ws_bytes, void* stream, const sqa_batch_opts* opts);
 
 /* ---- free list for blocked K/V allocation (host only) ----------------------
  * Book-keeping for the block numbers of ONE pool pair (the K and V pools of one layer share numbers, see

@@ -64,6 +64,21 @@ class BatchOptsStruct(C.Structure):
                 ("status", C.c_void_p), ("order", C.c_int32)]
 
 
+class TokenRowsStruct(C.Structure):
+    """Mirror of sqa_token_rows."""
+    _fields_ = [("data", C.c_void_p), ("seq_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class HeadPrepStruct(C.Structure):
+    """Mirror of sqa_head_prep."""
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("rope", C.c_void_p), ("eps", C.c_float),
+                ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+    weights, rope_rows = (), None                              # the tensors behind the pointers
+
+    def tensors(self):
+        return (*self.weights, self.rope_rows)
+
+
 ORDER = {"evict_then_attend": 0, "attend_then_evict": 1}
 
 _vp, _i, _i64, _sz, _f64 = C.c_void_p, C.c_int, C.c_int64, C.c_size_t, C.c_double
@@ -117,6 +132,17 @@ _lib.sqa_kept_idx_sorted.argtypes = [_LCp, _i, _i, _vp, _vp]
 _lib.sqa_decode_plan.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, _i, C.POINTER(DecodePlanInfo), C.POINTER(DecodeLayerPlan)]
 _lib.sqa_decode_plan_waves.restype = C.c_int32
 _lib.sqa_decode_plan_waves.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, _i]
+_TRp, _HPp = C.POINTER(TokenRowsStruct), C.POINTER(HeadPrepStruct)
+_lib.sqa_qk_norm_rope.restype = _i
+_lib.sqa_qk_norm_rope.argtypes = [_TRp, _TRp, _i, _i, _i, _i, _i, _i, _HPp, C.c_int32, _vp, _vp, _vp, _BOp]
+_lib.sqa_chunk_append.restype = _i
+_lib.sqa_chunk_append.argtypes = [_TRp, _TRp, _TRp, _i, _i, _i, _i, _i, _i, _HPp, C.c_int32, _vp, _vp, _vp, _BOp]
+_lib.sqa_chunk_workspace_bytes.restype = _sz
+_lib.sqa_chunk_workspace_bytes.argtypes = [_vp, _i, _i, _i, _i, _i]
+_lib.sqa_chunk_attention.restype = _i
+_lib.sqa_chunk_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _BOp]
+_lib.sqa_chunk_scores.restype = _i
+_lib.sqa_chunk_scores.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _sz, _vp, _BOp]
 _lib.sqa_block_pool_create.argtypes = [C.c_int32]
 _lib.sqa_block_pool_create.restype = _vp
 _lib.sqa_block_pool_destroy.argtypes = [_vp]
@@ -154,11 +180,13 @@ def _stream():
 def batch_opts(prompt_len: Optional[torch.Tensor] = None, budget_seq: Optional[torch.Tensor] = None,
                new_pos_seq: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                order: str = "evict_then_attend") -> BatchOptsStruct:
-    """sqa_batch_opts from int32 device tensors (the caller keeps them alive until the work has run)."""
+    """sqa_batch_opts from int32 device tensors (kept alive with the result)."""
     for t in (prompt_len, budget_seq, new_pos_seq, status):
         if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
             raise TypeError("per-sequence arrays are contiguous int32 tensors")
-    return BatchOptsStruct(_ptr(prompt_len), _ptr(budget_seq), _ptr(new_pos_seq), _ptr(status), ORDER[order])
+    o = BatchOptsStruct(_ptr(prompt_len), _ptr(budget_seq), _ptr(new_pos_seq), _ptr(status), ORDER[order])
+    o.tensors = (prompt_len, budget_seq, new_pos_seq, status)
+    return o
 
 
 # (a pure function of the shape; asked for anew it is 1 to 5 us of host arithmetic, a small call's 12 in all)
@@ -547,3 +575,165 @@ def kept_idx_sorted(caches: LayerCaches, layer: int) -> torch.Tensor:
     _check(_lib.sqa_kept_idx_sorted(caches.struct_ptr(layer), caches.B, caches.Hkv, _ptr(out), _stream()),
            "sqa_kept_idx_sorted")
     return out
+
+
+# ---- queries and keys as a projection leaves them, and chunks of a prompt ----
+
+def rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """[n_pos, rot_dim] fp32: cosines, then sines of p / base^(2 i / rot_dim), i < rot_dim / 2, the angles in 64 bits
+    (a caller with other frequencies fills such a table itself)."""
+    inv = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    angle = torch.arange(n_pos, dtype=torch.float64)[:, None] * inv
+    return torch.cat([angle.cos(), angle.sin()], 1).to(torch.float32).to(device)
+
+
+def head_prep(q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              rope: Optional[torch.Tensor] = None, interleaved: bool = False) -> HeadPrepStruct:
+    """sqa_head_prep: weights [D] of the heads' norms, a rope_table (kept alive with the result)."""
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dim() != 1 or not w.is_contiguous()):
+            raise TypeError("norm weights are contiguous tensors [D]")
+    if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 2 or not rope.is_contiguous()):
+        raise TypeError("rope is a contiguous fp32 tensor [n_pos, rot_dim]")
+    p = HeadPrepStruct(_ptr(q_weight), _ptr(k_weight), _ptr(rope), float(eps), 0 if rope is None else rope.shape[0],
+                       0 if rope is None else rope.shape[1], int(interleaved))
+    p.weights, p.rope_rows = tuple(w for w in (q_weight, k_weight) if w is not None), rope
+    return p
+
+
+def _on_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The library runs on the current device's stream: tensors of the host or of another device are refused."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != _get_device()):
+            raise ValueError("a tensor is not on the current device")
+
+
+def _token_rows(t: torch.Tensor) -> TokenRowsStruct:
+    """[B, T, H, D], dense within a token: a projection's output, a part of a packed one, or a slice of a longer prompt."""
+    s = t.stride()
+    if t.dim() != 4 or (s[3] != 1 and t.shape[3] != 1) or (s[2] != t.shape[3] and t.shape[2] != 1):
+        raise TypeError("heads of a token lie one after the other: [B, T, H, D] with strides (.., .., D, 1)")
+    return TokenRowsStruct(t.data_ptr(), s[0], s[1])
+
+
+def _check_prep(prep: Optional[HeadPrepStruct], dtype: torch.dtype, D: int):
+    if prep is None:
+        return
+    if any(w.dtype != dtype or w.shape[0] != D for w in prep.weights):
+        raise TypeError("norm weights are [D] tensors of the call's dtype")
+
+
+def _out_like(out: Optional[torch.Tensor], shape, dtype, device) -> torch.Tensor:
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or not out.is_contiguous():
+        raise TypeError("expected a contiguous %s tensor %s" % (dtype, tuple(shape)))
+    return out
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: int, prep: Optional[HeadPrepStruct] = None,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 opts: Optional[BatchOptsStruct] = None):
+    """q [B, T, Hq, D], k [B, T, Hkv, D] (either may be None) at positions new_pos .. -> q [B, Hq, T, D], k [B, Hkv, T, D],
+    normalised and rotated."""
+    some = q if q is not None else k
+    if some is None:
+        raise TypeError("queries or keys")
+    B, T, _, D = some.shape
+    Hq = q.shape[2] if q is not None else k.shape[2]
+    Hkv = k.shape[2] if k is not None else Hq
+    if q is not None and k is not None and (k.shape[:2] != q.shape[:2] or k.shape[3] != D or k.dtype != q.dtype):
+        raise TypeError("queries and keys of the same tokens, head size and dtype")
+    if q is None and q_out is not None or k is None and k_out is not None:
+        raise TypeError("an output without its input")
+    _check_prep(prep, some.dtype, D)
+    if q is not None:
+        q_out = _out_like(q_out, (B, Hq, T, D), q.dtype, q.device)
+    if k is not None:
+        k_out = _out_like(k_out, (B, Hkv, T, D), k.dtype, k.device)
+    rows = [None if t is None else _token_rows(t) for t in (q, k)]
+    _on_device(q, k, q_out, k_out, *(prep.tensors() if prep is not None else ()))
+    _check(_lib.sqa_qk_norm_rope(rows[0], rows[1], _dt(some), B, T, Hq, Hkv, D, prep, int(new_pos), _ptr(q_out), _ptr(k_out),
+                                 _stream(), opts), "sqa_qk_norm_rope")
+    return q_out, k_out
+
+
+def _layer_at(caches: "LayerCaches", layer: int, dtype: torch.dtype, B: int, Hkv: Optional[int], D: int) -> int:
+    """Address of a layer's record, after a look at whether the call's tensors are the cache's."""
+    if not 0 <= layer < caches.L:
+        raise IndexError("layer outside the table")
+    if dtype != caches.dtype or B != caches.B or D != caches.D or Hkv not in (None, caches.Hkv):
+        raise TypeError("the cache has another dtype, batch, heads or head size")
+    return C.addressof(caches.table) + layer * _LC_BYTES
+
+
+def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0,
+                 prep: Optional[HeadPrepStruct] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 opts: Optional[BatchOptsStruct] = None) -> Optional[torch.Tensor]:
+    """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
+    way; with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
+    B, T, Hkv, D = k.shape
+    at = _layer_at(caches, layer, k.dtype, B, Hkv, D)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise TypeError("keys and values of one shape and dtype")
+    Hq = Hkv
+    if q is not None:
+        if q.shape[:2] != k.shape[:2] or q.shape[3] != D or q.dtype != k.dtype:
+            raise TypeError("queries and keys of the same tokens, head size and dtype")
+        Hq = q.shape[2]
+        q_out = _out_like(q_out, (B, Hq, T, D), q.dtype, q.device)
+    elif q_out is not None:
+        raise TypeError("an output without its input")
+    _check_prep(prep, k.dtype, D)
+    rows = [None if t is None else _token_rows(t) for t in (q, k, v)]
+    _on_device(q, k, v, q_out, caches.K[layer], *(prep.tensors() if prep is not None else ()))
+    _check(_lib.sqa_chunk_append(*rows, _dt(k), B, T, Hq, Hkv, D, prep, int(new_pos), _ptr(q_out), at, _stream(), opts), "sqa_chunk_append")
+    return q_out
+
+
+def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> torch.Tensor:
+    """Scratch of chunk_attention and chunk_scores for chunks of up to T tokens, zero-filled."""
+    need = _lib.sqa_chunk_workspace_bytes(_layer_at(caches, layer, caches.dtype, caches.B, None, caches.D), caches.B, T, Hq,
+                                          caches.Hkv, caches.D)
+    if need == 0:
+        raise SqaError(2, "sqa_chunk_workspace_bytes")
+    ws = torch.empty(need, dtype=torch.uint8, device=caches.K[0].device)
+    _check(_lib.sqa_decode_workspace_init(_ptr(ws), need, _stream()), "sqa_decode_workspace_init")
+    return ws
+
+
+def _chunk_queries(q: torch.Tensor):
+    if q.dim() != 4 or not q.is_contiguous():
+        raise TypeError("a chunk's queries are a contiguous tensor [B, Hq, T, D]")
+    return q.shape
+
+
+def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                    opts: Optional[BatchOptsStruct] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """q [B, Hq, T, D] of an appended chunk -> (out [B, T, Hq, D], lse [B, Hq, T] fp32)."""
+    B, Hq, T, D = _chunk_queries(q)
+    at = _layer_at(caches, layer, q.dtype, B, None, D)
+    out = _out_like(out, (B, T, Hq, D), q.dtype, q.device)
+    lse = _out_like(lse, (B, Hq, T), torch.float32, q.device)
+    if workspace is None:
+        workspace = chunk_workspace(caches, Hq, T, layer)
+    _on_device(q, out, lse, workspace, caches.K[layer])
+    _check(_lib.sqa_chunk_attention(_ptr(q), _dt(q), B, T, Hq, caches.Hkv, D, int(new_pos), at, _ptr(out), _ptr(lse),
+                                    _ptr(workspace), workspace.numel(), _stream(), opts), "sqa_chunk_attention")
+    return out, lse
+
+
+def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0,
+                 workspace: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None) -> None:
+    """Adds what an appended chunk's queries [B, Hq, T, D] give to every slot to the layer's accumulated scores; lse [B, Hq, T]
+    from chunk_attention."""
+    B, Hq, T, D = _chunk_queries(q)
+    at = _layer_at(caches, layer, q.dtype, B, None, D)
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (B, Hq, T):
+        raise TypeError("lse is a contiguous fp32 tensor [B, Hq, T]")
+    if workspace is None:
+        workspace = chunk_workspace(caches, Hq, T, layer)
+    _on_device(q, lse, workspace, caches.K[layer])
+    _check(_lib.sqa_chunk_scores(_ptr(q), _ptr(lse), _dt(q), B, T, Hq, caches.Hkv, D, int(new_pos), at, _ptr(workspace),
+                                 workspace.numel(), _stream(), opts), "sqa_chunk_scores")
