@@ -103,7 +103,7 @@ __device__ __forceinline__ bool last_to_arrive(int32_t* count, int of, int* s_wo
 constexpr int kChunkCounters = 1024;                // at the head of a workspace, whatever the call's shape
 constexpr size_t kChunkCounterBytes = kChunkCounters * sizeof(int32_t);
 
-size_t chunk_attention_scratch(int B, int T, int Hq, int Hkv, int D, int64_t slots);    // bytes behind the counters
-size_t chunk_scores_scratch(int B, int T, int Hq, int Hkv, int D, int64_t slots);
+size_t chunk_attention_scratch(int T, int Hq, int Hkv, int D);                          // bytes behind the counters
+size_t chunk_scores_scratch();
 
 }  // namespace sqa

@@ -10,6 +10,7 @@
 //   O^T = V^T.P^T  a row's sums lie in the two lanes of its column: rescaling is a multiplication by a lane's own number
 // K and V tiles go from global memory straight to LDS, two buffers, in an order without bank conflicts (TileRows).
 #include "sqa_chunk_mma.h"
+#include <type_traits>
 
 namespace sqa {
 
@@ -25,29 +26,28 @@ struct AttentionArgs {
   int32_t* count;                                   // [items]
   float2* part;                                     // [items][splits][32 RW][D / 2 + 1]: a row's sums, then (m, l)
   float scale;                                      // log2(e) / sqrt(D)
+  float near;                                       // 8 / scale: logits that close to a row's reference do not move it
   int tiles, splits;
 };
 
-template <typename T, int D, int RW, int KT> struct AttentionTile {
-  using R = TileRows<T, D>;
-  static constexpr int KW = 4 / RW, KB = KT / KW / 32, M = 32 * RW, NB = D / 32;
-  static constexpr int TILE = KT * R::RB;
-  static constexpr int STAGE = 4 * TILE > 4 * 32 * D * 4 ? 4 * TILE : 4 * 32 * D * 4;
-};
+// the halves of a pair of bf16 that are not finite, as a mask
+__device__ __forceinline__ uint32_t odd_mask(uint32_t v) {
+  return ((v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
 
 // Does a tile of BYTES bytes in LDS hold a number that is not finite?  This thread's share of it; CLEAR: such numbers become 0.
-template <typename T, int BYTES, bool CLEAR> __device__ __forceinline__ bool odd_values(char* tile) {
+template <typename T, int BYTES, int NT, bool CLEAR> __device__ __forceinline__ bool odd_values(char* tile) {
   bool odd = false;
 #pragma unroll 1
-  for (int i = threadIdx.x * 16; i < BYTES; i += kAtThreads * 16) {
+  for (int i = threadIdx.x * 16; i < BYTES; i += NT * 16) {
     const uint4 w = *reinterpret_cast<const uint4*>(tile + i);
     uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (sizeof(T) == 2) {
-        const bool lo = (v[k] & 0x7f80u) == 0x7f80u, hi = (v[k] & 0x7f800000u) == 0x7f800000u;
-        odd |= lo || hi;
-        if constexpr (CLEAR) v[k] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
+        const uint32_t x = odd_mask(v[k]);
+        odd |= x != 0;
+        if constexpr (CLEAR) v[k] &= ~x;
       } else {
         const bool x = (v[k] & 0x7f800000u) == 0x7f800000u;
         odd |= x;
@@ -59,77 +59,203 @@ template <typename T, int BYTES, bool CLEAR> __device__ __forceinline__ bool odd
   return odd;
 }
 
+// What a workgroup of NT threads works on: M rows of one unit and a run of its slots, in tiles of KT.
+template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
+  using R = TileRows<T, D>;
+  static constexpr int PP = D / 4;                  // 16-byte pieces of a row of sums
+  static constexpr int REC = D / 2 + 1;             // a row of sums and its (m, l) as pairs
+  int64_t item;
+  int b, h, g, row0, rows, last_row;                // rows: of the whole unit
+  int split, parts, tile0, tile1, end;              // end: the slots that the rows see
+  int64_t pos;
+  ChunkUnit unit;
+
+  // false: nothing to do (or rows of zeros have been written)
+  __device__ __forceinline__ bool begin(const AttentionArgs& a, int* s_table) {
+    const int64_t items = (int64_t)a.c.B * a.c.Hkv * a.tiles;
+    const int64_t work = xcd_item(items * a.splits);
+    if (work < 0) return false;
+    const int tid = threadIdx.x;
+    split = (int)(work % a.splits);
+    item = work / a.splits;
+    const int u = (int)(item / a.tiles), tile = a.tiles - 1 - (int)(item % a.tiles);     // the longest first
+    b = u / a.c.Hkv; h = u % a.c.Hkv; g = a.c.g;
+    const ChunkSeq seq = chunk_seq(a.c, b, tid == 0 && h == 0 && tile == 0 && split == 0);
+    rows = __builtin_amdgcn_readfirstlane(seq.n) * g;
+    row0 = tile * M;
+    if (row0 >= rows) return false;
+    pos = seq.pos;
+    unit = chunk_unit(a.c.L, u);
+    last_row = min(row0 + M, rows) - 1;
+    // does the unit hold the chunk, and do its blocks lie in the pools
+    int why = chunk_held(a.c.L, unit, u, pos + seq.n) ? 0 : SQA_ERR_STATE;
+    if (!why && unit.table) {
+      int outside = 0;
+      for (int i = tid; i < (int)((pos + seq.n + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS); i += NT) {
+        const int blk = unit.table[i];
+        s_table[i] = blk;
+        outside |= (unsigned)blk >= (unsigned)a.c.L.n_blocks;
+      }
+      if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
+    }
+    if (why) {
+      if (split) return false;
+      if (tid == 0 && a.c.status) *a.c.status = why;
+      for (int i = tid; i < (last_row + 1 - row0) * R::PPR; i += NT) {
+        int t, head;
+        place(row0 + i / R::PPR, t, head);
+        st16(static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + i % R::PPR * R::E, make_uint4(0, 0, 0, 0));
+        if (a.lse && i % R::PPR == 0) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = -INFINITY;
+      }
+      return false;
+    }
+    end = __builtin_amdgcn_readfirstlane((int)(pos + last_row / g + 1));
+    const int nt = (end + KT - 1) / KT, per = (nt + a.splits - 1) / a.splits;
+    parts = (nt + per - 1) / per;
+    tile0 = split * per;
+    tile1 = min(tile0 + per, nt);
+    return split < parts;
+  }
+  __device__ __forceinline__ void place(int r, int& t, int& head) const { t = r / g; head = h * g + r % g; }
+
+  __device__ __forceinline__ void store4(const AttentionArgs& a, int row, int p, float4 v, float mm, float ll) const {
+    int t, head;
+    place(row0 + row, t, head);
+    const float inv = 1.f / ll;
+    T* dst = static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + 4 * p;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(dst) = make_uint2(f32_to_bf16_bits(v.x * inv) | (f32_to_bf16_bits(v.y * inv) << 16),
+                                                  f32_to_bf16_bits(v.z * inv) | (f32_to_bf16_bits(v.w * inv) << 16));
+    else
+      *reinterpret_cast<float4*>(dst) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+    if (p == 0 && a.lse) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = 0.6931471805599453f * fmaf(mm, a.scale, log2f(ll));
+  }
+
+  // The waves' sums (this one's: the rows 32 rw .. in o, their references m and sums l) joined over the KW waves of the same rows and
+  // the workgroups of the same rows, and stored.  Each wave's go through LDS as 32 rows, 16-byte pieces exchanged by the row.
+  template <int KW>
+  __device__ __forceinline__ void finish(const AttentionArgs& a, char* s_stage, float (*s_m)[M], float (*s_l)[M], int* s_word, int rw, int kw,
+                                         f32x16_t (&o)[D / 32], float m, float l) const {
+    constexpr int NB = D / 32;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    l = other_half_sum(l);
+    __syncthreads();
+    if (half == 0) { s_m[kw][32 * rw + col] = m; s_l[kw][32 * rw + col] = l; }
+    if constexpr (KW > 1) {
+      __syncthreads();
+      float top = s_m[0][32 * rw + col];
+#pragma unroll
+      for (int k = 1; k < KW; ++k) top = fmaxf(top, s_m[k][32 * rw + col]);
+      const float w = exp2_fast((m - top) * a.scale);
+#pragma unroll
+      for (int e = 0; e < NB; ++e) o[e] *= w;
+    }
+    float4* const mine4 = reinterpret_cast<float4*>(s_stage) + (kw * M + 32 * rw + col) * PP;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < NB; ++e) mine4[(8 * e + c_row(i, half) / 4) ^ (col & 15)] = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
+      } else if constexpr (NB == 4) {
+#pragma unroll
+        for (int x = i; x < i + 4; ++x) mine4[c_row(x, half) ^ (col & 15)] = make_float4(o[0][x], o[1][x], o[2][x], o[3][x]);
+      } else {
+#pragma unroll
+        for (int x = i; x < i + 4; x += 2) mine4[(c_row(x, half) / 2) ^ (col & 15)] = make_float4(o[0][x], o[1][x], o[0][x + 1], o[1][x + 1]);
+      }
+    __syncthreads();
+    auto joined = [&](int row, float& mm, float& ll) {
+      mm = s_m[0][row];
+#pragma unroll
+      for (int k = 1; k < KW; ++k) mm = fmaxf(mm, s_m[k][row]);
+      ll = 0.f;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) ll += s_l[k][row] * (KW > 1 ? exp2_fast((s_m[k][row] - mm) * a.scale) : 1.f);
+    };
+    auto piece4 = [&](int row, int p) {
+      float4 v = reinterpret_cast<const float4*>(s_stage)[row * PP + (p ^ (row & 15))];
+#pragma unroll
+      for (int k = 1; k < KW; ++k) {
+        const float4 x = reinterpret_cast<const float4*>(s_stage)[(k * M + row) * PP + (p ^ (row & 15))];
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
+      return v;
+    };
+    const int live = (last_row + 1 - row0) * PP;
+    if (parts == 1) {
+      for (int i = tid; i < live; i += NT) {
+        float mm, ll;
+        joined(i / PP, mm, ll);
+        store4(a, i / PP, i % PP, piece4(i / PP, i % PP), mm, ll);
+      }
+      return;
+    }
+    float2* const rec = a.part + (item * a.splits) * M * REC;
+    for (int i = tid; i < live; i += NT) {
+      const int row = i / PP, p = i % PP;
+      float2* dst = rec + ((int64_t)split * M + row) * REC;
+      const float4 v = piece4(row, p);
+      hand_over(dst + 2 * p, make_float2(v.x, v.y));
+      hand_over(dst + 2 * p + 1, make_float2(v.z, v.w));
+      if (p == 0) {
+        float mm, ll;
+        joined(row, mm, ll);
+        hand_over(dst + D / 2, make_float2(mm, ll));
+      }
+    }
+    if (!last_to_arrive(a.count + item, parts, s_word)) return;
+    for (int i = tid; i < live; i += NT) {
+      const int row = i / PP, p = i % PP;
+      float mm = -FLT_MAX, ll = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < parts; ++k) mm = fmaxf(mm, handed_over(rec + ((int64_t)k * M + row) * REC + D / 2).x);
+      for (int k = 0; k < parts; ++k) {
+        const float2* src = rec + ((int64_t)k * M + row) * REC;
+        const float2 ml = handed_over(src + D / 2), x = handed_over(src + 2 * p), y = handed_over(src + 2 * p + 1);
+        const float w = exp2_fast((ml.x - mm) * a.scale);
+        ll = fmaf(ml.y, w, ll);
+        v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(y.x, w, v.z); v.w = fmaf(y.y, w, v.w);
+      }
+      store4(a, row, p, v, mm, ll);
+    }
+  }
+};
+
+template <typename T, int D, int RW, int KT> struct AttentionTile {
+  using R = TileRows<T, D>;
+  static constexpr int KW = 4 / RW, KB = KT / KW / 32, M = 32 * RW, NB = D / 32;
+  static constexpr int TILE = KT * R::RB;
+  static constexpr int STAGE = 4 * TILE > 4 * 32 * D * 4 ? 4 * TILE : 4 * 32 * D * 4;
+};
+
 template <typename T, int D, int RW, int KT>
 __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const AttentionArgs a) {
   using C = AttentionTile<T, D, RW, KT>;
   using R = TileRows<T, D>;
   constexpr int KW = C::KW, KB = C::KB, M = C::M, NB = C::NB;
-  extern __shared__ char s_stage[];
+  extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // (16-byte reads of 8-byte places take 8 times as long)
   __shared__ float s_m[KW][M], s_l[KW][M];
   __shared__ int s_word;
   int* const s_table = reinterpret_cast<int*>(s_stage + C::STAGE);
-
-  const int64_t items = (int64_t)a.c.B * a.c.Hkv * a.tiles;
-  const int64_t work = xcd_item(items * a.splits);
-  if (work < 0) return;
-  const int split = (int)(work % a.splits);
-  const int64_t item = work / a.splits;
-  const int u = (int)(item / a.tiles), tile = a.tiles - 1 - (int)(item % a.tiles);     // the longest first
-  const int b = u / a.c.Hkv, h = u % a.c.Hkv, g = a.c.g;
-  const ChunkSeq seq = chunk_seq(a.c, b, threadIdx.x == 0 && h == 0 && tile == 0 && split == 0);
-  const int rows = seq.n * g, row0 = tile * M;
-  if (row0 >= rows) return;
-  const ChunkUnit unit = chunk_unit(a.c.L, u);
-  const int last_row = min(row0 + M, rows) - 1;
-  const int end = __builtin_amdgcn_readfirstlane((int)min(seq.pos + last_row / g + 1, (int64_t)INT32_MAX));   // slots that the tile's rows see
-
+  AttentionWork<T, D, kAtThreads, M, KT> w;
+  if (!w.begin(a, s_table)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW, col = lane & 31, half = lane >> 5;
 
-  // ---- does the unit hold the chunk, and do its blocks lie in the pools
-  int why = chunk_held(a.c.L, unit, u, seq.pos + seq.n) ? 0 : SQA_ERR_STATE;
-  if (!why && unit.table) {
-    int outside = 0;
-    for (int i = tid; i < (end + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS; i += kAtThreads) {
-      const int blk = unit.table[i];
-      s_table[i] = blk;
-      outside |= (unsigned)blk >= (unsigned)a.c.L.n_blocks;
-    }
-    if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
-  }
-  auto place = [&](int r, int& t, int& head) { t = r / g; head = h * g + r % g; };
-  T* const out = static_cast<T*>(a.out);
-  if (why) {
-    if (split) return;
-    if (tid == 0 && a.c.status) *a.c.status = why;
-    for (int i = tid; i < (last_row + 1 - row0) * R::PPR; i += kAtThreads) {
-      int t, head;
-      place(row0 + i / R::PPR, t, head);
-      st16(out + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + i % R::PPR * R::E, make_uint4(0, 0, 0, 0));
-      if (a.lse && i % R::PPR == 0) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = -INFINITY;
-    }
-    return;
-  }
-
-  // ---- the slots of this workgroup, in tiles of KT
-  const int nt = (end + KT - 1) / KT, per = (nt + a.splits - 1) / a.splits;
-  const int parts = (nt + per - 1) / per;
-  if (split >= parts) return;
-  const int tile0 = split * per, tile1 = min(tile0 + per, nt);
-
   // ---- this lane's query row
-  const int r = row0 + 32 * rw + col;
-  const bool mine = r < rows;
+  const int r = w.row0 + 32 * rw + col;
+  const bool mine = r < w.rows;
   int t, head;
-  place(mine ? r : row0, t, head);
-  const int see = (int)(seq.pos + t);                                                    // the last slot that the row sees
-  const int see_all = (int)(seq.pos + min(row0 + 32 * rw, last_row) / g);                // ... that all of the wave's rows see
-  const int see_all_tile = (int)(seq.pos + row0 / g);                                    // ... all of the workgroup's
+  w.place(mine ? r : w.row0, t, head);
+  const int see = (int)(w.pos + t);                                                    // the last slot that the row sees
+  const int see_all = (int)(w.pos + min(w.row0 + 32 * rw, w.last_row) / w.g);                // ... that all of the wave's rows see
+  const int see_all_tile = (int)(w.pos + w.row0 / w.g);                                    // ... all of the workgroup's
   Frag<T, D> q;
   {
-    const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)b * a.c.Hq + head) * a.c.T + t) * D);
+    const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)w.b * a.c.Hq + head) * a.c.T + t) * D);
 #pragma unroll
     for (int s = 0; s < q.NS; ++s) q.p[s] = mine ? ld16(src + (2 * s + half) * 16) : make_uint4(0, 0, 0, 0);
+    arrived(q);
   }
 
   // ---- copies of one tile: each wave the rows wave KT/4 .. of K and of V
@@ -140,8 +266,8 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
 #pragma unroll
     for (int i = 0; i < KT / 4 / R::RPI; ++i) {
       const int rr = wave * (KT / 4) + i * R::RPI, row = rr + lane / R::PPR;
-      const int slot = min(tl * KT + row, end - 1);
-      const int64_t at = unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit.first + slot;
+      const int slot = min(tl * KT + row, w.end - 1);
+      const int64_t at = w.unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : w.unit.first + slot;
       fetch16(Kp + at * R::RB + (((lane % R::PPR) ^ R::k_swizzle(row)) << 4), dst + rr * R::RB);
       fetch16(Vp + at * R::RB + (((lane % R::PPR) ^ R::v_swizzle(row)) << 4), dst + C::TILE + rr * R::RB);
     }
@@ -152,12 +278,12 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
   for (int e = 0; e < NB; ++e) o[e] = f32x16_t{};
   float m = -FLT_MAX, l = 0.f;                       // (finite: a row that sees nothing yet has no exp(inf - inf))
 
-  fetch(tile0, 0);
-  for (int tl = tile0; tl < tile1; ++tl) {
-    const int buf = (tl - tile0) & 1;
+  fetch(w.tile0, 0);
+  for (int tl = w.tile0; tl < w.tile1; ++tl) {
+    const int buf = (tl - w.tile0) & 1;
     fetched();
     __syncthreads();
-    if (tl + 1 < tile1) fetch(tl + 1, buf ^ 1);
+    if (tl + 1 < w.tile1) fetch(tl + 1, buf ^ 1);
     const char* const Kt = s_stage + buf * 2 * C::TILE;
     const char* const Vt = Kt + C::TILE;
     const int key0 = kw * (KT / KW);
@@ -209,7 +335,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
 
     // A slot that a row does not see has probability 0, but 0 x NaN is NaN: where some rows do not see all of the tile, its
     // values that are not finite are added to the sums of the rows that see them one by one, and are 0 for the product.
-    if (tl * KT + KT - 1 > see_all_tile && __syncthreads_or(odd_values<T, C::TILE, false>(s_stage + buf * 2 * C::TILE + C::TILE))) {
+    if (tl * KT + KT - 1 > see_all_tile && __syncthreads_or(odd_values<T, C::TILE, kAtThreads, false>(s_stage + buf * 2 * C::TILE + C::TILE))) {
 #pragma unroll 1
       for (int k = 0; k < 32 * KB; ++k) {
         const int row = key0 + k;
@@ -227,7 +353,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
           }
       }
       __syncthreads();
-      odd_values<T, C::TILE, true>(s_stage + buf * 2 * C::TILE + C::TILE);
+      odd_values<T, C::TILE, kAtThreads, true>(s_stage + buf * 2 * C::TILE + C::TILE);
       __syncthreads();
     }
 #pragma unroll
@@ -263,140 +389,260 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
       }
     }
   }
-  l = other_half_sum(l);
-
-  // ---- the waves of the same rows join: their sums as one list of 32 rows each in LDS, 16-byte pieces exchanged by the row
-  __syncthreads();
-  if (half == 0) { s_m[kw][32 * rw + col] = m; s_l[kw][32 * rw + col] = l; }
-  if constexpr (KW > 1) {
-    __syncthreads();
-    float top = s_m[0][32 * rw + col];
-#pragma unroll
-    for (int k = 1; k < KW; ++k) top = fmaxf(top, s_m[k][32 * rw + col]);
-    const float w = exp2_fast((m - top) * a.scale);
-#pragma unroll
-    for (int e = 0; e < NB; ++e) o[e] *= w;
-  }
-  constexpr int PP = D / 4;                          // pieces of a row of sums
-  float4* const mine4 = reinterpret_cast<float4*>(s_stage) + (kw * M + 32 * rw + col) * PP;
-#pragma unroll
-  for (int i = 0; i < 16; i += 4)
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int e = 0; e < NB; ++e) mine4[(8 * e + c_row(i, half) / 4) ^ (col & 15)] = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
-    } else if constexpr (NB == 4) {
-#pragma unroll
-      for (int x = i; x < i + 4; ++x) mine4[c_row(x, half) ^ (col & 15)] = make_float4(o[0][x], o[1][x], o[2][x], o[3][x]);
-    } else {
-#pragma unroll
-      for (int x = i; x < i + 4; x += 2) mine4[(c_row(x, half) / 2) ^ (col & 15)] = make_float4(o[0][x], o[1][x], o[0][x + 1], o[1][x + 1]);
-    }
-  __syncthreads();
-  auto joined = [&](int row, float& mm, float& ll) {
-    mm = s_m[0][row];
-#pragma unroll
-    for (int k = 1; k < KW; ++k) mm = fmaxf(mm, s_m[k][row]);
-    ll = 0.f;
-#pragma unroll
-    for (int k = 0; k < KW; ++k) ll += s_l[k][row] * (KW > 1 ? exp2_fast((s_m[k][row] - mm) * a.scale) : 1.f);
-  };
-  auto piece4 = [&](int row, int p) {
-    float4 v = reinterpret_cast<const float4*>(s_stage)[row * PP + (p ^ (row & 15))];
-#pragma unroll
-    for (int k = 1; k < KW; ++k) {
-      const float4 x = reinterpret_cast<const float4*>(s_stage)[(k * M + row) * PP + (p ^ (row & 15))];
-      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-    }
-    return v;
-  };
-  auto store4 = [&](int row, int p, float4 v, float mm, float ll) {
-    int tt, hh;
-    place(row0 + row, tt, hh);
-    const float inv = 1.f / ll;
-    T* dst = out + (((int64_t)b * a.c.T + tt) * a.c.Hq + hh) * D + 4 * p;
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint2*>(dst) = make_uint2(f32_to_bf16_bits(v.x * inv) | (f32_to_bf16_bits(v.y * inv) << 16),
-                                                  f32_to_bf16_bits(v.z * inv) | (f32_to_bf16_bits(v.w * inv) << 16));
-    else
-      *reinterpret_cast<float4*>(dst) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-    if (p == 0 && a.lse) a.lse[((int64_t)b * a.c.Hq + hh) * a.c.T + tt] = 0.6931471805599453f * fmaf(mm, a.scale, log2f(ll));
-  };
-  const int live = (last_row + 1 - row0) * PP;
-  if (parts == 1) {
-    for (int i = tid; i < live; i += kAtThreads) {
-      float mm, ll;
-      joined(i / PP, mm, ll);
-      store4(i / PP, i % PP, piece4(i / PP, i % PP), mm, ll);
-    }
-    return;
-  }
-
-  // ---- ... and the workgroups of the same rows
-  constexpr int REC = D / 2 + 1;
-  float2* const rec = a.part + (item * a.splits) * M * REC;
-  for (int i = tid; i < live; i += kAtThreads) {
-    const int row = i / PP, p = i % PP;
-    float2* dst = rec + ((int64_t)split * M + row) * REC;
-    const float4 v = piece4(row, p);
-    hand_over(dst + 2 * p, make_float2(v.x, v.y));
-    hand_over(dst + 2 * p + 1, make_float2(v.z, v.w));
-    if (p == 0) {
-      float mm, ll;
-      joined(row, mm, ll);
-      hand_over(dst + D / 2, make_float2(mm, ll));
-    }
-  }
-  if (!last_to_arrive(a.count + item, parts, &s_word)) return;
-  for (int i = tid; i < live; i += kAtThreads) {
-    const int row = i / PP, p = i % PP;
-    float mm = -FLT_MAX, ll = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < parts; ++k) mm = fmaxf(mm, handed_over(rec + ((int64_t)k * M + row) * REC + D / 2).x);
-    for (int k = 0; k < parts; ++k) {
-      const float2* src = rec + ((int64_t)k * M + row) * REC;
-      const float2 ml = handed_over(src + D / 2), x = handed_over(src + 2 * p), y = handed_over(src + 2 * p + 1);
-      const float w = exp2_fast((ml.x - mm) * a.scale);
-      ll = fmaf(ml.y, w, ll);
-      v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(y.x, w, v.z); v.w = fmaf(y.y, w, v.w);
-    }
-    store4(row, p, v, mm, ll);
-  }
+  w.template finish<KW>(a, s_stage, s_m, s_l, &s_word, rw, kw, o, m, l);
 }
 
-struct AttentionPlan { int rw, tiles, splits; };
+// The same for many rows in bf16: 8 waves of 32 rows, two per SIMD, that take turns.  A wave's work on a tile of 64 slots has two parts of
+// about equal length, products (K.Q^T of this tile and V^T.P^T of the one before) and softmax; waves 4-7 are one part
+// behind waves 0-3, so that of the two waves of a SIMD one keeps the matrix cores busy and the other one the vector ALUs.  A barrier
+// after each part keeps it so.  K of tile j + 1 and V of tile j are requested when the first waves begin the products of tile j, and
+// have a whole round to arrive.
+constexpr int kWideThreads = 512;
+constexpr int kWideRows = 256;
+constexpr int kWideSlots = 64;
+
+__device__ __forceinline__ void part_done() { asm volatile("s_barrier" ::: "memory"); }
+
+template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
+  using T = bf16_t;
+  using R = TileRows<T, D>;
+  constexpr int NB = D / 32, NS = Frag<T, D>::NS, TILE = kWideSlots * R::RB;
+  extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // K, K', V, V'; at the end all rows' sums
+  __shared__ float s_m[1][kWideRows], s_l[1][kWideRows];
+  __shared__ int s_word;
+  int* const s_table = reinterpret_cast<int*>(s_stage + kWideRows * D * 4);
+  AttentionWork<T, D, kWideThreads, kWideRows, kWideSlots> w;
+  if (!w.begin(a, s_table)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const bool late = wave >= 4;
+
+  // ---- this lane's query row
+  const int r = w.row0 + 32 * wave + col;
+  const bool mine = r < w.rows;
+  int t, head;
+  w.place(min(r, w.last_row), t, head);
+  const int see = (int)(w.pos + t);                                                                                            // the last slot that the row sees
+  const int see_all = __builtin_amdgcn_readfirstlane((int)(w.pos + min(w.row0 + 32 * wave, w.last_row) / w.g));                // ... that all of the wave's rows see
+  const int see_any = __builtin_amdgcn_readfirstlane((int)(w.pos + min(w.row0 + 32 * wave + 31, w.last_row) / w.g));           // ... that any of them sees
+  Frag<T, D> q;
+  {
+    const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)w.b * a.c.Hq + head) * a.c.T + t) * D);
+#pragma unroll
+    for (int x = 0; x < NS; ++x) q.p[x] = mine ? ld16(src + (2 * x + half) * 16) : make_uint4(0, 0, 0, 0);
+    arrived(q);
+  }
+
+  // ---- copies: each wave 8 rows of K and of V of a tile (they lie in one block)
+  const uint32_t lds0 = lds_at(s_stage);
+  auto copy = [&](const void* from, int tl, uint32_t dst, bool v) {
+#pragma unroll
+    for (int i = 0; i < 8 / R::RPI; ++i) {
+      const int rr = 8 * wave + i * R::RPI, row = rr + lane / R::PPR;
+      const int slot = min(tl * kWideSlots + row, w.end - 1);
+      const int64_t at = w.unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : w.unit.first + slot;
+      fetch16(static_cast<const char*>(from) + at * R::RB + (((lane % R::PPR) ^ (v ? R::v_swizzle(row) : R::k_swizzle(row))) << 4), dst + rr * R::RB);
+    }
+  };
+  auto request = [&](int j) {                        // what the round of tile j asks for
+    if (w.tile0 + j + 1 < w.tile1) copy(a.c.L.K, w.tile0 + j + 1, lds0 + ((j + 1) & 1) * TILE, false);
+    copy(a.c.L.V, w.tile0 + j, lds0 + (2 + (j & 1)) * TILE, true);
+  };
+
+  // ---- the lane's places in a tile of K and of V
+  int k_at[NS], v_at[NB];
+#pragma unroll
+  for (int x = 0; x < NS; ++x) k_at[x] = col * R::RB + (((2 * x + half) ^ R::k_swizzle(col)) << 4);
+  {
+    const int row = 4 * half + (lane & 15) / 4;
+#pragma unroll
+    for (int e = 0; e < NB; ++e)
+      v_at[e] = row * R::RB + (((4 * e + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ R::v_swizzle(row)) << 4) + (lane & 1) * 8;
+  }
+
+  f32x16_t o[NB], s[2];
+  bf16x8_t p[4];
+#pragma unroll
+  for (int e = 0; e < NB; ++e) o[e] = f32x16_t{};
+  float m = -FLT_MAX, l = 0.f;                       // m: a reference that a row's largest logit is near, not always that logit
+
+  auto keys = [&](int j) {                           // s = K.Q^T of tile j
+    const char* const Kt = s_stage + (j & 1) * TILE;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      uint4 k[NS];
+#pragma unroll
+      for (int x = 0; x < NS; ++x) k[x] = *reinterpret_cast<const uint4*>(Kt + k_at[x] + 32 * kb * R::RB);
+      s[kb] = f32x16_t{};
+#pragma unroll
+      for (int x = 0; x < NS; ++x) mma_piece<T>(k[x], q.p[x], s[kb]);
+    }
+  };
+  // edge: not all rows of the workgroup see all slots of the tile
+  auto values = [&](int j, auto edge) {              // o += V^T.P^T of tile j
+    const char* const Vt = s_stage + (2 + (j & 1)) * TILE;
+    const int first = (w.tile0 + j) * kWideSlots;
+    // a slot that a row does not see has probability 0, but 0 x NaN is NaN (see above)
+    bool any_odd = false;
+    if constexpr (decltype(edge)::value)
+      if (first + kWideSlots - 1 > see_all) {
+        uint32_t odd = 0;
+#pragma unroll 4
+        for (int i = 0; i < TILE / 1024; ++i) {
+          const uint4 v = *reinterpret_cast<const uint4*>(Vt + i * 1024 + lane * 16);
+          odd |= odd_mask(v.x) | odd_mask(v.y) | odd_mask(v.z) | odd_mask(v.w);
+        }
+        any_odd = __any(odd != 0);
+      }
+    if (any_odd) {
+#pragma unroll 1
+      for (int k = 0; k < kWideSlots; ++k) {
+        const bool sees = first + k <= see;
+        const char* const row = Vt + k * R::RB + 8 * half;
+        const int swz = R::v_swizzle(k) << 4;
+#pragma unroll
+        for (int e = 0; e < NB; ++e)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + ((64 * e + 4 * i) ^ swz));
+            o[e][i] += sees && odd_mask(v.x << 16) ? bf16_lo(v.x) : 0.f;
+            o[e][i + 1] += sees && odd_mask(v.x & 0xffff0000u) ? bf16_hi(v.x) : 0.f;
+            o[e][i + 2] += sees && odd_mask(v.y << 16) ? bf16_lo(v.y) : 0.f;
+            o[e][i + 3] += sees && odd_mask(v.y & 0xffff0000u) ? bf16_hi(v.y) : 0.f;
+          }
+      }
+    }
+    auto product = [&](auto clean) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+          const char* at = Vt + v_at[e] + 16 * ks * R::RB;
+          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at));
+          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * R::RB));
+          uint4 v = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          if constexpr (decltype(clean)::value) {
+            v.x &= ~odd_mask(v.x); v.y &= ~odd_mask(v.y); v.z &= ~odd_mask(v.z); v.w &= ~odd_mask(v.w);
+          }
+          o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[ks], o[e], 0, 0, 0);
+        }
+    };
+    if (any_odd) product(std::true_type{});
+    else product(std::false_type{});
+  };
+  auto softmax = [&](int j, auto edge) {
+    if constexpr (decltype(edge)::value) {
+      const int first = (w.tile0 + j) * kWideSlots;
+      if (first + kWideSlots - 1 > see_all) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (first + 32 * kb + c_row(i, half) > see) s[kb][i] = -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+    top = other_half_max(top);
+    if (__any(top > m + a.near)) {                   // the reference moves when a logit is 2^8 times beyond it: seldom after the first tiles
+      const float to = fmaxf(m, top), keep = exp2_fast((m - to) * a.scale);
+      m = to;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < NB; ++e) o[e] *= keep;
+    }
+    float off = m * a.scale;
+    // s scale - off in one operation is off by the rounding of `off`: far from 0 the difference is taken first
+    if (__any(fabsf(off) > kFarLogit)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) s[kb] -= m;
+      off = 0.f;
+    }
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = exp2_fast(fmaf(s[kb][i], a.scale, -off)), y = exp2_fast(fmaf(s[kb][i + 1], a.scale, -off));
+        l0 += x; l1 += y;
+        p[2 * kb + i / 8][i % 8] = (__bf16)x; p[2 * kb + i / 8][i % 8 + 1] = (__bf16)y;
+      }
+    l += l0 + l1;
+  };
+  const int n = w.tile1 - w.tile0;
+  const int see_all_tile = __builtin_amdgcn_readfirstlane((int)(w.pos + w.row0 / w.g));
+  const int whole = min(max((see_all_tile + 1) / kWideSlots - w.tile0, 0), n);        // the first tiles, that every row sees all of
+  auto round = [&](int j, auto edge) {
+    constexpr bool E = decltype(edge)::value;
+    auto seen = [&](int i) { return !E || (w.tile0 + i) * kWideSlots <= see_any; };
+    if (!late) request(j);
+    if (seen(j)) keys(j);
+    if (j > 0 && seen(j - 1)) values(j - 1, edge);
+    if (late) fetched();
+    part_done();
+    if (late && j + 1 < n) request(j + 1);
+    if (seen(j)) softmax(j, edge);
+    if (!late) fetched();
+    part_done();
+  };
+  copy(a.c.L.K, w.tile0, lds0, false);
+  fetched();
+  part_done();
+  if (late) {
+    request(0);
+    part_done();
+  }
+  int j = 0;
+  for (; j < whole; ++j) round(j, std::false_type{});
+  for (; j < n; ++j) round(j, std::true_type{});
+  if ((w.tile0 + n - 1) * kWideSlots <= see_any) values(n - 1, std::true_type{});
+  if (!late) part_done();
+  w.template finish<1>(a, s_stage, s_m, s_l, &s_word, wave, 0, o, m, l);
+}
+
+struct AttentionPlan { int rw, tiles, splits; };     // rw: 32-row blocks of a workgroup
 // (rows of 512 bytes have no form for 32 rows: its tiles would not fit the LDS)
-static int attention_rw(int rows, bool rows_of_512) { return rows <= 32 && !rows_of_512 ? 1 : (rows <= 64 ? 2 : 4); }
+static int attention_rw(int rows, bool bf16, int D) {
+  if (rows > 128 && bf16) return 8;
+  return rows <= 32 && (bf16 || D == 64) ? 1 : (rows <= 64 ? 2 : 4);
+}
+static int attention_items(int rw) { return rw == 8 ? kAtItems / 2 : kAtItems; }
 static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots) {
   AttentionPlan p;
   const int rows = T * (Hq / Hkv);
-  p.rw = attention_rw(rows, dt == SQA_F32 && D == 128);
+  p.rw = attention_rw(rows, dt == SQA_BF16, D);
   p.tiles = (rows + 32 * p.rw - 1) / (32 * p.rw);
   const int64_t items = (int64_t)B * Hkv * p.tiles;
-  int64_t s = kAtItems / items;
+  int64_t s = attention_items(p.rw) / items;
   s = s > slots / 256 ? slots / 256 : s;             // (a workgroup's start and the join cost what some hundred slots do)
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }
-// (any T' <= T, any length: items x splits <= kAtItems where there are splits)
-size_t chunk_attention_scratch(int B, int T, int Hq, int Hkv, int D, int64_t slots) {
-  (void)B; (void)slots;
-  return (size_t)kAtItems * 32 * attention_rw(T * (Hq / Hkv), D == 128) * (D / 2 + 1) * sizeof(float2);
+// (any T' <= T, any length, either type: items x splits <= attention_items() where there are splits)
+size_t chunk_attention_scratch(int T, int Hq, int Hkv, int D) {
+  const int rw = attention_rw(T * (Hq / Hkv), false, D);
+  return (size_t)kAtItems * 32 * rw * (D / 2 + 1) * sizeof(float2);
 }
 
-template <typename T, int D, int RW, int KT>
-static sqa_status launch_attention(const AttentionArgs& a, hipStream_t st) {
-  using C = AttentionTile<T, D, RW, KT>;
-  const auto fn = chunk_attention_kernel<T, D, RW, KT>;
-  size_t lds = C::STAGE;
+static sqa_status start_attention(void (*fn)(AttentionArgs), int threads, size_t lds, const AttentionArgs& a, hipStream_t st) {
   if (a.c.L.block_table) lds += (size_t)(a.c.L.blocks_per_unit + 3) / 4 * 16;
   SQA_HIP_CHECK(allow_dynamic_lds(reinterpret_cast<const void*>(fn), lds));
   const int64_t work = (int64_t)a.c.B * a.c.Hkv * a.tiles * a.splits;
-  fn<<<(unsigned)xcd_grid(work), kAtThreads, lds, st>>>(a);
+  fn<<<(unsigned)xcd_grid(work), threads, lds, st>>>(a);
   SQA_HIP_CHECK(hipGetLastError());
   return SQA_OK;
 }
+template <typename T, int D, int RW, int KT>
+static sqa_status launch_attention(const AttentionArgs& a, hipStream_t st) {
+  return start_attention(chunk_attention_kernel<T, D, RW, KT>, kAtThreads, AttentionTile<T, D, RW, KT>::STAGE, a, st);
+}
 template <typename T, int D>
 static sqa_status launch_attention(int rw, const AttentionArgs& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (rw == 8) return start_attention(chunk_attention_wide_kernel<D>, kWideThreads, kWideRows * D * 4, a, st);
   constexpr bool wide = D * sizeof(T) == 512;        // rows of 512 bytes: half the slots
   if (rw == 4) return launch_attention<T, D, 4, wide ? 32 : 64>(a, st);
   if constexpr (wide) return launch_attention<T, D, 2, 64>(a, st);
@@ -408,8 +654,8 @@ static sqa_status launch_attention(int rw, const AttentionArgs& a, hipStream_t s
 extern "C" size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int Hq, int Hkv, int D) {
   sqa_status why;
   if (!layer || sqa::bad_layer(*layer, &why) || sqa::bad_chunk_shape(B, T, Hq, Hkv, D, 0, nullptr)) return 0;
-  const size_t x = sqa::chunk_attention_scratch(B, T, Hq, Hkv, D, layer->capacity);
-  const size_t y = sqa::chunk_scores_scratch(B, T, Hq, Hkv, D, layer->capacity);
+  const size_t x = sqa::chunk_attention_scratch(T, Hq, Hkv, D);
+  const size_t y = sqa::chunk_scores_scratch();
   return (sqa::kChunkCounterBytes + (x > y ? x : y) + 255) / 256 * 256;
 }
 
@@ -435,6 +681,7 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
   const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, uniform ? (int64_t)new_pos + T : layer->capacity);
+  a.near = 8.f / a.scale;
   a.tiles = p.tiles; a.splits = p.splits;
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -64,6 +64,12 @@ template <typename T, int D> struct Frag {
   uint4 p[NS];
 };
 
+// The compiler waits for the row's loads here, not at their first use: inside a loop that wait would be for all copies in flight.
+template <typename T, int D> __device__ __forceinline__ void arrived(Frag<T, D>& f) {
+#pragma unroll
+  for (int i = 0; i < Frag<T, D>::NS; ++i) asm volatile("" : "+v"(f.p[i].x), "+v"(f.p[i].y), "+v"(f.p[i].z), "+v"(f.p[i].w));
+}
+
 // c += a.b over the contraction slots of one piece of each lane
 template <typename T> __device__ __forceinline__ void mma_piece(const uint4& a, const uint4& b, f32x16_t& c);
 template <> __device__ __forceinline__ void mma_piece<bf16_t>(const uint4& a, const uint4& b, f32x16_t& c) {

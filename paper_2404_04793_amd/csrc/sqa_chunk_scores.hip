@@ -28,7 +28,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const ScoresArgs a) {
   using R = TileRows<T, D>;
   constexpr int TILE = kScoreRows * R::RB;
-  extern __shared__ char s_stage[];                 // two tiles of rows
+  extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // two tiles of rows
   __shared__ float s_lse[2][kScoreRows];            // in powers of two; of rows that are none: infinity
   __shared__ int s_see[2][kScoreRows];              // the last slot that a row sees
   __shared__ float s_sum[kScoreSlots];
@@ -77,6 +77,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
     const char* src = static_cast<const char*>(a.c.L.K) + at * R::RB;
 #pragma unroll
     for (int x = 0; x < k.NS; ++x) k.p[x] = ld16(src + (2 * x + half) * 16);
+    arrived(k);
   }
   const int64_t head0 = (int64_t)b * a.c.Hq + h * g;
   const char* const Q = static_cast<const char*>(a.q) + head0 * a.c.T * R::RB;
@@ -150,7 +151,7 @@ static int scores_splits(int B, int T, int Hq, int Hkv, int tiles) {
   return s < 1 ? 1 : (int)s;
 }
 // (any length: items x splits <= kScoreItems where there are splits)
-size_t chunk_scores_scratch(int, int, int, int, int, int64_t) { return (size_t)kScoreItems * kScoreSlots * sizeof(float); }
+size_t chunk_scores_scratch() { return (size_t)kScoreItems * kScoreSlots * sizeof(float); }
 
 template <typename T, int D>
 static sqa_status launch_scores(const ScoresArgs& a, hipStream_t st) {
