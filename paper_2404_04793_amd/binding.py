@@ -73,10 +73,6 @@ class HeadPrepStruct(C.Structure):
     """Mirror of sqa_head_prep."""
     _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("rope", C.c_void_p), ("eps", C.c_float),
                 ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
-    weights, rope_rows = (), None                              # the tensors behind the pointers
-
-    def tensors(self):
-        return (*self.weights, self.rope_rows)
 
 
 ORDER = {"evict_then_attend": 0, "attend_then_evict": 1}
@@ -132,17 +128,16 @@ _lib.sqa_kept_idx_sorted.argtypes = [_LCp, _i, _i, _vp, _vp]
 _lib.sqa_decode_plan.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, _i, C.POINTER(DecodePlanInfo), C.POINTER(DecodeLayerPlan)]
 _lib.sqa_decode_plan_waves.restype = C.c_int32
 _lib.sqa_decode_plan_waves.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, _i]
-_TRp, _HPp = C.POINTER(TokenRowsStruct), C.POINTER(HeadPrepStruct)
 _lib.sqa_qk_norm_rope.restype = _i
-_lib.sqa_qk_norm_rope.argtypes = [_TRp, _TRp, _i, _i, _i, _i, _i, _i, _HPp, C.c_int32, _vp, _vp, _vp, _BOp]
+_lib.sqa_qk_norm_rope.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, _vp, C.c_int32, _vp, _vp, _vp, _vp]
 _lib.sqa_chunk_append.restype = _i
-_lib.sqa_chunk_append.argtypes = [_TRp, _TRp, _TRp, _i, _i, _i, _i, _i, _i, _HPp, C.c_int32, _vp, _vp, _vp, _BOp]
+_lib.sqa_chunk_append.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, C.c_int32, _vp, _vp, _vp, _vp]
 _lib.sqa_chunk_workspace_bytes.restype = _sz
 _lib.sqa_chunk_workspace_bytes.argtypes = [_vp, _i, _i, _i, _i, _i]
 _lib.sqa_chunk_attention.restype = _i
-_lib.sqa_chunk_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _BOp]
+_lib.sqa_chunk_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
 _lib.sqa_chunk_scores.restype = _i
-_lib.sqa_chunk_scores.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _sz, _vp, _BOp]
+_lib.sqa_chunk_scores.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _sz, _vp, _vp]
 _lib.sqa_block_pool_create.argtypes = [C.c_int32]
 _lib.sqa_block_pool_create.restype = _vp
 _lib.sqa_block_pool_destroy.argtypes = [_vp]
@@ -590,45 +585,53 @@ def rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, device="cuda:0")
 def head_prep(q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
               rope: Optional[torch.Tensor] = None, interleaved: bool = False) -> HeadPrepStruct:
     """sqa_head_prep: weights [D] of the heads' norms, a rope_table (kept alive with the result)."""
-    for w in (q_weight, k_weight):
-        if w is not None and (w.dim() != 1 or not w.is_contiguous()):
-            raise TypeError("norm weights are contiguous tensors [D]")
+    tensors = [t for t in (q_weight, k_weight, rope) if t is not None]
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if any(w.dim() != 1 or not w.is_contiguous() for w in weights) or len({(w.dtype, w.shape[0]) for w in weights}) > 1:
+        raise TypeError("norm weights are contiguous tensors [D] of one dtype")
     if rope is not None and (rope.dtype != torch.float32 or rope.dim() != 2 or not rope.is_contiguous()):
         raise TypeError("rope is a contiguous fp32 tensor [n_pos, rot_dim]")
+    if len({t.get_device() for t in tensors}) > 1:
+        raise ValueError("weights and rope on different devices")
     p = HeadPrepStruct(_ptr(q_weight), _ptr(k_weight), _ptr(rope), float(eps), 0 if rope is None else rope.shape[0],
                        0 if rope is None else rope.shape[1], int(interleaved))
-    p.weights, p.rope_rows = tuple(w for w in (q_weight, k_weight) if w is not None), rope
+    p.tensors = tensors
+    p.of = (weights[0].dtype, weights[0].shape[0]) if weights else None
+    p.device = tensors[0].get_device() if tensors else None
     return p
 
 
-def _on_device(*tensors: Optional[torch.Tensor]) -> None:
-    """The library runs on the current device's stream: tensors of the host or of another device are refused."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != _get_device()):
-            raise ValueError("a tensor is not on the current device")
+# (The calls below are kept short, their checks among them: in a model that makes them once per layer, the host's part of a small
+# chunk's call is longer than its kernel.)
 
-
-def _token_rows(t: torch.Tensor) -> TokenRowsStruct:
-    """[B, T, H, D], dense within a token: a projection's output, a part of a packed one, or a slice of a longer prompt."""
-    s = t.stride()
-    if t.dim() != 4 or (s[3] != 1 and t.shape[3] != 1) or (s[2] != t.shape[3] and t.shape[2] != 1):
+def _token_rows(t: torch.Tensor, D: int) -> array:
+    """sqa_token_rows of [B, T, H, D], dense within a token: a projection's output, a part of a packed one, or a slice of a
+    longer prompt."""
+    seq, row, head, one = t.stride()
+    if head != D and t.shape[2] != 1 or one != 1:
         raise TypeError("heads of a token lie one after the other: [B, T, H, D] with strides (.., .., D, 1)")
-    return TokenRowsStruct(t.data_ptr(), s[0], s[1])
+    return array("q", (t.data_ptr(), seq, row))
 
 
-def _check_prep(prep: Optional[HeadPrepStruct], dtype: torch.dtype, D: int):
-    if prep is None:
-        return
-    if any(w.dtype != dtype or w.shape[0] != D for w in prep.weights):
-        raise TypeError("norm weights are [D] tensors of the call's dtype")
-
-
-def _out_like(out: Optional[torch.Tensor], shape, dtype, device) -> torch.Tensor:
-    if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or not out.is_contiguous():
+def _check_out(t: torch.Tensor, shape, dtype) -> None:
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise TypeError("expected a contiguous %s tensor %s" % (dtype, tuple(shape)))
-    return out
+
+
+def _check_device(dev: int, *others: int) -> None:
+    """The library runs on the current device's stream: tensors of the host or of another device are refused."""
+    if dev < 0 or dev != _get_device() or any(o != dev for o in others):
+        raise ValueError("a tensor is not on the current device")
+
+
+def _prep(prep: Optional[HeadPrepStruct], dtype: torch.dtype, D: int, dev: int):
+    if prep is None:
+        return None
+    if prep.of is not None and prep.of != (dtype, D):
+        raise TypeError("norm weights are [D] tensors of the call's dtype")
+    if prep.device is not None and prep.device != dev:
+        raise ValueError("a tensor is not on the current device")
+    return C.addressof(prep)
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: int, prep: Optional[HeadPrepStruct] = None,
@@ -639,30 +642,45 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: 
     some = q if q is not None else k
     if some is None:
         raise TypeError("queries or keys")
-    B, T, _, D = some.shape
-    Hq = q.shape[2] if q is not None else k.shape[2]
-    Hkv = k.shape[2] if k is not None else Hq
-    if q is not None and k is not None and (k.shape[:2] != q.shape[:2] or k.shape[3] != D or k.dtype != q.dtype):
-        raise TypeError("queries and keys of the same tokens, head size and dtype")
-    if q is None and q_out is not None or k is None and k_out is not None:
-        raise TypeError("an output without its input")
-    _check_prep(prep, some.dtype, D)
+    B, T, Hq, D = some.shape
+    Hkv, dtype, dev = Hq, some.dtype, some.get_device()
+    q_rows = k_rows = q_to = k_to = None
     if q is not None:
-        q_out = _out_like(q_out, (B, Hq, T, D), q.dtype, q.device)
+        q_rows = _token_rows(q, D)
+        if q_out is None:
+            q_out = torch.empty((B, Hq, T, D), dtype=dtype, device=q.device)
+        else:
+            _check_out(q_out, (B, Hq, T, D), dtype)
+        q_to = q_out.data_ptr()
+    elif q_out is not None:
+        raise TypeError("an output without its input")
     if k is not None:
-        k_out = _out_like(k_out, (B, Hkv, T, D), k.dtype, k.device)
-    rows = [None if t is None else _token_rows(t) for t in (q, k)]
-    _on_device(q, k, q_out, k_out, *(prep.tensors() if prep is not None else ()))
-    _check(_lib.sqa_qk_norm_rope(rows[0], rows[1], _dt(some), B, T, Hq, Hkv, D, prep, int(new_pos), _ptr(q_out), _ptr(k_out),
-                                 _stream(), opts), "sqa_qk_norm_rope")
+        kB, kT, Hkv, kD = k.shape
+        if kB != B or kT != T or kD != D or k.dtype != dtype:
+            raise TypeError("queries and keys of the same tokens, head size and dtype")
+        k_rows = _token_rows(k, D)
+        if k_out is None:
+            k_out = torch.empty((B, Hkv, T, D), dtype=dtype, device=k.device)
+        else:
+            _check_out(k_out, (B, Hkv, T, D), dtype)
+        k_to = k_out.data_ptr()
+    elif k_out is not None:
+        raise TypeError("an output without its input")
+    how = _prep(prep, dtype, D, dev)
+    _check_device(dev, *[t.get_device() for t in (k, q_out, k_out) if t is not None])
+    code = _lib.sqa_qk_norm_rope(None if q is None else q_rows.buffer_info()[0], None if k is None else k_rows.buffer_info()[0],
+                                 _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos, q_to, k_to, _stream(),
+                                 None if opts is None else C.addressof(opts))
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_qk_norm_rope")
     return q_out, k_out
 
 
-def _layer_at(caches: "LayerCaches", layer: int, dtype: torch.dtype, B: int, Hkv: Optional[int], D: int) -> int:
+def _layer_at(caches: "LayerCaches", layer: int, dtype: torch.dtype, B: int, Hkv: int, D: int) -> int:
     """Address of a layer's record, after a look at whether the call's tensors are the cache's."""
     if not 0 <= layer < caches.L:
         raise IndexError("layer outside the table")
-    if dtype != caches.dtype or B != caches.B or D != caches.D or Hkv not in (None, caches.Hkv):
+    if dtype != caches.dtype or B != caches.B or D != caches.D or Hkv != caches.Hkv:
         raise TypeError("the cache has another dtype, batch, heads or head size")
     return C.addressof(caches.table) + layer * _LC_BYTES
 
@@ -673,27 +691,38 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
     """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
     way; with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
     B, T, Hkv, D = k.shape
-    at = _layer_at(caches, layer, k.dtype, B, Hkv, D)
-    if v.shape != k.shape or v.dtype != k.dtype:
+    dtype, dev, Hq, q_rows, q_to = k.dtype, k.get_device(), Hkv, None, None
+    at = _layer_at(caches, layer, dtype, B, Hkv, D)
+    if v.shape != k.shape or v.dtype != dtype:
         raise TypeError("keys and values of one shape and dtype")
-    Hq = Hkv
+    k_rows, v_rows = _token_rows(k, D), _token_rows(v, D)
+    devices = [v.get_device(), caches.K[layer].get_device()]
     if q is not None:
-        if q.shape[:2] != k.shape[:2] or q.shape[3] != D or q.dtype != k.dtype:
+        qB, qT, Hq, qD = q.shape
+        if qB != B or qT != T or qD != D or q.dtype != dtype:
             raise TypeError("queries and keys of the same tokens, head size and dtype")
-        Hq = q.shape[2]
-        q_out = _out_like(q_out, (B, Hq, T, D), q.dtype, q.device)
+        q_rows = _token_rows(q, D)
+        if q_out is None:
+            q_out = torch.empty((B, Hq, T, D), dtype=dtype, device=q.device)
+        else:
+            _check_out(q_out, (B, Hq, T, D), dtype)
+        q_to = q_out.data_ptr()
+        devices += [q.get_device(), q_out.get_device()]
     elif q_out is not None:
         raise TypeError("an output without its input")
-    _check_prep(prep, k.dtype, D)
-    rows = [None if t is None else _token_rows(t) for t in (q, k, v)]
-    _on_device(q, k, v, q_out, caches.K[layer], *(prep.tensors() if prep is not None else ()))
-    _check(_lib.sqa_chunk_append(*rows, _dt(k), B, T, Hq, Hkv, D, prep, int(new_pos), _ptr(q_out), at, _stream(), opts), "sqa_chunk_append")
+    how = _prep(prep, dtype, D, dev)
+    _check_device(dev, *devices)
+    code = _lib.sqa_chunk_append(None if q is None else q_rows.buffer_info()[0], k_rows.buffer_info()[0], v_rows.buffer_info()[0],
+                                 _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos, q_to, at, _stream(),
+                                 None if opts is None else C.addressof(opts))
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_chunk_append")
     return q_out
 
 
 def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> torch.Tensor:
     """Scratch of chunk_attention and chunk_scores for chunks of up to T tokens, zero-filled."""
-    need = _lib.sqa_chunk_workspace_bytes(_layer_at(caches, layer, caches.dtype, caches.B, None, caches.D), caches.B, T, Hq,
+    need = _lib.sqa_chunk_workspace_bytes(_layer_at(caches, layer, caches.dtype, caches.B, caches.Hkv, caches.D), caches.B, T, Hq,
                                           caches.Hkv, caches.D)
     if need == 0:
         raise SqaError(2, "sqa_chunk_workspace_bytes")
@@ -702,25 +731,30 @@ def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> t
     return ws
 
 
-def _chunk_queries(q: torch.Tensor):
-    if q.dim() != 4 or not q.is_contiguous():
-        raise TypeError("a chunk's queries are a contiguous tensor [B, Hq, T, D]")
-    return q.shape
-
-
 def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                     opts: Optional[BatchOptsStruct] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """q [B, Hq, T, D] of an appended chunk -> (out [B, T, Hq, D], lse [B, Hq, T] fp32)."""
-    B, Hq, T, D = _chunk_queries(q)
-    at = _layer_at(caches, layer, q.dtype, B, None, D)
-    out = _out_like(out, (B, T, Hq, D), q.dtype, q.device)
-    lse = _out_like(lse, (B, Hq, T), torch.float32, q.device)
+    B, Hq, T, D = q.shape
+    dtype, dev, Hkv = q.dtype, q.get_device(), caches.Hkv
+    if not q.is_contiguous():
+        raise TypeError("a chunk's queries are a contiguous tensor [B, Hq, T, D]")
+    at = _layer_at(caches, layer, dtype, B, Hkv, D)
+    if out is None:
+        out = torch.empty((B, T, Hq, D), dtype=dtype, device=q.device)
+    else:
+        _check_out(out, (B, T, Hq, D), dtype)
+    if lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+    else:
+        _check_out(lse, (B, Hq, T), torch.float32)
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
-    _on_device(q, out, lse, workspace, caches.K[layer])
-    _check(_lib.sqa_chunk_attention(_ptr(q), _dt(q), B, T, Hq, caches.Hkv, D, int(new_pos), at, _ptr(out), _ptr(lse),
-                                    _ptr(workspace), workspace.numel(), _stream(), opts), "sqa_chunk_attention")
+    _check_device(dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device())
+    code = _lib.sqa_chunk_attention(q.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, out.data_ptr(), lse.data_ptr(),
+                                    workspace.data_ptr(), workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_chunk_attention")
     return out, lse
 
 
@@ -728,12 +762,17 @@ def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "Laye
                  workspace: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None) -> None:
     """Adds what an appended chunk's queries [B, Hq, T, D] give to every slot to the layer's accumulated scores; lse [B, Hq, T]
     from chunk_attention."""
-    B, Hq, T, D = _chunk_queries(q)
-    at = _layer_at(caches, layer, q.dtype, B, None, D)
-    if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (B, Hq, T):
+    B, Hq, T, D = q.shape
+    dtype, dev, Hkv = q.dtype, q.get_device(), caches.Hkv
+    if not q.is_contiguous():
+        raise TypeError("a chunk's queries are a contiguous tensor [B, Hq, T, D]")
+    at = _layer_at(caches, layer, dtype, B, Hkv, D)
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != (B, Hq, T):
         raise TypeError("lse is a contiguous fp32 tensor [B, Hq, T]")
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
-    _on_device(q, lse, workspace, caches.K[layer])
-    _check(_lib.sqa_chunk_scores(_ptr(q), _ptr(lse), _dt(q), B, T, Hq, caches.Hkv, D, int(new_pos), at, _ptr(workspace),
-                                 workspace.numel(), _stream(), opts), "sqa_chunk_scores")
+    _check_device(dev, lse.get_device(), workspace.get_device(), caches.K[layer].get_device())
+    code = _lib.sqa_chunk_scores(q.data_ptr(), lse.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, workspace.data_ptr(),
+                                 workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_chunk_scores")

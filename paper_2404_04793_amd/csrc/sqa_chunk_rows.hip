@@ -46,26 +46,42 @@ template <> struct Piece<bf16_t> {
   }
 };
 
-// May unit u take the chunk?  The LPR lanes of a row ask together and all get the answer: 0 or an error code.
-// Other waves of the launch may have set the unit's state already: what is asked holds before and after that alike.
+// May a unit take the chunk?  What its LPR lanes (lane c of them) have to know is asked for before the rows are worked on, all at
+// once, and judged afterwards.  Other waves of the launch may have set the unit's state meanwhile: what is asked holds before and
+// after that alike.
+struct UnitAsked { ChunkUnit x; int4 state; int last, newest, block, budget; };
+__device__ __forceinline__ UnitAsked ask_unit(const ChunkArgs& a, int b, int u, const ChunkSeq& s, int c) {
+  UnitAsked k;
+  k.x = chunk_unit(a.L, u);
+  k.state = *reinterpret_cast<const int4*>(a.L.unit_state + (int64_t)u * SQA_ST_WORDS);
+  k.last = s.pos > 0 && s.pos <= k.x.slots ? a.L.pos[k.x.first + s.pos - 1] : 0;
+  k.budget = a.budget_seq ? a.budget_seq[b] : a.L.budget;
+  const int limit = min(k.budget, k.x.slots);
+  k.newest = limit > 0 ? a.L.pos[k.x.first + limit - 1] : 0;
+  const int64_t entry = s.pos / SQA_BLOCK_SLOTS + c;
+  k.block = k.x.table && entry <= (s.pos + s.n - 1) / SQA_BLOCK_SLOTS && entry < a.L.blocks_per_unit ? k.x.table[entry] : 0;
+  return k;
+}
+// 0 or an error code, the same in all LPR lanes
 template <int LPR>
-__device__ __forceinline__ int may_append(const ChunkArgs& a, const ChunkUnit& x, int b, int u, const ChunkSeq& s, int c) {
-  int budget = a.L.budget;
-  if (a.budget_seq) {
-    budget = a.budget_seq[b];
-    if (budget < 1 || budget > a.L.budget) return SQA_ERR_BUDGET;
-  }
-  const int limit = min(budget, x.slots);
-  if (!chunk_held(a.L, x, u, s.pos)) return SQA_ERR_STATE;
+__device__ __forceinline__ int judge_unit(const ChunkArgs& a, const UnitAsked& k, const ChunkSeq& s, int c) {
+  if (a.budget_seq && (k.budget < 1 || k.budget > a.L.budget)) return SQA_ERR_BUDGET;
+  const int limit = min(k.budget, k.x.slots), len = k.state.x;
+  if (s.pos > k.x.slots || len < s.pos || k.state.y != 0 || (s.pos > 0 && k.last != s.pos - 1)) return SQA_ERR_STATE;
   if (s.pos + s.n > limit) return SQA_ERR_CAPACITY;
-  int bad = 0;
-  // a full unit that is taken back may have evicted before: slot by slot
-  if (a.L.unit_state[(int64_t)u * SQA_ST_WORDS + SQA_ST_LEN] >= limit)
-    for (int64_t i = c; i < s.pos; i += LPR) bad |= a.L.pos[x.first + i] != i;
-  int outside = 0;
-  if (x.table)
-    for (int i = (int)(s.pos / SQA_BLOCK_SLOTS) + c; i <= (int)((s.pos + s.n - 1) / SQA_BLOCK_SLOTS); i += LPR)
-      outside |= (unsigned)x.table[i] >= (unsigned)a.L.n_blocks;
+  // A full unit may have evicted, and then be taken back to its first tokens.  None of the slots from budget / 2 on then holds its own
+  // position: `last` tells if it is one of them, and the newest if this call does not write it; the slots before, one by one.
+  int bad = 0, outside = 0;
+  if (len >= limit) {
+    if (s.pos + s.n < limit) bad = k.newest != limit - 1;
+    if (2 * s.pos <= limit)
+      for (int64_t i = c; i < s.pos; i += LPR) bad |= a.L.pos[k.x.first + i] != i;
+  }
+  if (k.x.table) {
+    outside = (unsigned)k.block >= (unsigned)a.L.n_blocks;
+    for (int i = (int)(s.pos / SQA_BLOCK_SLOTS) + LPR + c; i <= (int)((s.pos + s.n - 1) / SQA_BLOCK_SLOTS); i += LPR)
+      outside |= (unsigned)k.x.table[i] >= (unsigned)a.L.n_blocks;
+  }
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) { bad |= __shfl_xor(bad, o, LPR); outside |= __shfl_xor(outside, o, LPR); }
   return bad ? SQA_ERR_STATE : (outside ? SQA_ERR_SHAPE : 0);
@@ -105,6 +121,9 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
 #pragma unroll
     for (int i = 0; i < U; ++i) v[i] = ld16(static_cast<const T*>(a.v.data) + vat + min(i, nt - 1) * a.v.row_stride);
   }
+  const int u = b * a.c.Hkv + min(h, heads - 1);
+  UnitAsked asked;
+  if (kind == kKeyValue) asked = ask_unit(a.c, b, u, s, c);
 
   // ---- norm and rotation
   const void* wp = kind == kQuery ? a.prep.q_weight : a.prep.k_weight;
@@ -166,9 +185,8 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
       if (there && i < nt) st16(out + (int64_t)i * D, x[i]);
     return;
   }
-  const int u = b * a.c.Hkv + min(h, heads - 1);
-  const ChunkUnit unit = chunk_unit(a.c.L, u);
-  const int why = may_append<LPR>(a.c, unit, b, u, s, c);
+  const ChunkUnit& unit = asked.x;
+  const int why = judge_unit<LPR>(a.c, asked, s, c);
   if (!there) return;
   if (why) {
     if (c == 0 && tb == 0 && a.c.status) *a.c.status = why;
