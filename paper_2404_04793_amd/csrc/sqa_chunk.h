@@ -47,10 +47,21 @@ __device__ __forceinline__ ChunkUnit chunk_unit(const sqa_layer_cache& L, int u)
 // Does the unit hold the tokens of positions 0 .. end-1 in slots 0 .. end-1?  Exact while nothing was evicted; after that slot
 // end-1 or the ring tells, unless heavy hitters have changed places.
 __device__ __forceinline__ bool chunk_held(const sqa_layer_cache& L, const ChunkUnit& x, int u, int64_t end) {
-  const int32_t* st = L.unit_state + (int64_t)u * SQA_ST_WORDS;
-  if (end > x.slots || st[SQA_ST_LEN] < end || st[SQA_ST_RING_HEAD] != 0) return false;
-  return end == 0 || L.pos[x.first + end - 1] == end - 1;
+  const int4 st = *reinterpret_cast<const int4*>(L.unit_state + (int64_t)u * SQA_ST_WORDS);        // (both asked for together)
+  const int last = L.pos[x.first + max(min(end, (int64_t)x.slots), (int64_t)1) - 1];
+  return end <= x.slots && st.x >= end && st.y == 0 && (end == 0 || last == end - 1);
 }
+
+// x / d for 32-bit x by one high product: off by one at most, put right
+struct Divisor {
+  uint32_t d, m;
+  __device__ __forceinline__ explicit Divisor(uint32_t v) : d(v), m(0xffffffffu / v + (v > 1)) {}
+  __device__ __forceinline__ void operator()(uint32_t x, uint32_t& q, uint32_t& r) const {
+    q = d > 1 ? __umulhi(x, m) : x;
+    r = x - q * d;
+    if ((int32_t)r < 0) { --q; r += d; }
+  }
+};
 
 inline bool bad_layer(const sqa_layer_cache& c, sqa_status* why) {
   *why = SQA_OK;

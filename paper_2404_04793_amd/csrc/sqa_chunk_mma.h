@@ -26,7 +26,17 @@ __device__ __forceinline__ uint32_t lds_at(const char* p) { return (uint32_t)(ui
 __device__ __forceinline__ void fetch16(const void* g, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(g), "s"(__builtin_amdgcn_readfirstlane(lds)) : "m0", "memory");
 }
+__device__ __forceinline__ void fetch16(const void* base /*the same in all lanes*/, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "m0", "memory");
+}
 #pragma clang diagnostic pop
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);        // (the builtin's result is signed)
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+  return reinterpret_cast<const char*>((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

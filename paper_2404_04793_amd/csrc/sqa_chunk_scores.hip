@@ -1,17 +1,23 @@
 // What a chunk of tokens gives to the accumulated attention of every slot of a layer cache (sqa_chunk_scores):
 //   score[j] += sum over the unit's query heads and the tokens t with position >= j of exp(s_tj - lse_t),  s = q.K_j / sqrt(D)
-// The normalisers are known, so this is one product and a sum down its columns.  A wave keeps 32 slots' keys in registers and
-// walks the rows (head by head, only the tokens that see its workgroup's 128 slots), 64 at a time in LDS with two buffers:
-//   S = Q.K^T    a lane holds 16 of 32 rows of one slot and adds them up by itself; the two lane halves meet at the end
+// The normalisers are known, so this is one product and a sum down its columns.  A wave keeps the keys of one or two
+// blocks of 32 slots in registers and walks the rows (head by head, only the tokens that see its workgroup's slots), 64 at a time in LDS
+// with two buffers:
+//   S = Q.K^T    a lane holds 16 of 32 rows of one slot and adds them up by itself; the two lane halves meet at the end.  The
+//                exponentials of one block of rows are independent of the next one's products and are taken meanwhile
 // One workgroup owns a slot, so nothing is added atomically; where there are few slots the rows are shared out over workgroups
 // whose sums go through the workspace, and the last one to arrive adds them in order.
 #include "sqa_chunk_mma.h"
+#include <type_traits>
 
 namespace sqa {
 
 constexpr int kScoreThreads = 256;
-constexpr int kScoreSlots = 128;                    // of a workgroup
 constexpr int kScoreRows = 64;                      // of a tile in LDS
+// slots of a wave in blocks of 32: two in bf16 (each row read from LDS feeds both), one in fp32 (bound by the products either way)
+template <typename T> constexpr int score_blocks() { return sizeof(T) == 2 ? 2 : 1; }
+template <typename T> constexpr int score_slots() { return 4 * 32 * score_blocks<T>(); }
+constexpr int kScoreSlotsMost = 256;
 constexpr int kScoreItems = 1024;                   // workgroups that few slots are shared out to
 
 struct ScoresArgs {
@@ -19,7 +25,7 @@ struct ScoresArgs {
   const void* q;
   const float* lse;
   int32_t* count;                                   // [items]
-  float2* part;                                     // [items][splits][kScoreSlots / 2]
+  float2* part;                                     // [items][splits][slots of a workgroup / 2]
   float scale;                                      // log2(e) / sqrt(D)
   int tiles, splits;
 };
@@ -27,10 +33,10 @@ struct ScoresArgs {
 template <typename T, int D>
 __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const ScoresArgs a) {
   using R = TileRows<T, D>;
-  constexpr int TILE = kScoreRows * R::RB;
+  constexpr int TILE = kScoreRows * R::RB, KB = score_blocks<T>(), kScoreSlots = score_slots<T>();
   extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // two tiles of rows
-  __shared__ float s_lse[2][kScoreRows];            // in powers of two; of rows that are none: infinity
-  __shared__ int s_see[2][kScoreRows];              // the last slot that a row sees
+  __shared__ __attribute__((aligned(16))) float s_lse[4][kScoreRows];            // in powers of two; of rows that are none: infinity
+  __shared__ __attribute__((aligned(16))) int s_see[4][kScoreRows];              // the last slot that a row sees
   __shared__ float s_sum[kScoreSlots];
   __shared__ int s_word;
 
@@ -47,18 +53,36 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
   if (seq.n == 0) return;
   const ChunkUnit unit = chunk_unit(a.c.L, u);
   const int64_t slot0 = (int64_t)tile * kScoreSlots;
-  if (!chunk_held(a.c.L, unit, u, seq.pos + seq.n)) {
+  const int64_t held = seq.pos + seq.n;
+  if (held > unit.slots) {
     if (tid == 0 && tile == 0 && split == 0 && a.c.status) *a.c.status = SQA_ERR_STATE;
     return;
   }
-  const int end = (int)(seq.pos + seq.n);
-  if (unit.table) {                                  // a unit is left untouched as a whole: all of its blocks are looked at
+  const int end = __builtin_amdgcn_readfirstlane((int)held);
+  // ---- the lane's slots.  (Asked for before it is known whether the unit holds the chunk: a block number outside the pools reads block 0.)
+  const int slot = (int)min(slot0, (int64_t)end) + 32 * KB * wave + col;
+  Frag<T, D> k[KB];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    const int s = min(slot + 32 * kb, end - 1);
+    int64_t at = unit.first + s;
+    if (unit.table) {
+      const unsigned blk = (unsigned)unit.table[s / SQA_BLOCK_SLOTS];
+      at = (int64_t)(blk < (unsigned)a.c.L.n_blocks ? blk : 0u) * SQA_BLOCK_SLOTS + s % SQA_BLOCK_SLOTS;
+    }
+    const char* src = static_cast<const char*>(a.c.L.K) + at * R::RB;
+#pragma unroll
+    for (int x = 0; x < k[kb].NS; ++x) k[kb].p[x] = ld16(src + (2 * x + half) * 16);
+  }
+  int why = chunk_held(a.c.L, unit, u, held) ? 0 : SQA_ERR_STATE;
+  if (!why && unit.table) {                          // a unit is left untouched as a whole: all of its blocks are looked at
     int outside = 0;
     for (int i = tid; i < (end + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS; i += kScoreThreads) outside |= (unsigned)unit.table[i] >= (unsigned)a.c.L.n_blocks;
-    if (__syncthreads_or(outside)) {
-      if (tid == 0 && tile == 0 && split == 0 && a.c.status) *a.c.status = SQA_ERR_SHAPE;
-      return;
-    }
+    if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
+  }
+  if (why) {
+    if (tid == 0 && tile == 0 && split == 0 && a.c.status) *a.c.status = why;
+    return;
   }
   if (slot0 >= end) return;
   // the tokens that see any of the slots, and this workgroup's tiles of their rows
@@ -68,63 +92,137 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
   if (split >= parts) return;
   const int tile0 = split * per, tile1 = min(tile0 + per, nt);
 
-  // ---- the lane's slot
-  const int slot = (int)slot0 + 32 * wave + col;
-  Frag<T, D> k;
-  {
-    const int s = min(slot, end - 1);
-    const int64_t at = unit.table ? (int64_t)unit.table[s / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + s % SQA_BLOCK_SLOTS : unit.first + s;
-    const char* src = static_cast<const char*>(a.c.L.K) + at * R::RB;
-#pragma unroll
-    for (int x = 0; x < k.NS; ++x) k.p[x] = ld16(src + (2 * x + half) * 16);
-    arrived(k);
-  }
   const int64_t head0 = (int64_t)b * a.c.Hq + h * g;
   const char* const Q = static_cast<const char*>(a.q) + head0 * a.c.T * R::RB;
-  auto fetch = [&](int tl, int buf) {
-    const uint32_t dst = lds_at(s_stage) + (uint32_t)(buf * TILE);
+  const Divisor by_tv((uint32_t)tv);
+  constexpr int NI = kScoreRows / 4 / R::RPI;        // copies of a wave per tile
+  uint32_t place[NI];                                // the lane's row and piece in each of them
 #pragma unroll
-    for (int i = 0; i < kScoreRows / 4 / R::RPI; ++i) {
-      const int rr = wave * (kScoreRows / 4) + i * R::RPI, row = rr + lane / R::PPR;
-      const int x = min(tl * kScoreRows + row, rows - 1);
-      fetch16(Q + ((int64_t)(x / tv) * a.c.T + t0 + x % tv) * R::RB + (((lane % R::PPR) ^ R::k_swizzle(row)) << 4), dst + rr * R::RB);
-    }
-    if (tid < kScoreRows) {
-      const int x = tl * kScoreRows + tid, y = min(x, rows - 1);
-      const float v = a.lse[(head0 + y / tv) * a.c.T + t0 + y % tv];
-      s_lse[buf][tid] = x < rows ? v * 1.4426950408889634f : INFINITY;
-      s_see[buf][tid] = (int)seq.pos + t0 + y % tv;
+  for (int i = 0; i < NI; ++i) {
+    const int rr = wave * (kScoreRows / 4) + i * R::RPI, row = rr + lane / R::PPR;
+    place[i] = (uint32_t)(row * R::RB + (((lane % R::PPR) ^ R::k_swizzle(row)) << 4));
+  }
+  auto fetch = [&](int tl, int buf) {
+    const uint32_t dst = lds_at(s_stage) + (uint32_t)(buf * TILE + wave * (kScoreRows / 4) * R::RB);
+    uint32_t gi, tt;
+    by_tv((uint32_t)(tl * kScoreRows), gi, tt);
+    if ((int)tt + kScoreRows <= tv) {                // rows of one head, one after the other
+      const char* const base = uniform(Q + ((int64_t)gi * a.c.T + t0 + tt) * R::RB);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fetch16(base, place[i], dst + i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int row = wave * (kScoreRows / 4) + i * R::RPI + lane / R::PPR;
+        by_tv((uint32_t)min(tl * kScoreRows + row, rows - 1), gi, tt);
+        fetch16(Q + ((int64_t)gi * a.c.T + t0 + tt - row) * R::RB + place[i], dst + i * 1024);
+      }
     }
   };
-  float sum = 0.f;
+  // a tile's normalisers wait in registers of the first wave for a round, so that nothing waits for them
+  float lse_next = 0.f;
+  int see_next = 0;
+  auto ask = [&](int tl) {
+    if (tid < kScoreRows) {
+      uint32_t gi, tt;
+      by_tv((uint32_t)min(tl * kScoreRows + tid, rows - 1), gi, tt);
+      lse_next = a.lse[(head0 + gi) * a.c.T + t0 + tt];
+      see_next = (int)seq.pos + t0 + (int)tt;
+    }
+  };
+  auto keep = [&](int tl) {
+    if (tid < kScoreRows) {
+      s_lse[tl & 3][tid] = tl * kScoreRows + tid < rows ? lse_next * 1.4426950408889634f : INFINITY;
+      s_see[tl & 3][tid] = see_next;
+    }
+  };
+  // rows of a tile that are of one head and all see the workgroup's last slot need no look at what each one sees
+  const int last_slot = (int)slot0 + kScoreSlots - 1;
+  float sum[KB] = {}, sum2[KB] = {};
+  f32x16_t s[2][KB];                                 // a block's products, and the one before it, whose exponentials are taken meanwhile
+  auto add = [&](f32x16_t (&e)[KB], int tl, int rb, auto look) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 ref = *reinterpret_cast<const float4*>(&s_lse[tl & 3][32 * rb + 8 * j + 4 * half]);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        float x = exp2_fast(fmaf(e[kb][4 * j], a.scale, -ref.x)), y = exp2_fast(fmaf(e[kb][4 * j + 1], a.scale, -ref.y));
+        float z = exp2_fast(fmaf(e[kb][4 * j + 2], a.scale, -ref.z)), v = exp2_fast(fmaf(e[kb][4 * j + 3], a.scale, -ref.w));
+        if constexpr (decltype(look)::value) {
+          const int4 sees = *reinterpret_cast<const int4*>(&s_see[tl & 3][32 * rb + 8 * j + 4 * half]);
+          const int at = slot + 32 * kb;
+          x = sees.x >= at ? x : 0.f; y = sees.y >= at ? y : 0.f; z = sees.z >= at ? z : 0.f; v = sees.w >= at ? v : 0.f;
+        }
+        sum[kb] += x; sum2[kb] += y; sum[kb] += z; sum2[kb] += v;
+      }
+    }
+  };
+  // one block of 32 rows: its products, and the exponentials of the block before between them (each product takes the matrix core as long
+  // as five or six vector instructions take)
+  auto block = [&](const char* Qt, f32x16_t (&now)[KB], int rb, f32x16_t (&before)[KB], int tl_before, int rb_before, auto look) {
+    const int row = 32 * rb + col;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) now[kb] = f32x16_t{};
+#pragma unroll
+    for (int x = 0; x < Frag<T, D>::NS; ++x) {
+      const uint4 q = *reinterpret_cast<const uint4*>(Qt + row * R::RB + (((2 * x + half) ^ R::k_swizzle(row)) << 4));
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) mma_piece<T>(q, k[kb].p[x], now[kb]);
+    }
+    add(before, tl_before, rb_before, look);
+    if constexpr (sizeof(T) == 2) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < KB * Frag<T, D>::NS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 12 * 8 / Frag<T, D>::NS / 2, 0);
+      }
+    }
+  };
+  bool look = false;
+  ask(tile0);
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) arrived(k[kb]);
+  keep(tile0);
+  if (tid < kScoreRows) s_lse[(tile0 - 1) & 3][tid] = INFINITY;       // what comes before the first block adds nothing
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) s[1][kb] = f32x16_t{};
   fetch(tile0, 0);
+  ask(tile0 + 1);
   for (int tl = tile0; tl < tile1; ++tl) {
     const int buf = (tl - tile0) & 1;
     fetched();
     __syncthreads();
-    if (tl + 1 < tile1) fetch(tl + 1, buf ^ 1);
-    const char* const Qt = s_stage + buf * TILE;
-#pragma unroll
-    for (int rb = 0; rb < kScoreRows / 32; ++rb) {
-      f32x16_t s{};
-      const int row = 32 * rb + col;
-#pragma unroll
-      for (int x = 0; x < k.NS; ++x) {
-        const uint4 q = *reinterpret_cast<const uint4*>(Qt + row * R::RB + (((2 * x + half) ^ R::k_swizzle(row)) << 4));
-        mma_piece<T>(q, k.p[x], s);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = 32 * rb + c_row(i, half);
-        const float p = exp2_fast(fmaf(s[i], a.scale, -s_lse[buf][at]));
-        sum += s_see[buf][at] >= slot ? p : 0.f;
-      }
+    if (tl + 1 < tile1) {
+      keep(tl + 1);
+      fetch(tl + 1, buf ^ 1);
+      ask(tl + 2);
     }
+    const char* const Qt = s_stage + buf * TILE;
+    uint32_t gi, tt;
+    by_tv((uint32_t)(tl * kScoreRows), gi, tt);
+    const int t_first = (int)tt;
+    const bool look_now = t_first + kScoreRows > tv || (int)seq.pos + t0 + t_first < last_slot;
+    if (look || look_now) {
+      block(Qt, s[0], 0, s[1], tl - 1, 1, std::true_type{});
+      block(Qt, s[1], 1, s[0], tl, 0, std::true_type{});
+    } else {
+      block(Qt, s[0], 0, s[1], tl - 1, 1, std::false_type{});
+      block(Qt, s[1], 1, s[0], tl, 0, std::false_type{});
+    }
+    look = look_now;
   }
-  sum = other_half_sum(sum);
+  add(s[1], tile1 - 1, 1, std::true_type{});
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) sum[kb] += sum2[kb];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) sum[kb] = other_half_sum(sum[kb]);
 
   if (parts > 1) {
-    if (half == 0) s_sum[32 * wave + col] = sum;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+      if (half == 0) s_sum[32 * (KB * wave + kb) + col] = sum[kb];
     __syncthreads();
     float2* const rec = a.part + item * a.splits * (kScoreSlots / 2);
     if (tid < kScoreSlots / 2) hand_over(rec + (int64_t)split * (kScoreSlots / 2) + tid, make_float2(s_sum[2 * tid], s_sum[2 * tid + 1]));
@@ -138,9 +236,12 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
       s_sum[2 * tid] = v.x; s_sum[2 * tid + 1] = v.y;
     }
     __syncthreads();
-    sum = s_sum[32 * wave + col];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) sum[kb] = s_sum[32 * (KB * wave + kb) + col];
   }
-  if (half == 0 && slot < end) a.c.L.score_acc[unit.first + slot] += sum;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+    if (half == 0 && slot + 32 * kb < end) a.c.L.score_acc[unit.first + slot + 32 * kb] += sum[kb];
   if (tid == 0 && tile == 0) a.c.L.unit_state[(int64_t)u * SQA_ST_WORDS + SQA_ST_EVICT_HINT] = -2;   // what was decided by the old scores
 }
 
@@ -151,7 +252,7 @@ static int scores_splits(int B, int T, int Hq, int Hkv, int tiles) {
   return s < 1 ? 1 : (int)s;
 }
 // (any length: items x splits <= kScoreItems where there are splits)
-size_t chunk_scores_scratch() { return (size_t)kScoreItems * kScoreSlots * sizeof(float); }
+size_t chunk_scores_scratch() { return (size_t)kScoreItems * kScoreSlotsMost * sizeof(float); }
 
 template <typename T, int D>
 static sqa_status launch_scores(const ScoresArgs& a, hipStream_t st) {
@@ -185,7 +286,8 @@ extern "C" sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtyp
   a.part = reinterpret_cast<float2*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const int64_t slots = uniform ? (int64_t)new_pos + T : layer->capacity;
-  const int64_t tiles = (slots + sqa::kScoreSlots - 1) / sqa::kScoreSlots;
+  const int per = dt == SQA_F32 ? sqa::score_slots<float>() : sqa::score_slots<sqa::bf16_t>();
+  const int64_t tiles = (slots + per - 1) / per;
   if ((int64_t)B * Hkv > (INT32_MAX - 8) / tiles) return SQA_ERR_SHAPE;
   a.tiles = (int)tiles;
   a.splits = sqa::scores_splits(B, T, Hq, Hkv, a.tiles);
