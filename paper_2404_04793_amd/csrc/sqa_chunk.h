@@ -93,7 +93,20 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
-// Data that one workgroup hands to another inside a launch: written through, read from the coherent copy (no cache is flushed)
+// Data that one workgroup hands to another inside a launch: stored through to and loaded from where every XCD sees it (no
+// cache is flushed), 16 bytes at a time by buffer instructions with the agent-scope bits set, or 8 by atomics.
+struct HandOver {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ HandOver(float4* base /*the same in all lanes*/, uint32_t bytes)
+      : r(__builtin_amdgcn_make_buffer_rsrc(base, 0, (int)bytes, 0x00027000)) {}
+  static constexpr int kAgent = 16;                  // sc1
+  __device__ __forceinline__ void put(uint32_t i, float4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u_t, v), r, (int)(i * 16), 0, kAgent);
+  }
+  __device__ __forceinline__ float4 get(uint32_t i) const {
+    return __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(i * 16), 0, kAgent));
+  }
+};
 __device__ __forceinline__ void hand_over(float2* p, float2 v) {
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

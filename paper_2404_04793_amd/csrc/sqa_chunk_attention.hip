@@ -24,9 +24,10 @@ struct AttentionArgs {
   void* out;
   float* lse;
   int32_t* count;                                   // [items]
-  float2* part;                                     // [items][splits][32 RW][D / 2 + 1]: a row's sums, then (m, l)
+  float4* part;                                     // [items][splits][32 RW][D / 4 + 1]: a row's sums, then (m, l)
   float scale;                                      // log2(e) / sqrt(D)
   float near;                                       // 8 / scale: logits that close to a row's reference do not move it
+  uint32_t group_m;                                 // 2^32 / g, for divisions by g
   int tiles, splits;
 };
 
@@ -63,71 +64,89 @@ template <typename T, int BYTES, int NT, bool CLEAR> __device__ __forceinline__ 
 template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
   using R = TileRows<T, D>;
   static constexpr int PP = D / 4;                  // 16-byte pieces of a row of sums
-  static constexpr int REC = D / 2 + 1;             // a row of sums and its (m, l) as pairs
+  static constexpr int REC = D / 4 + 1;             // a row of sums and its (m, l), in 16 bytes
   int64_t item;
-  int b, h, g, row0, rows, last_row;                // rows: of the whole unit
+  int u, b, h, g, n, row0, rows, last_row;          // n tokens, rows of the whole unit
   int split, parts, tile0, tile1, end;              // end: the slots that the rows see
   int64_t pos;
   ChunkUnit unit;
+  bool held_slots;
 
-  // false: nothing to do (or rows of zeros have been written)
-  __device__ __forceinline__ bool begin(const AttentionArgs& a, int* s_table) {
-    const int64_t items = (int64_t)a.c.B * a.c.Hkv * a.tiles;
-    const int64_t work = xcd_item(items * a.splits);
-    if (work < 0) return false;
-    const int tid = threadIdx.x;
-    split = (int)(work % a.splits);
-    item = work / a.splits;
-    const int u = (int)(item / a.tiles), tile = a.tiles - 1 - (int)(item % a.tiles);     // the longest first
-    b = u / a.c.Hkv; h = u % a.c.Hkv; g = a.c.g;
-    const ChunkSeq seq = chunk_seq(a.c, b, tid == 0 && h == 0 && tile == 0 && split == 0);
-    rows = __builtin_amdgcn_readfirstlane(seq.n) * g;
+  uint32_t group_m;                                 // (division by g: rows are less than 2^31 / 64)
+
+  // Where the work is; false: there is none.  Nothing is known yet of what the unit holds, but its first `end` slots can be read where
+  // held_slots is true.
+  __device__ __forceinline__ bool locate(const AttentionArgs& a) {
+    const uint32_t count = (uint32_t)(a.c.B * a.c.Hkv) * (uint32_t)(a.tiles * a.splits);
+    const uint32_t per8 = (count + 7) / 8, work = (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);     // (one run of items per XCD, see xcd_item)
+    if (blockIdx.x >> 3 >= per8 || work >= count) return false;
+    split = (int)(work % (uint32_t)a.splits);
+    const uint32_t it = work / (uint32_t)a.splits;
+    item = it;
+    u = (int)(it / (uint32_t)a.tiles);
+    const int tile = a.tiles - 1 - (int)(it % (uint32_t)a.tiles);                        // the longest first
+    b = u / a.c.Hkv; h = u - b * a.c.Hkv; g = a.c.g;
+    group_m = a.group_m;
+    const ChunkSeq seq = chunk_seq(a.c, b, threadIdx.x == 0 && h == 0 && tile == 0 && split == 0);
+    n = __builtin_amdgcn_readfirstlane(seq.n);
+    rows = n * g;
     row0 = tile * M;
     if (row0 >= rows) return false;
     pos = seq.pos;
     unit = chunk_unit(a.c.L, u);
     last_row = min(row0 + M, rows) - 1;
-    // does the unit hold the chunk, and do its blocks lie in the pools
-    int why = chunk_held(a.c.L, unit, u, pos + seq.n) ? 0 : SQA_ERR_STATE;
-    if (!why && unit.table) {
-      int outside = 0;
-      for (int i = tid; i < (int)((pos + seq.n + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS); i += NT) {
-        const int blk = unit.table[i];
-        s_table[i] = blk;
-        outside |= (unsigned)blk >= (unsigned)a.c.L.n_blocks;
-      }
-      if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
-    }
-    if (why) {
-      if (split) return false;
-      if (tid == 0 && a.c.status) *a.c.status = why;
-      for (int i = tid; i < (last_row + 1 - row0) * R::PPR; i += NT) {
-        int t, head;
-        place(row0 + i / R::PPR, t, head);
-        st16(static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + i % R::PPR * R::E, make_uint4(0, 0, 0, 0));
-        if (a.lse && i % R::PPR == 0) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = -INFINITY;
-      }
-      return false;
-    }
-    end = __builtin_amdgcn_readfirstlane((int)(pos + last_row / g + 1));
+    int t, head;
+    place(last_row, t, head);
+    end = __builtin_amdgcn_readfirstlane((int)min(pos + t + 1, (int64_t)INT32_MAX));
+    held_slots = pos + n <= unit.slots;
     const int nt = (end + KT - 1) / KT, per = (nt + a.splits - 1) / a.splits;
     parts = (nt + per - 1) / per;
     tile0 = split * per;
     tile1 = min(tile0 + per, nt);
     return split < parts;
   }
-  __device__ __forceinline__ void place(int r, int& t, int& head) const { t = r / g; head = h * g + r % g; }
+  // Does the unit hold the chunk, and do its blocks (to s_table) lie in the pools?  Otherwise its rows become zeros.
+  __device__ __forceinline__ bool check(const AttentionArgs& a, int* s_table) const {
+    const int tid = threadIdx.x;
+    int why = held_slots && chunk_held(a.c.L, unit, u, pos + n) ? 0 : SQA_ERR_STATE;
+    if (held_slots && unit.table) {
+      int outside = 0;
+      for (int i = tid; i < (int)((pos + n + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS); i += NT) {
+        const int blk = unit.table[i];
+        s_table[i] = blk;
+        outside |= (unsigned)blk >= (unsigned)a.c.L.n_blocks;
+      }
+      if (__syncthreads_or(outside) && !why) why = SQA_ERR_SHAPE;
+    }
+    if (!why) return true;
+    if (split) return false;
+    if (tid == 0 && a.c.status) *a.c.status = why;
+    for (int i = tid; i < (last_row + 1 - row0) * R::PPR; i += NT) {
+      int t, head;
+      place(row0 + i / R::PPR, t, head);
+      st16(static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + i % R::PPR * R::E, make_uint4(0, 0, 0, 0));
+      if (a.lse && i % R::PPR == 0) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = -INFINITY;
+    }
+    return false;
+  }
+  __device__ __forceinline__ void place(int r, int& t, int& head) const {
+    t = g > 1 ? (int)__umulhi((uint32_t)r, group_m) : r;
+    int i = r - t * g;
+    if (i < 0) { --t; i += g; }
+    head = h * g + i;
+  }
 
-  __device__ __forceinline__ void store4(const AttentionArgs& a, int row, int p, float4 v, float mm, float ll) const {
+  // 32 bytes of a row of sums as the output's 8 (bf16) or 2 x 4 (fp32) elements
+  __device__ __forceinline__ void store8(const AttentionArgs& a, int row, int p, const float4 (&v)[2], float mm, float ll) const {
     int t, head;
     place(row0 + row, t, head);
     const float inv = 1.f / ll;
-    T* dst = static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + 4 * p;
+    T* dst = static_cast<T*>(a.out) + (((int64_t)b * a.c.T + t) * a.c.Hq + head) * D + 8 * p;
     if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint2*>(dst) = make_uint2(f32_to_bf16_bits(v.x * inv) | (f32_to_bf16_bits(v.y * inv) << 16),
-                                                  f32_to_bf16_bits(v.z * inv) | (f32_to_bf16_bits(v.w * inv) << 16));
+      st16(dst, make_uint4(pair(v[0].x * inv, v[0].y * inv), pair(v[0].z * inv, v[0].w * inv), pair(v[1].x * inv, v[1].y * inv), pair(v[1].z * inv, v[1].w * inv)));
     else
-      *reinterpret_cast<float4*>(dst) = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) reinterpret_cast<float4*>(dst)[k] = make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv);
     if (p == 0 && a.lse) a.lse[((int64_t)b * a.c.Hq + head) * a.c.T + t] = 0.6931471805599453f * fmaf(mm, a.scale, log2f(ll));
   }
 
@@ -181,42 +200,55 @@ template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
       }
       return v;
     };
-    const int live = (last_row + 1 - row0) * PP;
+    const int live = (last_row + 1 - row0) * (PP / 2);
     if (parts == 1) {
       for (int i = tid; i < live; i += NT) {
+        const int row = i / (PP / 2), p = i % (PP / 2);
         float mm, ll;
-        joined(i / PP, mm, ll);
-        store4(a, i / PP, i % PP, piece4(i / PP, i % PP), mm, ll);
+        joined(row, mm, ll);
+        const float4 v[2] = {piece4(row, 2 * p), piece4(row, 2 * p + 1)};
+        store8(a, row, p, v, mm, ll);
       }
       return;
     }
-    float2* const rec = a.part + (item * a.splits) * M * REC;
+    const char* const base = uniform(reinterpret_cast<const char*>(a.part + item * a.splits * (M * REC)));
+    const HandOver rec(reinterpret_cast<float4*>(const_cast<char*>(base)), (uint32_t)(a.splits * (M * REC * 16)));
     for (int i = tid; i < live; i += NT) {
-      const int row = i / PP, p = i % PP;
-      float2* dst = rec + ((int64_t)split * M + row) * REC;
-      const float4 v = piece4(row, p);
-      hand_over(dst + 2 * p, make_float2(v.x, v.y));
-      hand_over(dst + 2 * p + 1, make_float2(v.z, v.w));
+      const int row = i / (PP / 2), p = i % (PP / 2);
+      const uint32_t to = (uint32_t)((split * M + row) * REC);
+      rec.put(to + 2 * p, piece4(row, 2 * p));
+      rec.put(to + 2 * p + 1, piece4(row, 2 * p + 1));
       if (p == 0) {
         float mm, ll;
         joined(row, mm, ll);
-        hand_over(dst + D / 2, make_float2(mm, ll));
+        rec.put(to + PP, make_float4(mm, ll, 0.f, 0.f));
       }
     }
     if (!last_to_arrive(a.count + item, parts, s_word)) return;
     for (int i = tid; i < live; i += NT) {
-      const int row = i / PP, p = i % PP;
+      const int row = i / (PP / 2), p = i % (PP / 2);
       float mm = -FLT_MAX, ll = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = 0; k < parts; ++k) mm = fmaxf(mm, handed_over(rec + ((int64_t)k * M + row) * REC + D / 2).x);
-      for (int k = 0; k < parts; ++k) {
-        const float2* src = rec + ((int64_t)k * M + row) * REC;
-        const float2 ml = handed_over(src + D / 2), x = handed_over(src + 2 * p), y = handed_over(src + 2 * p + 1);
-        const float w = exp2_fast((ml.x - mm) * a.scale);
-        ll = fmaf(ml.y, w, ll);
-        v.x = fmaf(x.x, w, v.x); v.y = fmaf(x.y, w, v.y); v.z = fmaf(y.x, w, v.z); v.w = fmaf(y.y, w, v.w);
+      float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+      for (int k0 = 0; k0 < parts; k0 += 4) {        // four records in flight; in order
+        float4 ml[4], x[4], y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t from = (uint32_t)((min(k0 + k, parts - 1) * M + row) * REC);
+          ml[k] = rec.get(from + PP); x[k] = rec.get(from + 2 * p); y[k] = rec.get(from + 2 * p + 1);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < parts) {
+            const float top = fmaxf(mm, ml[k].x), w0 = exp2_fast((mm - top) * a.scale), w1 = exp2_fast((ml[k].x - top) * a.scale);
+            mm = top;
+            ll = fmaf(ll, w0, ml[k].y * w1);
+            v[0].x = fmaf(v[0].x, w0, x[k].x * w1); v[0].y = fmaf(v[0].y, w0, x[k].y * w1);
+            v[0].z = fmaf(v[0].z, w0, x[k].z * w1); v[0].w = fmaf(v[0].w, w0, x[k].w * w1);
+            v[1].x = fmaf(v[1].x, w0, y[k].x * w1); v[1].y = fmaf(v[1].y, w0, y[k].y * w1);
+            v[1].z = fmaf(v[1].z, w0, y[k].z * w1); v[1].w = fmaf(v[1].w, w0, y[k].w * w1);
+          }
       }
-      store4(a, row, p, v, mm, ll);
+      store8(a, row, p, v, mm, ll);
     }
   }
 };
@@ -238,7 +270,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
   __shared__ int s_word;
   int* const s_table = reinterpret_cast<int*>(s_stage + C::STAGE);
   AttentionWork<T, D, kAtThreads, M, KT> w;
-  if (!w.begin(a, s_table)) return;
+  if (!w.locate(a)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW, col = lane & 31, half = lane >> 5;
 
@@ -246,17 +278,20 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
   const int r = w.row0 + 32 * rw + col;
   const bool mine = r < w.rows;
   int t, head;
-  w.place(mine ? r : w.row0, t, head);
+  w.place(min(r, w.last_row), t, head);
   const int see = (int)(w.pos + t);                                                    // the last slot that the row sees
-  const int see_all = (int)(w.pos + min(w.row0 + 32 * rw, w.last_row) / w.g);                // ... that all of the wave's rows see
-  const int see_all_tile = (int)(w.pos + w.row0 / w.g);                                    // ... all of the workgroup's
+  int t_first, t_tile, any;
+  w.place(min(w.row0 + 32 * rw, w.last_row), t_first, any);
+  w.place(w.row0, t_tile, any);
+  const int see_all = (int)w.pos + t_first, see_all_tile = (int)w.pos + t_tile;          // ... that all of the wave's, of the workgroup's rows see
   Frag<T, D> q;
   {
     const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)w.b * a.c.Hq + head) * a.c.T + t) * D);
 #pragma unroll
     for (int s = 0; s < q.NS; ++s) q.p[s] = mine ? ld16(src + (2 * s + half) * 16) : make_uint4(0, 0, 0, 0);
-    arrived(q);
   }
+  if (!w.check(a, s_table)) return;
+  arrived(q);
 
   // ---- copies of one tile: each wave the rows wave KT/4 .. of K and of V
   const char* const Kp = static_cast<const char*>(a.c.L.K);
@@ -412,7 +447,7 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
   __shared__ int s_word;
   int* const s_table = reinterpret_cast<int*>(s_stage + kWideRows * D * 4);
   AttentionWork<T, D, kWideThreads, kWideRows, kWideSlots> w;
-  if (!w.begin(a, s_table)) return;
+  if (!w.locate(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const bool late = wave >= 4;
@@ -423,15 +458,21 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
   int t, head;
   w.place(min(r, w.last_row), t, head);
   const int see = (int)(w.pos + t);                                                                                            // the last slot that the row sees
-  const int see_all = __builtin_amdgcn_readfirstlane((int)(w.pos + min(w.row0 + 32 * wave, w.last_row) / w.g));                // ... that all of the wave's rows see
-  const int see_any = __builtin_amdgcn_readfirstlane((int)(w.pos + min(w.row0 + 32 * wave + 31, w.last_row) / w.g));           // ... that any of them sees
+  int t_first, t_last, t_tile, any;
+  w.place(min(w.row0 + 32 * wave, w.last_row), t_first, any);
+  w.place(min(w.row0 + 32 * wave + 31, w.last_row), t_last, any);
+  w.place(w.row0, t_tile, any);
+  const int see_all = __builtin_amdgcn_readfirstlane((int)w.pos + t_first);              // ... that all of the wave's rows see
+  const int see_any = __builtin_amdgcn_readfirstlane((int)w.pos + t_last);               // ... that any of them sees
+  const int see_all_tile = __builtin_amdgcn_readfirstlane((int)w.pos + t_tile);          // ... that all of the workgroup's see
   Frag<T, D> q;
   {
     const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)w.b * a.c.Hq + head) * a.c.T + t) * D);
 #pragma unroll
     for (int x = 0; x < NS; ++x) q.p[x] = mine ? ld16(src + (2 * x + half) * 16) : make_uint4(0, 0, 0, 0);
-    arrived(q);
   }
+  if (!w.check(a, s_table)) return;
+  arrived(q);
 
   // ---- copies: each wave 8 rows of K and of V of a tile (they lie in one block)
   const uint32_t lds0 = lds_at(s_stage);
@@ -573,7 +614,6 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
     l += l0 + l1;
   };
   const int n = w.tile1 - w.tile0;
-  const int see_all_tile = __builtin_amdgcn_readfirstlane((int)(w.pos + w.row0 / w.g));
   const int whole = min(max((see_all_tile + 1) / kWideSlots - w.tile0, 0), n);        // the first tiles, that every row sees all of
   auto round = [&](int j, auto edge) {
     constexpr bool E = decltype(edge)::value;
@@ -624,7 +664,7 @@ static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv,
 // (any T' <= T, any length, either type: items x splits <= attention_items() where there are splits)
 size_t chunk_attention_scratch(int T, int Hq, int Hkv, int D) {
   const int rw = attention_rw(T * (Hq / Hkv), false, D);
-  return (size_t)kAtItems * 32 * rw * (D / 2 + 1) * sizeof(float2);
+  return (size_t)kAtItems * 32 * rw * (D / 4 + 1) * sizeof(float4);
 }
 
 static sqa_status start_attention(void (*fn)(AttentionArgs), int threads, size_t lds, const AttentionArgs& a, hipStream_t st) {
@@ -677,11 +717,12 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   a.c = sqa::chunk_args(layer, B, T, Hq, Hkv, new_pos, opts);
   a.q = q; a.out = out; a.lse = lse;
   a.count = static_cast<int32_t*>(workspace);
-  a.part = reinterpret_cast<float2*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
+  a.part = reinterpret_cast<float4*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
   const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, uniform ? (int64_t)new_pos + T : layer->capacity);
   a.near = 8.f / a.scale;
+  a.group_m = 0xffffffffu / (uint32_t)a.c.g + 1;
   a.tiles = p.tiles; a.splits = p.splits;
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
