@@ -16,6 +16,7 @@ namespace sqa {
 
 constexpr int kAtThreads = 256;
 constexpr float kFarLogit = 64.f;                   // in powers of two: below it the rounding is 2e-6 at most
+constexpr int kAtJoin = 512;                        // slots of a workgroup, see attention_plan()
 constexpr int kAtItems = 512;                       // workgroups that few rows are shared out to: two per CU
 
 struct AttentionArgs {
@@ -432,13 +433,12 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
 // behind waves 0-3, so that of the two waves of a SIMD one keeps the matrix cores busy and the other one the vector ALUs.  A barrier
 // after each part keeps it so.  K of tile j + 1 and V of tile j are requested when the first waves begin the products of tile j, and
 // have a whole round to arrive.
-constexpr int kWideThreads = 512;
-constexpr int kWideRows = 256;
 constexpr int kWideSlots = 64;
 
 __device__ __forceinline__ void part_done() { asm volatile("s_barrier" ::: "memory"); }
 
-template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
+template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
+  constexpr int kWideThreads = 64 * NW, kWideRows = 32 * NW;
   using T = bf16_t;
   using R = TileRows<T, D>;
   constexpr int NB = D / 32, NS = Frag<T, D>::NS, TILE = kWideSlots * R::RB;
@@ -450,7 +450,7 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
   if (!w.locate(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const bool late = wave >= 4;
+  const bool late = NW == 8 && wave >= 4;
 
   // ---- this lane's query row
   const int r = w.row0 + 32 * wave + col;
@@ -478,8 +478,8 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
   const uint32_t lds0 = lds_at(s_stage);
   auto copy = [&](const void* from, int tl, uint32_t dst, bool v) {
 #pragma unroll
-    for (int i = 0; i < 8 / R::RPI; ++i) {
-      const int rr = 8 * wave + i * R::RPI, row = rr + lane / R::PPR;
+    for (int i = 0; i < kWideSlots / NW / R::RPI; ++i) {
+      const int rr = kWideSlots / NW * wave + i * R::RPI, row = rr + lane / R::PPR;
       const int slot = min(tl * kWideSlots + row, w.end - 1);
       const int64_t at = w.unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : w.unit.first + slot;
       fetch16(static_cast<const char*>(from) + at * R::RB + (((lane % R::PPR) ^ (v ? R::v_swizzle(row) : R::k_swizzle(row))) << 4), dst + rr * R::RB);
@@ -622,7 +622,7 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
     if (seen(j)) keys(j);
     if (j > 0 && seen(j - 1)) values(j - 1, edge);
     if (late) fetched();
-    part_done();
+    if constexpr (NW == 8) part_done();
     if (late && j + 1 < n) request(j + 1);
     if (seen(j)) softmax(j, edge);
     if (!late) fetched();
@@ -639,7 +639,7 @@ template <int D> __global__ __launch_bounds__(kWideThreads, 2) void chunk_attent
   for (; j < whole; ++j) round(j, std::false_type{});
   for (; j < n; ++j) round(j, std::true_type{});
   if ((w.tile0 + n - 1) * kWideSlots <= see_any) values(n - 1, std::true_type{});
-  if (!late) part_done();
+  if (NW == 8 && !late) part_done();
   w.template finish<1>(a, s_stage, s_m, s_l, &s_word, wave, 0, o, m, l);
 }
 
@@ -652,12 +652,17 @@ static int attention_rw(int rows, bool bf16, int D) {
 static int attention_items(int rw) { return rw == 8 ? kAtItems / 2 : kAtItems; }
 static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots) {
   AttentionPlan p;
-  const int rows = T * (Hq / Hkv);
-  p.rw = attention_rw(rows, dt == SQA_BF16, D);
-  p.tiles = (rows + 32 * p.rw - 1) / (32 * p.rw);
-  const int64_t items = (int64_t)B * Hkv * p.tiles;
-  int64_t s = attention_items(p.rw) / items;
-  s = s > slots / 256 ? slots / 256 : s;             // (a workgroup's start and the join cost what some hundred slots do)
+  const int rows = T * (Hq / Hkv), least = attention_rw(1, dt == SQA_BF16, D);
+  int64_t items, s;
+  for (p.rw = attention_rw(rows, dt == SQA_BF16, D);; p.rw /= 2) {
+    p.tiles = (rows + 32 * p.rw - 1) / (32 * p.rw);
+    items = (int64_t)B * Hkv * p.tiles;
+    s = attention_items(p.rw) / items;
+    // a join costs what some hundred slots do: short units are shared out by rows first
+    if (p.rw == least || s <= 1 || slots / s >= kAtJoin) break;
+  }
+  const int few = dt == SQA_BF16 ? 384 : 128;        // (fp32 products take 8 times as long)
+  s = s > slots / few ? slots / few : s;
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }
@@ -681,10 +686,13 @@ static sqa_status launch_attention(const AttentionArgs& a, hipStream_t st) {
 }
 template <typename T, int D>
 static sqa_status launch_attention(int rw, const AttentionArgs& a, hipStream_t st) {
-  if constexpr (sizeof(T) == 2)
-    if (rw == 8) return start_attention(chunk_attention_wide_kernel<D>, kWideThreads, kWideRows * D * 4, a, st);
+  if constexpr (sizeof(T) == 2) {
+    if (rw == 8) return start_attention(chunk_attention_wide_kernel<D, 8>, 512, 256 * D * 4, a, st);
+    if (rw == 4) return start_attention(chunk_attention_wide_kernel<D, 4>, 256, 128 * D * 4, a, st);
+  }
   constexpr bool wide = D * sizeof(T) == 512;        // rows of 512 bytes: half the slots
-  if (rw == 4) return launch_attention<T, D, 4, wide ? 32 : 64>(a, st);
+  if constexpr (sizeof(T) == 4)
+    if (rw == 4) return launch_attention<T, D, 4, wide ? 32 : 64>(a, st);
   if constexpr (wide) return launch_attention<T, D, 2, 64>(a, st);
   else return rw == 2 ? launch_attention<T, D, 2, 64>(a, st) : launch_attention<T, D, 1, 128>(a, st);
 }
