@@ -30,6 +30,7 @@ struct AttentionArgs {
   float near;                                       // 8 / scale: logits that close to a row's reference do not move it
   uint32_t group_m;                                 // 2^32 / g, for divisions by g
   int tiles, splits;
+  int group;                                        // units whose rows are taken in turn (below)
 };
 
 // the halves of a pair of bf16 that are not finite, as a mask
@@ -85,7 +86,13 @@ template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
     const uint32_t it = work / (uint32_t)a.splits;
     item = it;
     u = (int)(it / (uint32_t)a.tiles);
-    const int tile = a.tiles - 1 - (int)(it % (uint32_t)a.tiles);                        // the longest first
+    int tile = (int)(it - (uint32_t)u * (uint32_t)a.tiles);
+    if (a.group > 1) {                               // ... of `group` units, not of one
+      const uint32_t of = (uint32_t)(a.group * a.tiles), first = it / of, rest = it - first * of;
+      tile = (int)(rest / (uint32_t)a.group);
+      u = (int)(first * (uint32_t)a.group + rest % (uint32_t)a.group);
+    }
+    tile = a.tiles - 1 - tile;                       // the longest first
     b = u / a.c.Hkv; h = u - b * a.c.Hkv; g = a.c.g;
     group_m = a.group_m;
     const ChunkSeq seq = chunk_seq(a.c, b, threadIdx.x == 0 && h == 0 && tile == 0 && split == 0);
@@ -428,17 +435,16 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
   w.template finish<KW>(a, s_stage, s_m, s_l, &s_word, rw, kw, o, m, l);
 }
 
-// The same for many rows in bf16: 8 waves of 32 rows, two per SIMD, that take turns.  A wave's work on a tile of 64 slots has two parts of
-// about equal length, products (K.Q^T of this tile and V^T.P^T of the one before) and softmax; waves 4-7 are one part
-// behind waves 0-3, so that of the two waves of a SIMD one keeps the matrix cores busy and the other one the vector ALUs.  A barrier
-// after each part keeps it so.  K of tile j + 1 and V of tile j are requested when the first waves begin the products of tile j, and
-// have a whole round to arrive.
+// The same for many rows in bf16: 128 rows and tiles of 64 slots, two workgroups per CU.  Nothing orders the two waves of a SIMD, which
+// drift apart until one's products run beside the other's softmax.  V^T.P^T of a tile follows K.Q^T of the next one, K of tile j + 1
+// and V of tile j are asked for when tile j begins; the reference m moves only when a logit is 2^8 times beyond it, so that the sums
+// are seldom multiplied.  Tiles that not all rows see are worked off afterwards, one after the other.
 constexpr int kWideSlots = 64;
 
 __device__ __forceinline__ void part_done() { asm volatile("s_barrier" ::: "memory"); }
 
-template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
-  constexpr int kWideThreads = 64 * NW, kWideRows = 32 * NW;
+template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
+  constexpr int NW = kAtThreads / 64, kWideRows = 32 * NW;
   using T = bf16_t;
   using R = TileRows<T, D>;
   constexpr int NB = D / 32, NS = Frag<T, D>::NS, TILE = kWideSlots * R::RB;
@@ -446,11 +452,10 @@ template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_att
   __shared__ float s_m[1][kWideRows], s_l[1][kWideRows];
   __shared__ int s_word;
   int* const s_table = reinterpret_cast<int*>(s_stage + kWideRows * D * 4);
-  AttentionWork<T, D, kWideThreads, kWideRows, kWideSlots> w;
+  AttentionWork<T, D, kAtThreads, kWideRows, kWideSlots> w;
   if (!w.locate(a)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const bool late = NW == 8 && wave >= 4;
 
   // ---- this lane's query row
   const int r = w.row0 + 32 * wave + col;
@@ -474,20 +479,39 @@ template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_att
   if (!w.check(a, s_table)) return;
   arrived(q);
 
-  // ---- copies: each wave 8 rows of K and of V of a tile (they lie in one block)
-  const uint32_t lds0 = lds_at(s_stage);
-  auto copy = [&](const void* from, int tl, uint32_t dst, bool v) {
+  // ---- copies: each wave 64 / NW rows of K and of V of a tile (they lie in one block)
+  constexpr int WR = kWideSlots / NW, NI = WR / R::RPI;
+  const uint32_t lds0 = lds_at(s_stage) + wave * WR * R::RB;
+  uint32_t k_from[NI], v_from[NI];                   // the lane's row and piece among the wave's
 #pragma unroll
-    for (int i = 0; i < kWideSlots / NW / R::RPI; ++i) {
-      const int rr = kWideSlots / NW * wave + i * R::RPI, row = rr + lane / R::PPR;
-      const int slot = min(tl * kWideSlots + row, w.end - 1);
-      const int64_t at = w.unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : w.unit.first + slot;
-      fetch16(static_cast<const char*>(from) + at * R::RB + (((lane % R::PPR) ^ (v ? R::v_swizzle(row) : R::k_swizzle(row))) << 4), dst + rr * R::RB);
-    }
+  for (int i = 0; i < NI; ++i) {
+    const int r0 = i * R::RPI + lane / R::PPR, row = wave * WR + r0;
+    k_from[i] = (uint32_t)(r0 * R::RB + (((lane % R::PPR) ^ R::k_swizzle(row)) << 4));
+    v_from[i] = (uint32_t)(r0 * R::RB + (((lane % R::PPR) ^ R::v_swizzle(row)) << 4));
+  }
+  auto wave_slot = [&](int j) { return (w.tile0 + j) * kWideSlots + wave * WR; };
+  auto block_of = [&](int j) { return w.unit.table ? s_table[min(wave_slot(j), w.end - 1) / SQA_BLOCK_SLOTS] : 0; };
+  auto row_of = [&](int j, int block) {              // where the wave's first row lies
+    return w.unit.table ? (int64_t)__builtin_amdgcn_readfirstlane(block) * SQA_BLOCK_SLOTS + wave_slot(j) % SQA_BLOCK_SLOTS : w.unit.first + wave_slot(j);
   };
-  auto request = [&](int j) {                        // what the round of tile j asks for
-    if (w.tile0 + j + 1 < w.tile1) copy(a.c.L.K, w.tile0 + j + 1, lds0 + ((j + 1) & 1) * TILE, false);
-    copy(a.c.L.V, w.tile0 + j, lds0 + (2 + (j & 1)) * TILE, true);
+  auto copy = [&](const void* from, int j, int64_t row, uint32_t dst, const uint32_t (&at)[NI]) {
+    const int last = w.end - 1 - wave_slot(j);       // (rows behind the last: that one again)
+    const char* const base = uniform(static_cast<const char*>(from) + row * R::RB);
+    if (last >= WR - 1) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fetch16(base, at[i], dst + i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int r0 = i * R::RPI + lane / R::PPR, back = r0 - min(r0, last);
+        if (last >= 0) fetch16(base + (int64_t)at[i] - back * R::RB, dst + i * 1024);
+        else {                                       // (they lie elsewhere)
+          const int slot = w.end - 1;
+          const int64_t to = w.unit.table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : w.unit.first + slot;
+          fetch16(static_cast<const char*>(from) + to * R::RB + at[i] - r0 * R::RB, dst + i * 1024);
+        }
+      }
+    }
   };
 
   // ---- the lane's places in a tile of K and of V
@@ -519,58 +543,20 @@ template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_att
       for (int x = 0; x < NS; ++x) mma_piece<T>(k[x], q.p[x], s[kb]);
     }
   };
-  // edge: not all rows of the workgroup see all slots of the tile
-  auto values = [&](int j, auto edge) {              // o += V^T.P^T of tile j
+  auto values = [&](int j) {                         // o += V^T.P^T of tile j
     const char* const Vt = s_stage + (2 + (j & 1)) * TILE;
-    const int first = (w.tile0 + j) * kWideSlots;
-    // a slot that a row does not see has probability 0, but 0 x NaN is NaN (see above)
-    bool any_odd = false;
-    if constexpr (decltype(edge)::value)
-      if (first + kWideSlots - 1 > see_all) {
-        uint32_t odd = 0;
-#pragma unroll 4
-        for (int i = 0; i < TILE / 1024; ++i) {
-          const uint4 v = *reinterpret_cast<const uint4*>(Vt + i * 1024 + lane * 16);
-          odd |= odd_mask(v.x) | odd_mask(v.y) | odd_mask(v.z) | odd_mask(v.w);
-        }
-        any_odd = __any(odd != 0);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int e = 0; e < NB; ++e) {
+        const char* at = Vt + v_at[e] + 16 * ks * R::RB;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * R::RB));
+        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[ks], o[e], 0, 0, 0);
       }
-    if (any_odd) {
-#pragma unroll 1
-      for (int k = 0; k < kWideSlots; ++k) {
-        const bool sees = first + k <= see;
-        const char* const row = Vt + k * R::RB + 8 * half;
-        const int swz = R::v_swizzle(k) << 4;
-#pragma unroll
-        for (int e = 0; e < NB; ++e)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const uint2 v = *reinterpret_cast<const uint2*>(row + ((64 * e + 4 * i) ^ swz));
-            o[e][i] += sees && odd_mask(v.x << 16) ? bf16_lo(v.x) : 0.f;
-            o[e][i + 1] += sees && odd_mask(v.x & 0xffff0000u) ? bf16_hi(v.x) : 0.f;
-            o[e][i + 2] += sees && odd_mask(v.y << 16) ? bf16_lo(v.y) : 0.f;
-            o[e][i + 3] += sees && odd_mask(v.y & 0xffff0000u) ? bf16_hi(v.y) : 0.f;
-          }
-      }
-    }
-    auto product = [&](auto clean) {
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int e = 0; e < NB; ++e) {
-          const char* at = Vt + v_at[e] + 16 * ks * R::RB;
-          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at));
-          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * R::RB));
-          uint4 v = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          if constexpr (decltype(clean)::value) {
-            v.x &= ~odd_mask(v.x); v.y &= ~odd_mask(v.y); v.z &= ~odd_mask(v.z); v.w &= ~odd_mask(v.w);
-          }
-          o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[ks], o[e], 0, 0, 0);
-        }
-    };
-    if (any_odd) product(std::true_type{});
-    else product(std::false_type{});
   };
+  // edge: not all rows of the workgroup see all slots of the tile
   auto softmax = [&](int j, auto edge) {
     if constexpr (decltype(edge)::value) {
       const int first = (w.tile0 + j) * kWideSlots;
@@ -613,43 +599,84 @@ template <int D, int NW> __global__ __launch_bounds__(64 * NW, 2) void chunk_att
       }
     l += l0 + l1;
   };
+  // a slot that a row does not see has probability 0, but 0 x NaN is NaN (see the kernel above)
+  auto take_odd_values = [&](int j) {
+    char* const Vt = s_stage + (2 + (j & 1)) * TILE;
+    if (!__syncthreads_or(odd_values<T, TILE, kAtThreads, false>(Vt))) return;
+    const int first = (w.tile0 + j) * kWideSlots;
+#pragma unroll 1
+    for (int k = 0; k < kWideSlots; ++k) {
+      const bool sees = first + k <= see;
+      const char* const row = Vt + k * R::RB + 8 * half;
+      const int swz = R::v_swizzle(k) << 4;
+#pragma unroll
+      for (int e = 0; e < NB; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const uint2 v = *reinterpret_cast<const uint2*>(row + ((64 * e + 4 * i) ^ swz));
+          o[e][i] += sees && odd_mask(v.x << 16) ? bf16_lo(v.x) : 0.f;
+          o[e][i + 1] += sees && odd_mask(v.x & 0xffff0000u) ? bf16_hi(v.x) : 0.f;
+          o[e][i + 2] += sees && odd_mask(v.y << 16) ? bf16_lo(v.y) : 0.f;
+          o[e][i + 3] += sees && odd_mask(v.y & 0xffff0000u) ? bf16_hi(v.y) : 0.f;
+        }
+    }
+    __syncthreads();
+    odd_values<T, TILE, kAtThreads, true>(Vt);
+    __syncthreads();
+  };
+
   const int n = w.tile1 - w.tile0;
   const int whole = min(max((see_all_tile + 1) / kWideSlots - w.tile0, 0), n);        // the first tiles, that every row sees all of
-  auto round = [&](int j, auto edge) {
-    constexpr bool E = decltype(edge)::value;
-    auto seen = [&](int i) { return !E || (w.tile0 + i) * kWideSlots <= see_any; };
-    if (!late) request(j);
-    if (seen(j)) keys(j);
-    if (j > 0 && seen(j - 1)) values(j - 1, edge);
-    if (late) fetched();
-    if constexpr (NW == 8) part_done();
-    if (late && j + 1 < n) request(j + 1);
-    if (seen(j)) softmax(j, edge);
-    if (!late) fetched();
-    part_done();
+  int64_t row_k = row_of(0, block_of(0)), row_v = row_k;           // of the tile whose keys were asked for last, and of the one before
+  int block = 0;                                                   // of the tile after that
+  auto copy_k = [&](int j) {
+    if (j >= n) return;
+    row_v = row_k;
+    row_k = row_of(j, block);
+    copy(a.c.L.K, j, row_k, lds0 + (j & 1) * TILE, k_from);
+    block = block_of(j + 1);
   };
-  copy(a.c.L.K, w.tile0, lds0, false);
+  auto copy_v = [&](int j, int64_t row) { if (j < n) copy(a.c.L.V, j, row, lds0 + (2 + (j & 1)) * TILE, v_from); };
+  copy(a.c.L.K, 0, row_k, lds0, k_from);
+  block = block_of(1);
   fetched();
   part_done();
-  if (late) {
-    request(0);
+  // ---- the tiles that all rows see: K of tile j + 1 and V of tile j are asked for when tile j begins
+  if (whole > 0) {
+    for (int j = 0; j < whole; ++j) {
+      copy_k(j + 1); copy_v(j, j + 1 < n ? row_v : row_k);
+      keys(j);
+      if (j > 0) values(j - 1);
+      softmax(j, std::false_type{});
+      fetched();
+      part_done();
+    }
+    values(whole - 1);
     part_done();
   }
-  int j = 0;
-  for (; j < whole; ++j) round(j, std::false_type{});
-  for (; j < n; ++j) round(j, std::true_type{});
-  if ((w.tile0 + n - 1) * kWideSlots <= see_any) values(n - 1, std::true_type{});
-  if (NW == 8 && !late) part_done();
+  // ---- the others, in step: K and V of tile j + 1 are asked for when tile j begins
+  copy_v(whole, row_k);                              // (row_k: tile `whole`, the last that was asked for)
+  for (int j = whole; j < n; ++j) {
+    fetched();
+    part_done();
+    copy_k(j + 1);
+    copy_v(j + 1, row_k);
+    const bool seen = (w.tile0 + j) * kWideSlots <= see_any;
+    if (seen) {
+      keys(j);
+      softmax(j, std::true_type{});
+    }
+    take_odd_values(j);
+    if (seen) values(j);
+  }
   w.template finish<1>(a, s_stage, s_m, s_l, &s_word, wave, 0, o, m, l);
 }
 
 struct AttentionPlan { int rw, tiles, splits; };     // rw: 32-row blocks of a workgroup
 // (rows of 512 bytes have no form for 32 rows: its tiles would not fit the LDS)
 static int attention_rw(int rows, bool bf16, int D) {
-  if (rows > 128 && bf16) return 8;
   return rows <= 32 && (bf16 || D == 64) ? 1 : (rows <= 64 ? 2 : 4);
 }
-static int attention_items(int rw) { return rw == 8 ? kAtItems / 2 : kAtItems; }
 static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots) {
   AttentionPlan p;
   const int rows = T * (Hq / Hkv), least = attention_rw(1, dt == SQA_BF16, D);
@@ -657,7 +684,7 @@ static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv,
   for (p.rw = attention_rw(rows, dt == SQA_BF16, D);; p.rw /= 2) {
     p.tiles = (rows + 32 * p.rw - 1) / (32 * p.rw);
     items = (int64_t)B * Hkv * p.tiles;
-    s = attention_items(p.rw) / items;
+    s = kAtItems / items;
     // a join costs what some hundred slots do: short units are shared out by rows first
     if (p.rw == least || s <= 1 || slots / s >= kAtJoin) break;
   }
@@ -666,7 +693,7 @@ static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv,
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }
-// (any T' <= T, any length, either type: items x splits <= attention_items() where there are splits)
+// (any T' <= T, any length, either type: items x splits <= kAtItems where there are splits)
 size_t chunk_attention_scratch(int T, int Hq, int Hkv, int D) {
   const int rw = attention_rw(T * (Hq / Hkv), false, D);
   return (size_t)kAtItems * 32 * rw * (D / 4 + 1) * sizeof(float4);
@@ -687,8 +714,7 @@ static sqa_status launch_attention(const AttentionArgs& a, hipStream_t st) {
 template <typename T, int D>
 static sqa_status launch_attention(int rw, const AttentionArgs& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
-    if (rw == 8) return start_attention(chunk_attention_wide_kernel<D, 8>, 512, 256 * D * 4, a, st);
-    if (rw == 4) return start_attention(chunk_attention_wide_kernel<D, 4>, 256, 128 * D * 4, a, st);
+    if (rw == 4) return start_attention(chunk_attention_wide_kernel<D>, kAtThreads, 128 * D * 4, a, st);
   }
   constexpr bool wide = D * sizeof(T) == 512;        // rows of 512 bytes: half the slots
   if constexpr (sizeof(T) == 4)
@@ -732,6 +758,13 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   a.near = 8.f / a.scale;
   a.group_m = 0xffffffffu / (uint32_t)a.c.g + 1;
   a.tiles = p.tiles; a.splits = p.splits;
+  // Row tiles of a unit see from new_pos to new_pos + T slots.  Where that is not much the same for all, an XCD (an eighth of the units)
+  // takes the longest of several units first, so that the launch ends in short ones.
+  a.group = 1;
+  // (8 x 32 heads x 2048 tokens 383 -> 363 us, one sequence of them 66 -> 59; 16 or 32 units at a time 378, 396.)
+  if (p.splits == 1 && p.tiles >= 8 && uniform && new_pos < T)
+    for (int k = 8; k > 1; k /= 2)
+      if ((int64_t)B * Hkv % (8 * k) == 0) { a.group = k; break; }
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dt == SQA_F32) return D == 64 ? sqa::launch_attention<float, 64>(p.rw, a, st) : sqa::launch_attention<float, 128>(p.rw, a, st);
