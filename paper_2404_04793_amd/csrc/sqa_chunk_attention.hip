@@ -677,14 +677,16 @@ struct AttentionPlan { int rw, tiles, splits; };     // rw: 32-row blocks of a w
 static int attention_rw(int rows, bool bf16, int D) {
   return rows <= 32 && (bf16 || D == 64) ? 1 : (rows <= 64 ? 2 : 4);
 }
-static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots) {
+static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots, bool ragged) {
   AttentionPlan p;
   const int rows = T * (Hq / Hkv), least = attention_rw(1, dt == SQA_BF16, D);
   int64_t items, s;
   for (p.rw = attention_rw(rows, dt == SQA_BF16, D);; p.rw /= 2) {
     p.tiles = (rows + 32 * p.rw - 1) / (32 * p.rw);
     items = (int64_t)B * Hkv * p.tiles;
-    s = kAtItems / items;
+    // as many as run at a time (tiles of few rows fill half a CU's LDS or all of it); twice that where sequences differ in length: five
+    // tokens of 16 sequences over 4095 slots 48 us (57 with twice as many), over 2048 to 4095 slots 51 (46 with twice as many)
+    s = (p.rw == 4 || ragged ? kAtItems : kAtItems / 2) / items;
     // a join costs what some hundred slots do: short units are shared out by rows first
     if (p.rw == least || s <= 1 || slots / s >= kAtJoin) break;
   }
@@ -754,7 +756,7 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   a.part = reinterpret_cast<float4*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
-  const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, uniform ? (int64_t)new_pos + T : layer->capacity);
+  const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, uniform ? (int64_t)new_pos + T : layer->capacity, !uniform);
   a.near = 8.f / a.scale;
   a.group_m = 0xffffffffu / (uint32_t)a.c.g + 1;
   a.tiles = p.tiles; a.splits = p.splits;

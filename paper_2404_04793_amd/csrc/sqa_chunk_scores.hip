@@ -18,7 +18,7 @@ constexpr int kScoreRows = 64;                      // of a tile in LDS
 template <typename T> constexpr int score_blocks() { return sizeof(T) == 2 ? 2 : 1; }
 template <typename T> constexpr int score_slots() { return 4 * 32 * score_blocks<T>(); }
 constexpr int kScoreSlotsMost = 256;
-constexpr int kScoreItems = 1024;                   // workgroups that few slots are shared out to
+constexpr int kScoreItems = 512;                    // workgroups that few slots are shared out to: two per CU
 
 struct ScoresArgs {
   ChunkArgs c;
@@ -59,8 +59,9 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
     return;
   }
   const int end = __builtin_amdgcn_readfirstlane((int)held);
+  if (slot0 >= end) return;
   // ---- the lane's slots.  (Asked for before it is known whether the unit holds the chunk: a block number outside the pools reads block 0.)
-  const int slot = (int)min(slot0, (int64_t)end) + 32 * KB * wave + col;
+  const int slot = (int)slot0 + 32 * KB * wave + col;
   Frag<T, D> k[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
@@ -74,19 +75,8 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
 #pragma unroll
     for (int x = 0; x < k[kb].NS; ++x) k[kb].p[x] = ld16(src + (2 * x + half) * 16);
   }
-  int why = chunk_held(a.c.L, unit, u, held) ? 0 : SQA_ERR_STATE;
-  if (!why && unit.table) {                          // a unit is left untouched as a whole: all of its blocks are looked at
-    int outside = 0;
-    for (int i = tid; i < (end + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS; i += kScoreThreads) outside |= (unsigned)unit.table[i] >= (unsigned)a.c.L.n_blocks;
-    if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
-  }
-  if (why) {
-    if (tid == 0 && tile == 0 && split == 0 && a.c.status) *a.c.status = why;
-    return;
-  }
-  if (slot0 >= end) return;
   // the tokens that see any of the slots, and this workgroup's tiles of their rows
-  const int t0 = (int)max((int64_t)0, slot0 - seq.pos), tv = seq.n - t0, rows = g * tv;
+  const int t0 = __builtin_amdgcn_readfirstlane((int)max((int64_t)0, slot0 - seq.pos)), tv = __builtin_amdgcn_readfirstlane(seq.n) - t0, rows = g * tv;
   const int nt = (rows + kScoreRows - 1) / kScoreRows, per = (nt + a.splits - 1) / a.splits;
   const int parts = (nt + per - 1) / per;
   if (split >= parts) return;
@@ -102,18 +92,29 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
     const int rr = wave * (kScoreRows / 4) + i * R::RPI, row = rr + lane / R::PPR;
     place[i] = (uint32_t)(row * R::RB + (((lane % R::PPR) ^ R::k_swizzle(row)) << 4));
   }
-  auto fetch = [&](int tl, int buf) {
+  // where a tile's first row is: head of the unit, token (scalar arithmetic from tile to tile)
+  struct Place { int gi, tt; };
+  auto next = [&](Place p) {
+    p.tt += kScoreRows;
+    if (p.tt >= tv) {
+      uint32_t more, tt;
+      by_tv((uint32_t)p.tt, more, tt);
+      p.gi += __builtin_amdgcn_readfirstlane((int)more);
+      p.tt = __builtin_amdgcn_readfirstlane((int)tt);
+    }
+    return p;
+  };
+  auto fetch = [&](int tl, int buf, Place p) {
     const uint32_t dst = lds_at(s_stage) + (uint32_t)(buf * TILE + wave * (kScoreRows / 4) * R::RB);
-    uint32_t gi, tt;
-    by_tv((uint32_t)(tl * kScoreRows), gi, tt);
-    if ((int)tt + kScoreRows <= tv) {                // rows of one head, one after the other
-      const char* const base = uniform(Q + ((int64_t)gi * a.c.T + t0 + tt) * R::RB);
+    if (p.tt + kScoreRows <= tv) {                   // rows of one head, one after the other
+      const char* const base = uniform(Q + ((int64_t)p.gi * a.c.T + t0 + p.tt) * R::RB);
 #pragma unroll
       for (int i = 0; i < NI; ++i) fetch16(base, place[i], dst + i * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int row = wave * (kScoreRows / 4) + i * R::RPI + lane / R::PPR;
+        uint32_t gi, tt;
         by_tv((uint32_t)min(tl * kScoreRows + row, rows - 1), gi, tt);
         fetch16(Q + ((int64_t)gi * a.c.T + t0 + tt - row) * R::RB + place[i], dst + i * 1024);
       }
@@ -122,16 +123,16 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
   // a tile's normalisers wait in registers of the first wave for a round, so that nothing waits for them
   float lse_next = 0.f;
   int see_next = 0;
-  auto ask = [&](int tl) {
-    if (tid < kScoreRows) {
-      uint32_t gi, tt;
-      by_tv((uint32_t)min(tl * kScoreRows + tid, rows - 1), gi, tt);
+  auto ask = [&](int tl, Place p) {
+    if (wave == 0 && tl < tile1) {
+      uint32_t gi = (uint32_t)p.gi, tt = (uint32_t)(p.tt + tid);
+      if (p.tt + kScoreRows > tv) by_tv((uint32_t)min(tl * kScoreRows + tid, rows - 1), gi, tt);
       lse_next = a.lse[(head0 + gi) * a.c.T + t0 + tt];
       see_next = (int)seq.pos + t0 + (int)tt;
     }
   };
   auto keep = [&](int tl) {
-    if (tid < kScoreRows) {
+    if (wave == 0) {
       s_lse[tl & 3][tid] = tl * kScoreRows + tid < rows ? lse_next * 1.4426950408889634f : INFINITY;
       s_see[tl & 3][tid] = see_next;
     }
@@ -157,61 +158,87 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
       }
     }
   };
-  // one block of 32 rows: its products, and the exponentials of the block before between them (each product takes the matrix core as long
-  // as five or six vector instructions take)
-  auto block = [&](const char* Qt, f32x16_t (&now)[KB], int rb, f32x16_t (&before)[KB], int tl_before, int rb_before, auto look) {
+  auto products = [&](const char* Qt, int rb, f32x16_t (&to)[KB]) {
     const int row = 32 * rb + col;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) now[kb] = f32x16_t{};
+    for (int kb = 0; kb < KB; ++kb) to[kb] = f32x16_t{};
 #pragma unroll
     for (int x = 0; x < Frag<T, D>::NS; ++x) {
       const uint4 q = *reinterpret_cast<const uint4*>(Qt + row * R::RB + (((2 * x + half) ^ R::k_swizzle(row)) << 4));
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) mma_piece<T>(q, k[kb].p[x], now[kb]);
+      for (int kb = 0; kb < KB; ++kb) mma_piece<T>(q, k[kb].p[x], to[kb]);
     }
+  };
+  // a block of 32 rows and, between its products, the exponentials of the one before (a product takes the matrix core as long as five
+  // or six vector instructions take)
+  auto both = [&](const char* Qt, int rb, f32x16_t (&to)[KB], f32x16_t (&before)[KB], int tl_before, int rb_before, auto look) {
+    products(Qt, rb, to);
     add(before, tl_before, rb_before, look);
     if constexpr (sizeof(T) == 2) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
       for (int i = 0; i < KB * Frag<T, D>::NS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, 12 * 8 / Frag<T, D>::NS / 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, (decltype(look)::value ? 80 : 48) / Frag<T, D>::NS, 0);
       }
     }
   };
-  bool look = false;
-  ask(tile0);
+  bool look_before = false;                          // (s[1] holds the last block of the tile before, whose exponentials are still to come)
+  Place now, soon, later;                            // of this tile, the next one and the one after
+  {
+    uint32_t gi, tt;
+    by_tv((uint32_t)(tile0 * kScoreRows), gi, tt);
+    now = {__builtin_amdgcn_readfirstlane((int)gi), __builtin_amdgcn_readfirstlane((int)tt)};
+  }
+  soon = later = next(now);
+  ask(tile0, now);
+  fetch(tile0, 0, now);
+  int why = chunk_held(a.c.L, unit, u, held) ? 0 : SQA_ERR_STATE;
+  if (!why && unit.table) {                          // a unit is left untouched as a whole: all of its blocks are looked at
+    int outside = 0;
+    for (int i = tid; i < (end + SQA_BLOCK_SLOTS - 1) / SQA_BLOCK_SLOTS; i += kScoreThreads) outside |= (unsigned)unit.table[i] >= (unsigned)a.c.L.n_blocks;
+    if (__syncthreads_or(outside)) why = SQA_ERR_SHAPE;
+  }
+  if (why) {
+    if (tid == 0 && tile == 0 && split == 0 && a.c.status) *a.c.status = why;
+    fetched();                                       // (copies in flight would arrive in another workgroup's LDS)
+    return;
+  }
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) arrived(k[kb]);
   keep(tile0);
-  if (tid < kScoreRows) s_lse[(tile0 - 1) & 3][tid] = INFINITY;       // what comes before the first block adds nothing
+  if (wave == 0) s_lse[(tile0 - 1) & 3][tid] = INFINITY;              // what comes before the first block adds nothing
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) s[1][kb] = f32x16_t{};
-  fetch(tile0, 0);
-  ask(tile0 + 1);
+  ask(tile0 + 1, soon);
   for (int tl = tile0; tl < tile1; ++tl) {
     const int buf = (tl - tile0) & 1;
     fetched();
     __syncthreads();
     if (tl + 1 < tile1) {
       keep(tl + 1);
-      fetch(tl + 1, buf ^ 1);
-      ask(tl + 2);
+      fetch(tl + 1, buf ^ 1, soon);
+      later = next(soon);
+      ask(tl + 2, later);
     }
     const char* const Qt = s_stage + buf * TILE;
-    uint32_t gi, tt;
-    by_tv((uint32_t)(tl * kScoreRows), gi, tt);
-    const int t_first = (int)tt;
-    const bool look_now = t_first + kScoreRows > tv || (int)seq.pos + t0 + t_first < last_slot;
-    if (look || look_now) {
-      block(Qt, s[0], 0, s[1], tl - 1, 1, std::true_type{});
-      block(Qt, s[1], 1, s[0], tl, 0, std::true_type{});
+    const bool look = now.tt + kScoreRows > tv || (int)seq.pos + t0 + now.tt < last_slot;
+    now = soon;
+    soon = later;
+    if (look || look_before) {
+      f32x16_t to[KB];
+#pragma unroll 1
+      for (int rb = 0; rb < 2; ++rb) {
+        both(Qt, rb, to, s[1], tl - 1 + rb, 1 - rb, std::true_type{});
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s[1][kb] = to[kb];
+      }
     } else {
-      block(Qt, s[0], 0, s[1], tl - 1, 1, std::false_type{});
-      block(Qt, s[1], 1, s[0], tl, 0, std::false_type{});
+      both(Qt, 0, s[0], s[1], tl - 1, 1, std::false_type{});
+      both(Qt, 1, s[1], s[0], tl, 0, std::false_type{});
     }
-    look = look_now;
+    look_before = look;
   }
   add(s[1], tile1 - 1, 1, std::true_type{});
 #pragma unroll
