@@ -5,6 +5,11 @@
 
 namespace sqa {
 
+__device__ __forceinline__ uint32_t pair(float lo, float hi) {                           // two bf16, round to nearest even
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
+}
+
 struct ChunkSeq { int n; int64_t pos; };            // tokens of a sequence in this call, position of the first
 
 struct ChunkArgs {                                  // (by value to the kernels)

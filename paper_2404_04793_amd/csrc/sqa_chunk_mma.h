@@ -40,10 +40,6 @@ __device__ __forceinline__ const char* uniform(const char* p) {
 __device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ uint32_t pair(float lo, float hi) {                           // two bf16, round to nearest even
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
-}
 __device__ __forceinline__ float other_half_max(float v) {
   typedef unsigned u2_t __attribute__((ext_vector_type(2)));
   const u2_t r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

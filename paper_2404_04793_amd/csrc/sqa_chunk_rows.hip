@@ -41,10 +41,16 @@ template <> struct Piece<bf16_t> {
   static __device__ __forceinline__ uint4 close(const float* x) {
     uint32_t v[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = f32_to_bf16_bits(x[2 * i]) | (f32_to_bf16_bits(x[2 * i + 1]) << 16);
+    for (int i = 0; i < 4; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
     return make_uint4(v[0], v[1], v[2], v[3]);
   }
 };
+
+// the value of the lane half a row away, rows of LPR lanes: where a whole head is rotated
+template <int LPR> __device__ __forceinline__ float half_row_away(float v) {
+  if constexpr (LPR == 16) return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true));      // row_ror:8
+  else return __shfl_xor(v, LPR / 2, LPR);
+}
 
 // May a unit take the chunk?  What its LPR lanes (lane c of them) have to know is asked for before the rows are worked on, all at
 // once, and judged afterwards.  Other waves of the launch may have set the unit's state meanwhile: what is asked holds before and
@@ -168,7 +174,7 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float other = __shfl(y[e], partner);
+          const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
           const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
           y[e] = mine ? z : y[e];
         }
@@ -226,11 +232,12 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   a.kv_groups = (a.k_out || a.c.L.K) ? (a.c.Hkv + HPW - 1) / HPW : 0;
   const int64_t groups = (int64_t)a.c.B * (a.q_groups + a.kv_groups);
   constexpr int waves = kRowsThreads / SQA_WAVE;
-  // four tokens per wave where that leaves every SIMD a wave, otherwise one
-  const bool four = groups * ((a.c.T + 3) / 4) >= 1024;
-  a.t_blocks = four ? (a.c.T + 3) / 4 : a.c.T;
+  // two tokens per wave where that leaves every SIMD a wave, otherwise one.  (4 x 2048 tokens of 32 + 8 heads: 35.7 us with two, 39.1
+  // with four, 42.3 with one; rows stored non-temporally 34.7, but what reads them next is slower by more.)
+  const bool two = groups * ((a.c.T + 1) / 2) >= 1024;
+  a.t_blocks = two ? (a.c.T + 1) / 2 : a.c.T;
   const int64_t blocks = (groups * a.t_blocks + waves - 1) / waves;
-  if (four) chunk_rows_kernel<T, D, 4><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
+  if (two) chunk_rows_kernel<T, D, 2><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
   else chunk_rows_kernel<T, D, 1><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
 }
 
