@@ -62,6 +62,39 @@ template <typename T, int BYTES, int NT, bool CLEAR> __device__ __forceinline__ 
   return odd;
 }
 
+// Adds the values of slots from .. from + n - 1 of a tile in LDS that are not finite to the sums of the rows that see them.
+template <typename T, int D>
+__device__ __forceinline__ void add_odd_values(const char* Vt, int from, int n, int tile_slot, int see, int half, f32x16_t (&o)[D / 32]) {
+  using R = TileRows<T, D>;
+  constexpr int NB = D / 32;
+#pragma unroll 1
+  for (int k = from; k < from + n; ++k) {
+    const bool sees = tile_slot + k <= see;
+    const char* const row = Vt + k * R::RB;
+    if constexpr (sizeof(T) == 2) {
+      const int swz = R::v_swizzle(k) << 4;
+#pragma unroll
+      for (int e = 0; e < NB; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const uint2 v = *reinterpret_cast<const uint2*>(row + ((64 * e + 4 * i) ^ swz) + 8 * half);
+          o[e][i] += sees && odd_mask(v.x << 16) ? bf16_lo(v.x) : 0.f;
+          o[e][i + 1] += sees && odd_mask(v.x & 0xffff0000u) ? bf16_hi(v.x) : 0.f;
+          o[e][i + 2] += sees && odd_mask(v.y << 16) ? bf16_lo(v.y) : 0.f;
+          o[e][i + 3] += sees && odd_mask(v.y & 0xffff0000u) ? bf16_hi(v.y) : 0.f;
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < NB; ++e) {
+          const float v = reinterpret_cast<const float*>(row + 4 * NB * c_row(0, half))[NB * c_row(i, 0) + e];
+          o[e][i] += sees && !isfinite(v) ? v : 0.f;
+        }
+    }
+  }
+}
+
 // What a workgroup of NT threads works on: M rows of one unit and a run of its slots, in tiles of KT.
 template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
   using R = TileRows<T, D>;
@@ -379,22 +412,7 @@ __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const At
     // A slot that a row does not see has probability 0, but 0 x NaN is NaN: where some rows do not see all of the tile, its
     // values that are not finite are added to the sums of the rows that see them one by one, and are 0 for the product.
     if (tl * KT + KT - 1 > see_all_tile && __syncthreads_or(odd_values<T, C::TILE, kAtThreads, false>(s_stage + buf * 2 * C::TILE + C::TILE))) {
-#pragma unroll 1
-      for (int k = 0; k < 32 * KB; ++k) {
-        const int row = key0 + k;
-        const bool seen = tl * KT + row <= see;
-#pragma unroll
-        for (int e = 0; e < NB; ++e)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int d = sizeof(T) == 2 ? 32 * e + c_row(i, half) : NB * c_row(i, half) + e;
-            const int at = row * R::RB + (((d / R::E) ^ R::v_swizzle(row)) << 4) + d % R::E * (int)sizeof(T);
-            float v;
-            if constexpr (sizeof(T) == 2) v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(Vt + at) << 16);
-            else v = *reinterpret_cast<const float*>(Vt + at);
-            if (seen && !isfinite(v)) o[e][i] += v;
-          }
-      }
+      add_odd_values<T, D>(Vt, key0, 32 * KB, tl * KT, see, half, o);
       __syncthreads();
       odd_values<T, C::TILE, kAtThreads, true>(s_stage + buf * 2 * C::TILE + C::TILE);
       __syncthreads();
@@ -603,23 +621,7 @@ template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attentio
   auto take_odd_values = [&](int j) {
     char* const Vt = s_stage + (2 + (j & 1)) * TILE;
     if (!__syncthreads_or(odd_values<T, TILE, kAtThreads, false>(Vt))) return;
-    const int first = (w.tile0 + j) * kWideSlots;
-#pragma unroll 1
-    for (int k = 0; k < kWideSlots; ++k) {
-      const bool sees = first + k <= see;
-      const char* const row = Vt + k * R::RB + 8 * half;
-      const int swz = R::v_swizzle(k) << 4;
-#pragma unroll
-      for (int e = 0; e < NB; ++e)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const uint2 v = *reinterpret_cast<const uint2*>(row + ((64 * e + 4 * i) ^ swz));
-          o[e][i] += sees && odd_mask(v.x << 16) ? bf16_lo(v.x) : 0.f;
-          o[e][i + 1] += sees && odd_mask(v.x & 0xffff0000u) ? bf16_hi(v.x) : 0.f;
-          o[e][i + 2] += sees && odd_mask(v.y << 16) ? bf16_lo(v.y) : 0.f;
-          o[e][i + 3] += sees && odd_mask(v.y & 0xffff0000u) ? bf16_hi(v.y) : 0.f;
-        }
-    }
+    add_odd_values<T, D>(Vt, 0, kWideSlots, (w.tile0 + j) * kWideSlots, see, half, o);
     __syncthreads();
     odd_values<T, TILE, kAtThreads, true>(Vt);
     __syncthreads();

@@ -15,7 +15,8 @@ from . import workloads as W
 class Session:
     def __init__(self, wl: W.Workload, device="cuda:0", keep_prompt_q: bool = False, uniform_budget: bool = False,
                  full_cache: bool = False, probe_tokens: Optional[int] = None, fused_probe: bool = False,
-                 order: str = "evict_then_attend", prompt_len: Optional[List[int]] = None, blocked: bool = False):
+                 order: str = "evict_then_attend", prompt_len: Optional[List[int]] = None, blocked: bool = False,
+                 prompt_chunk: Optional[int] = None):
         """probe_tokens: hidden-state rows per layer given to the probe (default: all B*P prompt tokens;
         a smaller number keeps the hidden states of the largest workloads within HBM).
         fused_probe: the probe runs inside the residual add that writes h_out (Sec. 3).
@@ -23,7 +24,10 @@ class Session:
         tensors stay padded to P); each sequence is then probed and budgeted on its own
         (sqa_layer_importance_seq, one sqa_allocate_budgets per sequence) and decodes at its own position.
         blocked: K and V of every layer live in pools of 16-row blocks that a block table deals to the units
-        (in a seeded random order, so that no unit is contiguous)."""
+        (in a seeded random order, so that no unit is contiguous).
+        prompt_chunk: the prompt comes in pieces of that many tokens, as a serving loop feeds it: each is appended to
+        an uncompressed layer, attends it and (H2O) adds to its accumulated scores; what compression then takes is that
+        layer.  Otherwise the prompt is there whole and its scores come from sqa_prefill_scores."""
         self.wl, self.dev = wl, device
         self.blocked = blocked
         assert not (blocked and prompt_len is not None)
@@ -60,6 +64,15 @@ class Session:
         self.Kp, self.Vp, self.scores, self.Qp = [], [], [], []
         for l in range(L):
             K, V = W.prompt_kv(wl, l, device, self.u, self.mask)
+            if prompt_chunk is not None:
+                Q = W.prompt_q(wl, l, device, self.u)
+                K, V, score = self._prompt_in_chunks(Q, K, V, int(prompt_chunk))
+                self.Kp.append(K); self.Vp.append(V)
+                self.scores.append(score if wl.policy == "h2o" else None)
+                if keep_prompt_q:
+                    self.Qp.append(Q)
+                del Q
+                continue
             self.Kp.append(K); self.Vp.append(V)
             if wl.policy == "h2o":
                 Q = W.prompt_q(wl, l, device, self.u)
@@ -88,6 +101,28 @@ class Session:
         self.budgets: Optional[List[int]] = None
         self.groups: Optional[List[int]] = None
         torch.cuda.synchronize()
+
+    # -- the prompt of one layer, a chunk at a time --------------------------------
+    def _prompt_in_chunks(self, Q, K, V, chunk: int):
+        """Q [B, Hq, P, D], K, V [B, Hkv, P, D] of one layer -> K, V and accumulated scores [B, Hkv, P] of an uncompressed
+        layer that has taken them in chunks (the generated keys carry their positions already: nothing is rotated)."""
+        wl = self.wl
+        B, Hq, P, D = Q.shape
+        layer = sqa.LayerCaches([P], [P], B, wl.Hkv, D, wl.torch_dtype, self.dev, True)
+        ws = sqa.chunk_workspace(layer, Hq, min(chunk, P))
+        opts = None
+        for at in range(0, P, chunk):
+            n = min(chunk, P - at)
+            if self.ragged:                                # sequences whose prompt has ended take no part
+                left = (self.plen_dev - at).clamp(min=0, max=n).to(torch.int32)
+                opts = sqa.batch_opts(prompt_len=left, new_pos_seq=torch.where(left > 0, at, -1).to(torch.int32), status=self.status)
+            k, v = (x[:, :, at:at + n].transpose(1, 2).contiguous() for x in (K, V))
+            q = Q[:, :, at:at + n].contiguous()
+            sqa.chunk_append(k, v, at, layer, opts=opts)
+            _, lse = sqa.chunk_attention(q, at, layer, workspace=ws, opts=opts)
+            if wl.policy == "h2o":
+                sqa.chunk_scores(q, lse, at, layer, workspace=ws, opts=opts)
+        return layer.K[0], layer.V[0], layer.score[0]
 
     # -- Algorithm 1 steps 1-11 ------------------------------------------------
     def probe_and_allocate(self):
