@@ -604,13 +604,8 @@ def head_prep(q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.
 # (The calls below are kept short, their checks among them: in a model that makes them once per layer, the host's part of a small
 # chunk's call is longer than its kernel.)
 
-def _token_rows(t: torch.Tensor, D: int) -> array:
-    """sqa_token_rows of [B, T, H, D], dense within a token: a projection's output, a part of a packed one, or a slice of a
-    longer prompt."""
-    seq, row, head, one = t.stride()
-    if head != D and t.shape[2] != 1 or one != 1:
-        raise TypeError("heads of a token lie one after the other: [B, T, H, D] with strides (.., .., D, 1)")
-    return array("q", (t.data_ptr(), seq, row))
+_ROWS_BYTES = C.sizeof(TokenRowsStruct)
+_ARRAY = "heads of a token lie one after the other: [B, T, H, D] with strides (.., .., D, 1)"
 
 
 def _check_out(t: torch.Tensor, shape, dtype) -> None:
@@ -618,9 +613,10 @@ def _check_out(t: torch.Tensor, shape, dtype) -> None:
         raise TypeError("expected a contiguous %s tensor %s" % (dtype, tuple(shape)))
 
 
-def _check_device(dev: int, *others: int) -> None:
+def _check_device(devices) -> None:
     """The library runs on the current device's stream: tensors of the host or of another device are refused."""
-    if dev < 0 or dev != _get_device() or any(o != dev for o in others):
+    dev = devices[0]
+    if dev < 0 or dev != _get_device() or devices.count(dev) != len(devices):
         raise ValueError("a tensor is not on the current device")
 
 
@@ -644,33 +640,42 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: 
         raise TypeError("queries or keys")
     B, T, Hq, D = some.shape
     Hkv, dtype, dev = Hq, some.dtype, some.get_device()
-    q_rows = k_rows = q_to = k_to = None
+    rows, devices, q_to, k_to = [], [dev], None, None      # sqa_token_rows one after the other
     if q is not None:
-        q_rows = _token_rows(q, D)
+        seq, row, head, one = q.stride()
+        if one != 1 or head != D and Hq != 1:
+            raise TypeError(_ARRAY)
+        rows += (q.data_ptr(), seq, row)
         if q_out is None:
             q_out = torch.empty((B, Hq, T, D), dtype=dtype, device=q.device)
         else:
             _check_out(q_out, (B, Hq, T, D), dtype)
         q_to = q_out.data_ptr()
+        devices.append(q_out.get_device())
     elif q_out is not None:
         raise TypeError("an output without its input")
     if k is not None:
         kB, kT, Hkv, kD = k.shape
         if kB != B or kT != T or kD != D or k.dtype != dtype:
             raise TypeError("queries and keys of the same tokens, head size and dtype")
-        k_rows = _token_rows(k, D)
+        seq, row, head, one = k.stride()
+        if one != 1 or head != D and Hkv != 1:
+            raise TypeError(_ARRAY)
+        rows += (k.data_ptr(), seq, row)
         if k_out is None:
             k_out = torch.empty((B, Hkv, T, D), dtype=dtype, device=k.device)
         else:
             _check_out(k_out, (B, Hkv, T, D), dtype)
         k_to = k_out.data_ptr()
+        devices += (k.get_device(), k_out.get_device())
     elif k_out is not None:
         raise TypeError("an output without its input")
+    rows = array("q", rows)
+    at = rows.buffer_info()[0]
     how = _prep(prep, dtype, D, dev)
-    _check_device(dev, *[t.get_device() for t in (k, q_out, k_out) if t is not None])
-    code = _lib.sqa_qk_norm_rope(None if q is None else q_rows.buffer_info()[0], None if k is None else k_rows.buffer_info()[0],
-                                 _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos, q_to, k_to, _stream(),
-                                 None if opts is None else C.addressof(opts))
+    _check_device(devices)
+    code = _lib.sqa_qk_norm_rope(None if q is None else at, None if k is None else at if q is None else at + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos,
+                                 q_to, k_to, _stream(), None if opts is None else C.addressof(opts))
     if code != SQA_OK:
         raise SqaError(code, "sqa_qk_norm_rope")
     return q_out, k_out
@@ -691,30 +696,38 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
     """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
     way; with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
     B, T, Hkv, D = k.shape
-    dtype, dev, Hq, q_rows, q_to = k.dtype, k.get_device(), Hkv, None, None
+    dtype, dev, Hq, q_to = k.dtype, k.get_device(), Hkv, None
     at = _layer_at(caches, layer, dtype, B, Hkv, D)
     if v.shape != k.shape or v.dtype != dtype:
         raise TypeError("keys and values of one shape and dtype")
-    k_rows, v_rows = _token_rows(k, D), _token_rows(v, D)
-    devices = [v.get_device(), caches.K[layer].get_device()]
-    if q is not None:
+    k_seq, k_row, k_head, k_one = k.stride()
+    v_seq, v_row, v_head, v_one = v.stride()
+    if k_one != 1 or v_one != 1 or (k_head != D or v_head != D) and Hkv != 1:
+        raise TypeError(_ARRAY)
+    devices = [dev, v.get_device(), caches.K[layer].get_device()]
+    if q is None:
+        if q_out is not None:
+            raise TypeError("an output without its input")
+        rows = array("q", (k.data_ptr(), k_seq, k_row, v.data_ptr(), v_seq, v_row))
+    else:
         qB, qT, Hq, qD = q.shape
         if qB != B or qT != T or qD != D or q.dtype != dtype:
             raise TypeError("queries and keys of the same tokens, head size and dtype")
-        q_rows = _token_rows(q, D)
+        seq, row, head, one = q.stride()
+        if one != 1 or head != D and Hq != 1:
+            raise TypeError(_ARRAY)
         if q_out is None:
             q_out = torch.empty((B, Hq, T, D), dtype=dtype, device=q.device)
         else:
             _check_out(q_out, (B, Hq, T, D), dtype)
         q_to = q_out.data_ptr()
-        devices += [q.get_device(), q_out.get_device()]
-    elif q_out is not None:
-        raise TypeError("an output without its input")
+        devices += (q.get_device(), q_out.get_device())
+        rows = array("q", (k.data_ptr(), k_seq, k_row, v.data_ptr(), v_seq, v_row, q.data_ptr(), seq, row))
     how = _prep(prep, dtype, D, dev)
-    _check_device(dev, *devices)
-    code = _lib.sqa_chunk_append(None if q is None else q_rows.buffer_info()[0], k_rows.buffer_info()[0], v_rows.buffer_info()[0],
-                                 _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos, q_to, at, _stream(),
-                                 None if opts is None else C.addressof(opts))
+    _check_device(devices)
+    first = rows.buffer_info()[0]                            # sqa_token_rows one after the other: keys, values, queries
+    code = _lib.sqa_chunk_append(None if q is None else first + 2 * _ROWS_BYTES, first, first + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq,
+                                 Hkv, D, how, new_pos, q_to, at, _stream(), None if opts is None else C.addressof(opts))
     if code != SQA_OK:
         raise SqaError(code, "sqa_chunk_append")
     return q_out
@@ -750,7 +763,7 @@ def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer:
         _check_out(lse, (B, Hq, T), torch.float32)
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
-    _check_device(dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device())
+    _check_device([dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
     code = _lib.sqa_chunk_attention(q.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, out.data_ptr(), lse.data_ptr(),
                                     workspace.data_ptr(), workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
     if code != SQA_OK:
@@ -771,7 +784,7 @@ def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "Laye
         raise TypeError("lse is a contiguous fp32 tensor [B, Hq, T]")
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
-    _check_device(dev, lse.get_device(), workspace.get_device(), caches.K[layer].get_device())
+    _check_device([dev, lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
     code = _lib.sqa_chunk_scores(q.data_ptr(), lse.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, workspace.data_ptr(),
                                  workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
     if code != SQA_OK:
