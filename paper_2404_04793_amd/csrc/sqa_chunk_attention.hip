@@ -301,8 +301,9 @@ template <typename T, int D, int RW, int KT> struct AttentionTile {
   static constexpr int STAGE = 4 * TILE > 4 * 32 * D * 4 ? 4 * TILE : 4 * 32 * D * 4;
 };
 
+// (Rows of 512 bytes and tiles of 64 slots fill a CU's LDS: one wave per SIMD, and registers for it.)
 template <typename T, int D, int RW, int KT>
-__global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kAtThreads, KT * D * sizeof(T) == 64 * 512 && RW == 2 ? 1 : 2) void chunk_attention_kernel(const AttentionArgs a) {
   using C = AttentionTile<T, D, RW, KT>;
   using R = TileRows<T, D>;
   constexpr int KW = C::KW, KB = C::KB, M = C::M, NB = C::NB;
