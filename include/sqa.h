@@ -493,8 +493,9 @@ size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int
  *         sqa_prefill_scores_lse and sqa_chunk_scores
  * The softmax is in fp32; in bf16 the probabilities are rounded to bf16 for the product with V, as in sqa_decode_step on the
  * matrix cores.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
- * A unit that does not hold the chunk at its slots (see sqa_chunk_append) gets rows of zeros and lse -inf, status
- * SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  Results are the same from run to run. */
+ * A unit that does not hold the chunk (too few tokens, a ring that has turned, another token in the chunk's last slot) gets rows of
+ * zeros and lse -inf, status SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  That is not a search for evicted tokens:
+ * the call belongs between the append and the first eviction after it.  Results are the same from run to run. */
 sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
                                const sqa_layer_cache* layer, void* out, float* lse,
                                void* workspace, size_t ws_bytes, void* stream, const sqa_batch_opts* opts);

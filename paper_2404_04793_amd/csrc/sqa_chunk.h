@@ -82,7 +82,7 @@ inline bool bad_layer(const sqa_layer_cache& c, sqa_status* why) {
 
 inline bool bad_chunk_shape(int B, int T, int Hq, int Hkv, int D, int32_t new_pos, const sqa_batch_opts* opts) {
   return B < 1 || T < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || (D != 64 && D != 128) || (int64_t)B * Hq > INT32_MAX / T ||
-         (new_pos < 0 && !(opts && opts->new_pos_seq)) || (int64_t)new_pos + T > INT32_MAX;
+         (!(opts && opts->new_pos_seq) && (new_pos < 0 || (int64_t)new_pos + T > INT32_MAX));
 }
 
 inline ChunkArgs chunk_args(const sqa_layer_cache* layer, int B, int T, int Hq, int Hkv, int32_t new_pos, const sqa_batch_opts* opts) {

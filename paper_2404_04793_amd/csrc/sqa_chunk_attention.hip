@@ -460,7 +460,8 @@ __global__ __launch_bounds__(kAtThreads, KT * D * sizeof(T) == 64 * 512 && RW ==
 // are seldom multiplied.  Tiles that not all rows see are worked off afterwards, one after the other.
 constexpr int kWideSlots = 64;
 
-__device__ __forceinline__ void part_done() { asm volatile("s_barrier" ::: "memory"); }
+// (Copies stay in flight; what was read from LDS has arrived, so that the buffers may be overwritten.)
+__device__ __forceinline__ void part_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attention_wide_kernel(const AttentionArgs a) {
   constexpr int NW = kAtThreads / 64, kWideRows = 32 * NW;

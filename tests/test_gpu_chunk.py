@@ -458,6 +458,68 @@ def test_from_another_stream(sqa):
     assert R.same(want, got)
 
 
+def test_new_pos_is_not_looked_at_where_each_sequence_has_its_own(sqa):
+    dt, _, c, q, opts, status = setup(sqa, "bf16", 64, "dense", 2, 5, [30, 7], 4, 2, [5, 3], 9)
+    k = torch.randn(2, 5, 2, 64, device=DEV, generator=generator(9)).to(dt)
+    got = []
+    for new_pos in (0, -5, 2 ** 31 - 1, -2 ** 31):
+        x = torch.zeros(2, 4, 5, 64, dtype=dt, device=DEV)
+        sqa.chunk_append(k, k, new_pos, c, q=q.transpose(1, 2).contiguous(), q_out=x, opts=opts)
+        out, lse = torch.zeros(2, 5, 4, 64, dtype=dt, device=DEV), torch.zeros(2, 4, 5, device=DEV)
+        sqa.chunk_attention(x, new_pos, c, out=out, lse=lse, opts=opts)
+        c.score[0].zero_()
+        sqa.chunk_scores(x, lse, new_pos, c, opts=opts)
+        got.append([x, out, lse, c.score[0].clone()])
+    assert int(status) == 0 and all(R.same(got[0], other) for other in got[1:])
+
+
+def test_sequences_that_take_no_part(sqa):
+    """All of them out, by position or by length: nothing is read or written."""
+    dt, _, c, q, _, _ = setup(sqa, "bf16", 128, "blocked", 2, 70, [30, 7], 4, 2, [0, 0], 9)
+    k = torch.full((2, 70, 2, 128), math.nan, dtype=dt, device=DEV)
+    ws = sqa.chunk_workspace(c, 4, 70)
+    for pos, n in ((ints([-1, -7]), None), (None, ints([0, 0])), (ints([-1, 3]), ints([70, 0]))):
+        status = ints([0])
+        opts = sqa.batch_opts(prompt_len=n, new_pos_seq=pos, status=status)
+        outs = [torch.full((2, 4, 70, 128), 3.0, dtype=dt, device=DEV), torch.full((2, 70, 4, 128), 3.0, dtype=dt, device=DEV),
+                torch.full((2, 4, 70), 3.0, device=DEV)]
+        before = [t.clone() for t in outs] + R.snapshot(c)
+        sqa.chunk_append(k, k, 0, c, q=q.transpose(1, 2).contiguous(), q_out=outs[0], opts=opts)
+        sqa.chunk_attention(q, 0, c, out=outs[1], lse=outs[2], workspace=ws, opts=opts)
+        sqa.chunk_scores(q, outs[2], 0, c, workspace=ws, opts=opts)
+        assert int(status) == 0 and R.same(before, outs + R.snapshot(c))
+    assert bool((ws[:4096] == 0).all())
+
+
+def test_two_calls_at_once(sqa):
+    """Two layers' calls on two streams, a workspace each: what each gives alone."""
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    made = [setup(sqa, "bf16", 128, layout, 4, T, [3000] * 4, 8, 2, None, 20 + T) for layout, T in (("dense", 4), ("blocked", 300))]
+    wss = [sqa.chunk_workspace(m[2], 8, m[3].shape[2]) for m in made]
+
+    def run(i):
+        c, q = made[i][2], made[i][3]
+        out, lse = sqa.chunk_attention(q, 3000, c, workspace=wss[i])
+        sqa.chunk_scores(q, lse, 3000, c, workspace=wss[i])
+        return [out, lse]
+
+    alone, score0 = [], [m[2].score[0].clone() for m in made]
+    for i in range(2):
+        alone.append(run(i) + [made[i][2].score[0].clone()])
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for i in range(2):
+            made[i][2].score[0].copy_(score0[i])
+        torch.cuda.synchronize()
+        got = [None, None]
+        for i in range(2):
+            with torch.cuda.stream(sides[i]):
+                got[i] = run(i)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert R.same(alone[i], got[i] + [made[i][2].score[0]])
+
+
 def test_captured_and_replayed(sqa):
     """A chunk's three calls in a HIP graph, positions and inputs changing between the replays, two graphs on one workspace."""
     B, T, Hq, Hkv, D, dt, gen = 2, 4, 8, 2, 128, torch.bfloat16, generator(8)
