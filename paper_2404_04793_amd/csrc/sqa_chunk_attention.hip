@@ -25,7 +25,7 @@ struct AttentionArgs {
   void* out;
   float* lse;
   int32_t* count;                                   // [items]
-  float4* part;                                     // [items][splits][32 RW][D / 4 + 1]: a row's sums, then (m, l)
+  float4* part;                                     // [items]: [splits][32 RW][D / 4] rows of sums, [splits][32 RW] (m, l)
   float scale;                                      // log2(e) / sqrt(D)
   float near;                                       // 8 / scale: logits that close to a row's reference do not move it
   uint32_t group_m;                                 // 2^32 / g, for divisions by g
@@ -99,7 +99,7 @@ __device__ __forceinline__ void add_odd_values(const char* Vt, int from, int n, 
 template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
   using R = TileRows<T, D>;
   static constexpr int PP = D / 4;                  // 16-byte pieces of a row of sums
-  static constexpr int REC = D / 4 + 1;             // a row of sums and its (m, l), in 16 bytes
+  static constexpr int REC = PP + 1;                // a row of sums and its (m, l)
   int64_t item;
   int u, b, h, g, n, row0, rows, last_row;          // n tokens, rows of the whole unit
   int split, parts, tile0, tile1, end;              // end: the slots that the rows see
@@ -254,42 +254,57 @@ template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
     }
     const char* const base = uniform(reinterpret_cast<const char*>(a.part + item * a.splits * (M * REC)));
     const HandOver rec(reinterpret_cast<float4*>(const_cast<char*>(base)), (uint32_t)(a.splits * (M * REC * 16)));
-    for (int i = tid; i < live; i += NT) {
-      const int row = i / (PP / 2), p = i % (PP / 2);
-      const uint32_t to = (uint32_t)((split * M + row) * REC);
-      rec.put(to + 2 * p, piece4(row, 2 * p));
-      rec.put(to + 2 * p + 1, piece4(row, 2 * p + 1));
-      if (p == 0) {
-        float mm, ll;
-        joined(row, mm, ll);
-        rec.put(to + PP, make_float4(mm, ll, 0.f, 0.f));
-      }
+    const uint32_t refs = (uint32_t)(a.splits * M * PP);                                     // all rows' sums, then all rows' (m, l)
+    for (int i = tid; i < 2 * live; i += NT) rec.put((uint32_t)(split * M * PP + i), piece4(i / PP, i % PP));
+    for (int row = tid; row <= last_row - row0; row += NT) {
+      float mm, ll;
+      joined(row, mm, ll);
+      rec.put(refs + split * M + row, make_float4(mm, ll, 0.f, 0.f));
     }
     if (!last_to_arrive(a.count + item, parts, s_word)) return;
-    for (int i = tid; i < live; i += NT) {
-      const int row = i / (PP / 2), p = i % (PP / 2);
-      float mm = -FLT_MAX, ll = 0.f;
-      float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-      for (int k0 = 0; k0 < parts; k0 += 4) {        // four records in flight; in order
-        float4 ml[4], x[4], y[4];
+    // eight records' loads in flight: of one piece where every thread has one at most, otherwise of several
+    if (live <= NT) join<1, 8>(a, rec, refs, live);
+    else if (parts == 2) join<(M * PP / 2 < 4 * NT ? 2 : 4), 2>(a, rec, refs, live);
+    else join<2, 4>(a, rec, refs, live);
+  }
+
+  // the records of all workgroups of these rows added up in order and stored: NI pieces of 32 bytes, K records of each in flight
+  template <int NI, int K> __device__ __forceinline__ void join(const AttentionArgs& a, const HandOver& rec, uint32_t refs, int live) const {
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < live; i0 += NI * NT) {
+      float mm[NI], ll[NI];
+      float4 v[NI][2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t from = (uint32_t)((min(k0 + k, parts - 1) * M + row) * REC);
-          ml[k] = rec.get(from + PP); x[k] = rec.get(from + 2 * p); y[k] = rec.get(from + 2 * p + 1);
-        }
+      for (int x = 0; x < NI; ++x) { mm[x] = -FLT_MAX; ll[x] = 0.f; v[x][0] = v[x][1] = make_float4(0.f, 0.f, 0.f, 0.f); }
+#pragma unroll 1
+      for (int k0 = 0; k0 < parts; k0 += K) {
+        float4 ml[NI][K], lo[NI][K], hi[NI][K];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k0 + k < parts) {
-            const float top = fmaxf(mm, ml[k].x), w0 = exp2_fast((mm - top) * a.scale), w1 = exp2_fast((ml[k].x - top) * a.scale);
-            mm = top;
-            ll = fmaf(ll, w0, ml[k].y * w1);
-            v[0].x = fmaf(v[0].x, w0, x[k].x * w1); v[0].y = fmaf(v[0].y, w0, x[k].y * w1);
-            v[0].z = fmaf(v[0].z, w0, x[k].z * w1); v[0].w = fmaf(v[0].w, w0, x[k].w * w1);
-            v[1].x = fmaf(v[1].x, w0, y[k].x * w1); v[1].y = fmaf(v[1].y, w0, y[k].y * w1);
-            v[1].z = fmaf(v[1].z, w0, y[k].z * w1); v[1].w = fmaf(v[1].w, w0, y[k].w * w1);
+        for (int x = 0; x < NI; ++x)
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            const int i = min(i0 + x * NT, live - 1), row = i / (PP / 2), p = i % (PP / 2);
+            const uint32_t from = (uint32_t)(min(k0 + k, parts - 1) * M + row);
+            ml[x][k] = rec.get(refs + from); lo[x][k] = rec.get(from * PP + 2 * p); hi[x][k] = rec.get(from * PP + 2 * p + 1);
           }
+#pragma unroll
+        for (int x = 0; x < NI; ++x)
+#pragma unroll
+          for (int k = 0; k < K; ++k)
+            if (k0 + k < parts) {
+              const float top = fmaxf(mm[x], ml[x][k].x), w0 = exp2_fast((mm[x] - top) * a.scale), w1 = exp2_fast((ml[x][k].x - top) * a.scale);
+              mm[x] = top;
+              ll[x] = fmaf(ll[x], w0, ml[x][k].y * w1);
+              const float4 l4 = lo[x][k], h4 = hi[x][k];
+              v[x][0] = make_float4(fmaf(v[x][0].x, w0, l4.x * w1), fmaf(v[x][0].y, w0, l4.y * w1), fmaf(v[x][0].z, w0, l4.z * w1), fmaf(v[x][0].w, w0, l4.w * w1));
+              v[x][1] = make_float4(fmaf(v[x][1].x, w0, h4.x * w1), fmaf(v[x][1].y, w0, h4.y * w1), fmaf(v[x][1].z, w0, h4.z * w1), fmaf(v[x][1].w, w0, h4.w * w1));
+            }
       }
-      store8(a, row, p, v, mm, ll);
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        const int i = i0 + x * NT;
+        if (i < live) store8(a, i / (PP / 2), i % (PP / 2), v[x], mm[x], ll[x]);
+      }
     }
   }
 };
