@@ -3,8 +3,11 @@
 // The normalisers are known, so this is one product and a sum down its columns.  A wave keeps the keys of one or two
 // blocks of 32 slots in registers and walks the rows (head by head, only the tokens that see its workgroup's slots), 64 at a time in LDS
 // with two buffers:
-//   S = Q.K^T    a lane holds 16 of 32 rows of one slot and adds them up by itself; the two lane halves meet at the end.  The
-//                exponentials of one block of rows are independent of the next one's products and are taken meanwhile
+//   S^T = K.Q^T  a lane holds 16 of 32 slots of one row and adds up each by itself, over its rows: one normaliser per lane and
+//                block, and no sum across lanes before the end.  The exponentials of one block of rows are independent of the next
+//                one's products and are taken meanwhile: 16 blocks of 32 x 32 products and 64 exponentials of a lane in a tile
+// Bound by the vector instructions of a logit (multiply-add, exp2, add) beside its product: 32 heads over 8, 2048 tokens after 30000
+// 1050 TFLOP/s; 64 over 8, 512 after 7680 86 us, 770 (what a workgroup does before its first product weighs).
 // One workgroup owns a slot, so nothing is added atomically; where there are few slots the rows are shared out over workgroups
 // whose sums go through the workspace, and the last one to arrive adds them in order.
 #include "sqa_chunk_mma.h"
@@ -33,7 +36,7 @@ struct ScoresArgs {
 template <typename T, int D>
 __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const ScoresArgs a) {
   using R = TileRows<T, D>;
-  constexpr int TILE = kScoreRows * R::RB, KB = score_blocks<T>(), kScoreSlots = score_slots<T>();
+  constexpr int TILE = kScoreRows * R::RB, KB = score_blocks<T>(), kScoreSlots = score_slots<T>(), NS = Frag<T, D>::NS;
   extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // two tiles of rows
   __shared__ __attribute__((aligned(16))) float s_lse[4][kScoreRows];            // in powers of two; of rows that are none: infinity
   __shared__ __attribute__((aligned(16))) int s_see[4][kScoreRows];              // the last slot that a row sees
@@ -61,7 +64,8 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
   const int end = __builtin_amdgcn_readfirstlane((int)held);
   if (slot0 >= end) return;
   // ---- the lane's slots.  (Asked for before it is known whether the unit holds the chunk: a block number outside the pools reads block 0.)
-  const int slot = (int)slot0 + 32 * KB * wave + col;
+  const int slot = (int)slot0 + 32 * KB * wave + col;                    // ... whose keys it holds, and the first whose sums it holds
+  const int slot_of = (int)slot0 + 32 * KB * wave + 4 * half;
   Frag<T, D> k[KB];
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
@@ -139,49 +143,55 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
   };
   // rows of a tile that are of one head and all see the workgroup's last slot need no look at what each one sees
   const int last_slot = (int)slot0 + kScoreSlots - 1;
-  float sum[KB] = {}, sum2[KB] = {};
-  f32x16_t s[2][KB];                                 // a block's products, and the one before it, whose exponentials are taken meanwhile
-  auto add = [&](f32x16_t (&e)[KB], int tl, int rb, auto look) {
+  float sum[KB][16] = {};                            // of a lane's rows
+  f32x16_t s[2][KB];                                 // a block's products, and the one before it
+  int q_at[NS];                                      // the lane's row and pieces in a block of 32 rows
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 ref = *reinterpret_cast<const float4*>(&s_lse[tl & 3][32 * rb + 8 * j + 4 * half]);
+  for (int x = 0; x < NS; ++x) q_at[x] = col * R::RB + (((2 * x + half) ^ R::k_swizzle(col)) << 4);
+  // logits of slots that a row does not see, of the rows 32 rb .. of tile tl
+  auto hide = [&](f32x16_t (&e)[KB], int tl, int rb) {
+    const int sees = s_see[tl & 3][32 * rb + col] - slot_of;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[kb][i] = sees >= 32 * kb + c_row(i, 0) ? e[kb][i] : -INFINITY;
+  };
+  // 16 / NS of a block's logits of each block of slots, x of NS
+  auto add = [&](const f32x16_t (&e)[KB], int x, float ref) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 16 * x / NS; i < 16 * (x + 1) / NS; ++i) sum[kb][i] += exp2_fast(fmaf(e[kb][i], a.scale, -ref));
+  };
+  // The two blocks of rows of a tile, the exponentials of the block before each between its products (a product of bf16 takes the matrix
+  // core as long as five multiply-adds or two exponentials take), its rows read from LDS some steps ahead.  The steps are kept apart: left
+  // to itself the compiler gathers the products.
+  auto rows_of = [&](const char* Qt, int tl, bool look_before, bool look) {
+    constexpr int AHEAD = 3;
+    uint4 q[2 * NS];
+    auto read = [&](int y) { q[y] = *reinterpret_cast<const uint4*>(Qt + q_at[y % NS] + (y / NS) * 32 * R::RB); };
+#pragma unroll
+    for (int y = 0; y < AHEAD; ++y) read(y);
+    const float ref[2] = {s_lse[(tl - 1) & 3][32 + col], s_lse[tl & 3][col]};
+    if (look_before) hide(s[1], tl - 1, 1);
+#pragma unroll
+    for (int y = 0; y < 2 * NS; ++y) {
+      const int rb = y / NS, x = y % NS;
+      if (y == NS) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(sum[kb][i]));      // (the branch is no reason to add them up later)
+        if (look) hide(s[0], tl, 0);
+      }
+      if (y + AHEAD < 2 * NS) read(y + AHEAD);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        float x = exp2_fast(fmaf(e[kb][4 * j], a.scale, -ref.x)), y = exp2_fast(fmaf(e[kb][4 * j + 1], a.scale, -ref.y));
-        float z = exp2_fast(fmaf(e[kb][4 * j + 2], a.scale, -ref.z)), v = exp2_fast(fmaf(e[kb][4 * j + 3], a.scale, -ref.w));
-        if constexpr (decltype(look)::value) {
-          const int4 sees = *reinterpret_cast<const int4*>(&s_see[tl & 3][32 * rb + 8 * j + 4 * half]);
-          const int at = slot + 32 * kb;
-          x = sees.x >= at ? x : 0.f; y = sees.y >= at ? y : 0.f; z = sees.z >= at ? z : 0.f; v = sees.w >= at ? v : 0.f;
-        }
-        sum[kb] += x; sum2[kb] += y; sum[kb] += z; sum2[kb] += v;
+        if (x == 0) s[rb][kb] = f32x16_t{};
+        mma_piece<T>(k[kb].p[x], q[y], s[rb][kb]);
       }
-    }
-  };
-  auto products = [&](const char* Qt, int rb, f32x16_t (&to)[KB]) {
-    const int row = 32 * rb + col;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) to[kb] = f32x16_t{};
-#pragma unroll
-    for (int x = 0; x < Frag<T, D>::NS; ++x) {
-      const uint4 q = *reinterpret_cast<const uint4*>(Qt + row * R::RB + (((2 * x + half) ^ R::k_swizzle(row)) << 4));
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) mma_piece<T>(q, k[kb].p[x], to[kb]);
-    }
-  };
-  // a block of 32 rows and, between its products, the exponentials of the one before (a product takes the matrix core as long as five
-  // or six vector instructions take)
-  auto both = [&](const char* Qt, int rb, f32x16_t (&to)[KB], f32x16_t (&before)[KB], int tl_before, int rb_before, auto look) {
-    products(Qt, rb, to);
-    add(before, tl_before, rb_before, look);
-    if constexpr (sizeof(T) == 2) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-      for (int i = 0; i < KB * Frag<T, D>::NS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, (decltype(look)::value ? 80 : 48) / Frag<T, D>::NS, 0);
-      }
+      add(s[1 - rb], x, ref[rb]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   bool look_before = false;                          // (s[1] holds the last block of the tile before, whose exponentials are still to come)
@@ -226,31 +236,37 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
     const bool look = now.tt + kScoreRows > tv || (int)seq.pos + t0 + now.tt < last_slot;
     now = soon;
     soon = later;
-    if (look || look_before) {
-      f32x16_t to[KB];
-#pragma unroll 1
-      for (int rb = 0; rb < 2; ++rb) {
-        both(Qt, rb, to, s[1], tl - 1 + rb, 1 - rb, std::true_type{});
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[1][kb] = to[kb];
-      }
-    } else {
-      both(Qt, 0, s[0], s[1], tl - 1, 1, std::false_type{});
-      both(Qt, 1, s[1], s[0], tl, 0, std::false_type{});
-    }
+    rows_of(Qt, tl, look_before, look);
     look_before = look;
   }
-  add(s[1], tile1 - 1, 1, std::true_type{});
+  if (look_before) hide(s[1], tile1 - 1, 1);
 #pragma unroll
-  for (int kb = 0; kb < KB; ++kb) sum[kb] += sum2[kb];
+  for (int x = 0; x < NS; ++x) add(s[1], x, s_lse[(tile1 - 1) & 3][32 + col]);
+  // the 32 rows of a slot's lanes: each exchange halves what a lane holds, the last leaves it one slot
 #pragma unroll
-  for (int kb = 0; kb < KB; ++kb) sum[kb] = other_half_sum(sum[kb]);
+  for (int kb = 0; kb < KB; ++kb) {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = sum[kb][i];
+    auto exchange = [&](auto n_) {
+      constexpr int n = decltype(n_)::value;
+      const bool upper = (lane & (2 * n)) != 0;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float give = upper ? v[i] : v[i + n], mine = upper ? v[i + n] : v[i];
+        v[i] = mine + __shfl_xor(give, 2 * n);
+      }
+    };
+    exchange(std::integral_constant<int, 8>{});
+    exchange(std::integral_constant<int, 4>{});
+    exchange(std::integral_constant<int, 2>{});
+    exchange(std::integral_constant<int, 1>{});
+    const float all = v[0] + __shfl_xor(v[0], 1);
+    if ((lane & 1) == 0) s_sum[32 * (KB * wave + kb) + c_row((lane & 31) >> 1, half)] = all;
+  }
+  __syncthreads();
 
   if (parts > 1) {
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      if (half == 0) s_sum[32 * (KB * wave + kb) + col] = sum[kb];
-    __syncthreads();
     float2* const rec = a.part + item * a.splits * (kScoreSlots / 2);
     if (tid < kScoreSlots / 2) hand_over(rec + (int64_t)split * (kScoreSlots / 2) + tid, make_float2(s_sum[2 * tid], s_sum[2 * tid + 1]));
     if (!last_to_arrive(a.count + item, parts, &s_word)) return;
@@ -263,12 +279,8 @@ __global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const Sc
       s_sum[2 * tid] = v.x; s_sum[2 * tid + 1] = v.y;
     }
     __syncthreads();
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) sum[kb] = s_sum[32 * (KB * wave + kb) + col];
   }
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-    if (half == 0 && slot + 32 * kb < end) a.c.L.score_acc[unit.first + slot + 32 * kb] += sum[kb];
+  if (tid < kScoreSlots && slot0 + tid < end) a.c.L.score_acc[unit.first + slot0 + tid] += s_sum[tid];
   if (tid == 0 && tile == 0) a.c.L.unit_state[(int64_t)u * SQA_ST_WORDS + SQA_ST_EVICT_HINT] = -2;   // what was decided by the old scores
 }
 
