@@ -5,7 +5,7 @@
 // with two buffers:
 //   S^T = K.Q^T  a lane holds 16 of 32 slots of one row and adds up each by itself, over its rows: one normaliser per lane and
 //                block, and no sum across lanes before the end.  The exponentials of one block of rows are independent of the next
-//                one's products and are taken meanwhile: 16 blocks of 32 x 32 products and 64 exponentials of a lane in a tile
+//                one's products and are taken meanwhile
 // Bound by the vector instructions of a logit (multiply-add, exp2, add) beside its product: 32 heads over 8, 2048 tokens after 30000
 // 1050 TFLOP/s; 64 over 8, 512 after 7680 86 us, 770 (what a workgroup does before its first product weighs).
 // One workgroup owns a slot, so nothing is added atomically; where there are few slots the rows are shared out over workgroups
@@ -17,9 +17,11 @@ namespace sqa {
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreRows = 64;                      // of a tile in LDS
-// slots of a wave in blocks of 32: two in bf16 (each row read from LDS feeds both), one in fp32 (bound by the products either way)
-template <typename T> constexpr int score_blocks() { return sizeof(T) == 2 ? 2 : 1; }
-template <typename T> constexpr int score_slots() { return 4 * 32 * score_blocks<T>(); }
+// slots of a wave in blocks of 32: two in bf16 with D = 128 (each row read from LDS feeds both), else one: in fp32 the products bound it
+// either way; with D = 64 in bf16 three workgroups fit a CU then (8 x 2048 tokens of 16 heads 105 -> 83 us, 512 of 64 heads over 8
+// after 7680 65 -> 68; with D = 128 201 against 219 and 89 against 85, 4096 tokens of 32 heads over 8 117 against 95)
+template <typename T, int D> constexpr int score_blocks() { return sizeof(T) == 2 && D == 128 ? 2 : 1; }
+template <typename T, int D> constexpr int score_slots() { return 4 * 32 * score_blocks<T, D>(); }
 constexpr int kScoreSlotsMost = 256;
 constexpr int kScoreItems = 512;                    // workgroups that few slots are shared out to: two per CU
 
@@ -34,9 +36,9 @@ struct ScoresArgs {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kScoreThreads, 2) void chunk_scores_kernel(const ScoresArgs a) {
+__global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) void chunk_scores_kernel(const ScoresArgs a) {
   using R = TileRows<T, D>;
-  constexpr int TILE = kScoreRows * R::RB, KB = score_blocks<T>(), kScoreSlots = score_slots<T>(), NS = Frag<T, D>::NS;
+  constexpr int TILE = kScoreRows * R::RB, KB = score_blocks<T, D>(), kScoreSlots = score_slots<T, D>(), NS = Frag<T, D>::NS;
   extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // two tiles of rows
   __shared__ __attribute__((aligned(16))) float s_lse[4][kScoreRows];            // in powers of two; of rows that are none: infinity
   __shared__ __attribute__((aligned(16))) int s_see[4][kScoreRows];              // the last slot that a row sees
@@ -325,7 +327,7 @@ extern "C" sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtyp
   a.part = reinterpret_cast<float2*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const int64_t slots = uniform ? (int64_t)new_pos + T : layer->capacity;
-  const int per = dt == SQA_F32 ? sqa::score_slots<float>() : sqa::score_slots<sqa::bf16_t>();
+  const int per = dt == SQA_F32 || D == 64 ? sqa::score_slots<float, 64>() : sqa::score_slots<sqa::bf16_t, 128>();
   const int64_t tiles = (slots + per - 1) / per;
   if ((int64_t)B * Hkv > (INT32_MAX - 8) / tiles) return SQA_ERR_SHAPE;
   a.tiles = (int)tiles;
