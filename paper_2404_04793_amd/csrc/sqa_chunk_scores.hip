@@ -7,7 +7,7 @@
 //                block, and no sum across lanes before the end.  The exponentials of one block of rows are independent of the next
 //                one's products and are taken meanwhile
 // Bound by the vector instructions of a logit (multiply-add, exp2, add) beside its product: 32 heads over 8, 2048 tokens after 30000
-// 1050 TFLOP/s; 64 over 8, 512 after 7680 86 us, 770 (what a workgroup does before its first product weighs).
+// 1050 TFLOP/s; 64 over 8, 512 after 7680 80 us, 830 (what a workgroup does before its first product weighs).
 // One workgroup owns a slot, so nothing is added atomically; where there are few slots the rows are shared out over workgroups
 // whose sums go through the workspace, and the last one to arrive adds them in order.
 #include "sqa_chunk_mma.h"
