@@ -150,9 +150,16 @@ __global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) v
   int q_at[NS];                                      // the lane's row and pieces in a block of 32 rows
 #pragma unroll
   for (int x = 0; x < NS; ++x) q_at[x] = col * R::RB + (((2 * x + half) ^ R::k_swizzle(col)) << 4);
-  // logits of slots that a row does not see, of the rows 32 rb .. of tile tl
-  auto hide = [&](f32x16_t (&e)[KB], int tl, int rb) {
+  // Logits of slots that a row does not see, of the rows 32 rb .. of tile tl.  (Their exponential is 0 unless the row's normaliser is NaN
+  // or -inf: that goes into the logits that the row sees.)
+  auto hide = [&](f32x16_t (&e)[KB], int tl, int rb, float& ref) {
     const int sees = s_see[tl & 3][32 * rb + col] - slot_of;
+    if (__any(!(ref > -INFINITY))) {
+      const float odd = ref > -INFINITY ? 0.f : ref;
+      ref = ref > -INFINITY ? ref : 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) e[kb] -= odd;
+    }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -174,8 +181,8 @@ __global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) v
     auto read = [&](int y) { q[y] = *reinterpret_cast<const uint4*>(Qt + q_at[y % NS] + (y / NS) * 32 * R::RB); };
 #pragma unroll
     for (int y = 0; y < AHEAD; ++y) read(y);
-    const float ref[2] = {s_lse[(tl - 1) & 3][32 + col], s_lse[tl & 3][col]};
-    if (look_before) hide(s[1], tl - 1, 1);
+    float ref[2] = {s_lse[(tl - 1) & 3][32 + col], s_lse[tl & 3][col]};
+    if (look_before) hide(s[1], tl - 1, 1, ref[0]);
 #pragma unroll
     for (int y = 0; y < 2 * NS; ++y) {
       const int rb = y / NS, x = y % NS;
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) v
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(sum[kb][i]));      // (the branch is no reason to add them up later)
-        if (look) hide(s[0], tl, 0);
+        if (look) hide(s[0], tl, 0, ref[1]);
       }
       if (y + AHEAD < 2 * NS) read(y + AHEAD);
 #pragma unroll
@@ -241,9 +248,10 @@ __global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) v
     rows_of(Qt, tl, look_before, look);
     look_before = look;
   }
-  if (look_before) hide(s[1], tile1 - 1, 1);
+  float ref = s_lse[(tile1 - 1) & 3][32 + col];
+  if (look_before) hide(s[1], tile1 - 1, 1, ref);
 #pragma unroll
-  for (int x = 0; x < NS; ++x) add(s[1], x, s_lse[(tile1 - 1) & 3][32 + col]);
+  for (int x = 0; x < NS; ++x) add(s[1], x, ref);
   // the 32 rows of a slot's lanes: each exchange halves what a lane holds, the last leaves it one slot
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {

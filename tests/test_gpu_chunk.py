@@ -363,6 +363,25 @@ def test_what_a_row_does_not_see_does_not_matter(sqa, dtype, D):
                 mem[r] = o
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_a_row_without_a_normaliser_spoils_only_what_it_sees(sqa, dtype, D):
+    """A row whose log-sum-exp is NaN or -inf (its query or its keys were): the scores of later slots are what they are without it."""
+    for B, T, first, Hq, Hkv, t in ((1, 70, 30, 4, 2, 20), (2, 200, 0, 2, 2, 63), (1, 5, 300, 8, 1, 0), (1, 130, 500, 3, 3, 129)):
+        dt, _, c, q, _, _ = setup(sqa, dtype, D, "dense", B, T, [first] * B, Hq, Hkv, None, 31)
+        _, lse = sqa.chunk_attention(q, first, c)
+        score0, got = c.score[0].clone(), []
+        for value in (math.inf, math.nan, -math.inf):                   # (infinite: the row gives nothing)
+            lse[0, 0, t] = value
+            c.score[0].copy_(score0)
+            sqa.chunk_scores(q, lse, first, c)
+            got.append(c.score[0][..., :first + T].clone())
+        without, seen = got[0], first + t + 1
+        assert bool(torch.isfinite(without).all())
+        for other in got[1:]:
+            assert not bool(torch.isfinite(other[0, 0, :seen]).any())
+            assert R.same([without[0, 0, seen:], without[:, 1:]], [other[0, 0, seen:], other[:, 1:]]), (B, T, first, t)
+
+
 def test_logits_of_every_size(sqa):
     """Rows whose logits are all very low, very high or far apart; one slot that takes all; a chunk whose logits are -inf but for its own."""
     D, T, first = 64, 40, 90
