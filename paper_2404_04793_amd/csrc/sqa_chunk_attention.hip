@@ -10,8 +10,8 @@
 //   O^T = V^T.P^T  a row's sums lie in the two lanes of its column: rescaling is a multiplication by a lane's own number
 // K and V tiles go from global memory straight to LDS, two buffers, in an order without bank conflicts (TileRows).
 // Few rows are bound by memory (16 x 1-5 tokens of 32 heads over 8, up to 4095 slots, bf16: 44 us, 4.6 TB/s), many by the vector
-// instructions beside the products (8 x 2048 tokens of 32 heads 350 us, 785 TFLOP/s; 512 of 64 heads over 8 after 7680 143 us, 930) and, where
-// those run long enough, by power (2048 of 32 heads over 8 after 30000 980 us, 1060 TFLOP/s at 1.85 GHz).
+// instructions beside the products (8 x 2048 tokens of 32 heads 350 us, 785 TFLOP/s; 512 of 64 heads over 8 after 7680 140 us, 950) and, where
+// those run long enough, by power (2048 of 32 heads over 8 after 30000 930 to 1010 us from card to card, 1120 to 1030 TFLOP/s).
 #include "sqa_chunk_mma.h"
 #include <type_traits>
 
@@ -668,8 +668,10 @@ template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attentio
   if (whole > 0) {
     for (int j = 0; j < whole; ++j) {
       copy_k(j + 1); copy_v(j, j + 1 < n ? row_v : row_k);
+      __builtin_amdgcn_s_setprio(1);                 // the wave that has products to give goes first: 954 -> 929 us (30000 slots), 143 -> 140
       keys(j);
       if (j > 0) values(j - 1);
+      __builtin_amdgcn_s_setprio(0);
       softmax(j, std::false_type{});
       fetched();
       part_done();
