@@ -491,8 +491,8 @@ size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int
  *   out : DEVICE [B][T][Hq][D], dtype dt (what an output projection takes)
  *   lse : DEVICE float [B][Hq][T] or NULL: ln sum_{j <= new_pos + t} exp(q . K_j / sqrt(D)), the row_lse of
  *         sqa_prefill_scores_lse and sqa_chunk_scores
- * The softmax is in fp32; in bf16 the probabilities are rounded to bf16 for the product with V, as in sqa_decode_step on the
- * matrix cores.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
+ * The softmax is in fp32.  In bf16 the product with V takes probabilities that are right to 2^-15 of each; where a workgroup has 128 rows (long
+ * chunks) they are rounded to bf16 for it, as sqa_decode_step does for 4 or 8 query heads per KV head at D = 128.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
  * A unit that does not hold the chunk (too few tokens, a ring that has turned, another token in the chunk's last slot) gets rows of
  * zeros and lse -inf, status SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  That is not a search for evicted tokens:
  * the call belongs between the append and the first eviction after it.  Results are the same from run to run. */
