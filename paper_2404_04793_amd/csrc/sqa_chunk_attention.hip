@@ -423,11 +423,13 @@ __global__ __launch_bounds__(kAtThreads, KT * D * sizeof(T) == 64 * 512 && RW ==
     const float keep = exp2_fast((m - top) * a.scale);
     float off = top * a.scale;
     m = top;
-    // s scale - off in one operation is off by the rounding of `off`: far from 0 the difference is taken first
-    if (__any(fabsf(off) > kFarLogit)) {
+    // s scale - off in one operation is off by the rounding of `off`: far from 0 the difference is taken first.  (Each row for itself, so that
+    // no row's bits depend on slots that only others see.)
+    if (const bool far = fabsf(off) > kFarLogit; __any(far)) {
+      const float from = far ? top : 0.f;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) s[kb] -= top;
-      off = 0.f;
+      for (int kb = 0; kb < KB; ++kb) s[kb] -= from;
+      off = far ? 0.f : off;
     }
     l *= keep;
 #pragma unroll
@@ -632,19 +634,21 @@ template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attentio
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
     top = other_half_max(top);
-    if (__any(top > m + a.near)) {                   // the reference moves when a logit is 2^8 times beyond it: seldom after the first tiles
-      const float to = fmaxf(m, top), keep = exp2_fast((m - to) * a.scale);
+    // the reference of a row moves when one of its logits is 2^8 times beyond it: seldom after the first tiles
+    if (const bool beyond = top > m + a.near; __any(beyond)) {
+      const float to = beyond ? top : m, keep = exp2_fast((m - to) * a.scale);
       m = to;
       l *= keep;
 #pragma unroll
       for (int e = 0; e < NB; ++e) o[e] *= keep;
     }
     float off = m * a.scale;
-    // s scale - off in one operation is off by the rounding of `off`: far from 0 the difference is taken first
-    if (__any(fabsf(off) > kFarLogit)) {
+    // (see the kernel above)
+    if (const bool far = fabsf(off) > kFarLogit; __any(far)) {
+      const float from = far ? m : 0.f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) s[kb] -= m;
-      off = 0.f;
+      for (int kb = 0; kb < 2; ++kb) s[kb] -= from;
+      off = far ? 0.f : off;
     }
     float l0 = 0.f, l1 = 0.f;
 #pragma unroll
