@@ -492,7 +492,7 @@ size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int
  *   lse : DEVICE float [B][Hq][T] or NULL: ln sum_{j <= new_pos + t} exp(q . K_j / sqrt(D)), the row_lse of
  *         sqa_prefill_scores_lse and sqa_chunk_scores
  * The softmax is in fp32.  In bf16 the product with V takes probabilities that are right to 2^-15 of each; where a workgroup has 128 rows (long
- * chunks) they are rounded to bf16 for it, as sqa_decode_step does for 4 or 8 query heads per KV head at D = 128.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
+ * chunks: sqa_chunk_plan) they are rounded to bf16 for it, as sqa_decode_step does for 4 or 8 query heads per KV head at D = 128.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
  * A unit that does not hold the chunk (too few tokens, a ring that has turned, another token in the chunk's last slot) gets rows of
  * zeros and lse -inf, status SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  That is not a search for evicted tokens:
  * the call belongs between the append and the first eviction after it.  Results are the same from run to run. */
@@ -510,6 +510,22 @@ sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, int T, int Hq
 sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D,
                             int32_t new_pos, const sqa_layer_cache* layer,
                             void* workspace, size_t ws_bytes, void* stream, const sqa_batch_opts* opts);
+
+/* How sqa_chunk_attention and sqa_chunk_scores would lay a chunk out on the chip (host arithmetic, no GPU call): for logs, for telling which form's
+ * precision a call has, and so that it can be checked without a GPU that a shape reaches a form.  Of `layer` only capacity is read, of opts
+ * whether prompt_len and new_pos_seq are NULL.  Refuses the shapes that those calls refuse. */
+typedef struct sqa_chunk_plan_info {
+  int32_t rows;             /* attention: query rows (tokens x query heads of a KV head) of a workgroup: 32, 64 or 128     */
+  int32_t row_tiles;        /* workgroups that the rows of a unit take                                             */
+  int32_t slot_splits;      /* k > 1: k workgroups share out the slots of the same rows, and the last one joins them */
+  int32_t units_in_turn;    /* k > 1: the row tiles of k units are taken in turn, the longest first               */
+  int32_t rounded_probs;    /* 1: probabilities are rounded to bf16 for the product with V                          */
+  int32_t score_slots;      /* scores: slots of a workgroup                                                        */
+  int32_t score_slot_tiles; /* workgroups that the slots of a unit take                                            */
+  int32_t score_row_splits; /* k > 1: k workgroups share out the rows of the same slots, and the last one joins them */
+} sqa_chunk_plan_info;
+sqa_status sqa_chunk_plan(const sqa_layer_cache* layer, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                          const sqa_batch_opts* opts, sqa_chunk_plan_info* info);
 
 /* ---- free list for blocked K/V allocation (host only) ----------------------
  * Book-keeping for the block numbers of ONE pool pair (the K and V pools of one layer share numbers, see

@@ -75,6 +75,12 @@ class HeadPrepStruct(C.Structure):
                 ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
+class ChunkPlanInfo(C.Structure):
+    """Mirror of sqa_chunk_plan_info."""
+    _fields_ = [(f, C.c_int32) for f in ("rows", "row_tiles", "slot_splits", "units_in_turn", "rounded_probs", "score_slots",
+                                         "score_slot_tiles", "score_row_splits")]
+
+
 ORDER = {"evict_then_attend": 0, "attend_then_evict": 1}
 
 _vp, _i, _i64, _sz, _f64 = C.c_void_p, C.c_int, C.c_int64, C.c_size_t, C.c_double
@@ -138,6 +144,8 @@ _lib.sqa_chunk_attention.restype = _i
 _lib.sqa_chunk_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
 _lib.sqa_chunk_scores.restype = _i
 _lib.sqa_chunk_scores.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _sz, _vp, _vp]
+_lib.sqa_chunk_plan.restype = _i
+_lib.sqa_chunk_plan.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, C.c_int32, _BOp, C.POINTER(ChunkPlanInfo)]
 _lib.sqa_block_pool_create.argtypes = [C.c_int32]
 _lib.sqa_block_pool_create.restype = _vp
 _lib.sqa_block_pool_destroy.argtypes = [_vp]
@@ -742,6 +750,14 @@ def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> t
     ws = torch.empty(need, dtype=torch.uint8, device=caches.K[0].device)
     _check(_lib.sqa_decode_workspace_init(_ptr(ws), need, _stream()), "sqa_decode_workspace_init")
     return ws
+
+
+def chunk_plan(capacity: int, B: int, T: int, Hq: int, Hkv: int, D: int, dtype: str, new_pos: int = 0, ragged: bool = False) -> dict:
+    """sqa_chunk_plan: how chunk_attention and chunk_scores would lay a chunk out (host arithmetic, no GPU).  dtype: "bf16" or "f32"; ragged: with
+    prompt_len or new_pos_seq."""
+    layer, opts, info = LayerCacheStruct(capacity=capacity), BatchOptsStruct(prompt_len=0x1000 if ragged else None), ChunkPlanInfo()
+    _check(_lib.sqa_chunk_plan(C.byref(layer), {"f32": 0, "bf16": 1}[dtype], B, T, Hq, Hkv, D, new_pos, C.byref(opts), C.byref(info)), "sqa_chunk_plan")
+    return {f: int(getattr(info, f)) for f, _ in ChunkPlanInfo._fields_}
 
 
 def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0, out: Optional[torch.Tensor] = None,

@@ -134,5 +134,7 @@ constexpr size_t kChunkCounterBytes = kChunkCounters * sizeof(int32_t);
 
 size_t chunk_attention_scratch(int T, int Hq, int Hkv, int D);                          // bytes behind the counters
 size_t chunk_scores_scratch();
+struct ScoresPlan { int slots, tiles, splits; };     // slots of a workgroup, of which a unit has `tiles`, and the workgroups of each that share out the rows
+ScoresPlan scores_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos, int32_t capacity, bool uniform);
 
 }  // namespace sqa

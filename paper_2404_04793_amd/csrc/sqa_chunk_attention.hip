@@ -720,13 +720,16 @@ template <int D> __global__ __launch_bounds__(kAtThreads, 2) void chunk_attentio
   w.template finish<1>(a, s_stage, s_m, s_l, &s_word, wave, 0, o, m, l);
 }
 
-struct AttentionPlan { int rw, tiles, splits; };     // rw: 32-row blocks of a workgroup
+struct AttentionPlan { int rw, tiles, splits, group; };          // rw: 32-row blocks of a workgroup
 // (rows of 512 bytes have no form for 32 rows: its tiles would not fit the LDS)
 static int attention_rw(int rows, bool bf16, int D) {
   return rows <= 32 && (bf16 || D == 64) ? 1 : (rows <= 64 ? 2 : 4);
 }
-static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int64_t slots, bool ragged) {
+// uniform: every sequence brings T tokens at new_pos; otherwise nothing is known on the host of what the units hold but their room
+static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos, int32_t capacity, bool uniform) {
   AttentionPlan p;
+  const bool ragged = !uniform;
+  const int64_t slots = uniform ? (int64_t)new_pos + T : capacity;
   const int rows = T * (Hq / Hkv), least = attention_rw(1, dt == SQA_BF16, D);
   int64_t items, s;
   for (p.rw = attention_rw(rows, dt == SQA_BF16, D);; p.rw /= 2) {
@@ -741,6 +744,13 @@ static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv,
   const int few = dt == SQA_BF16 ? 384 : 128;        // (fp32 products take 8 times as long)
   s = s > slots / few ? slots / few : s;
   p.splits = s < 1 ? 1 : (int)s;
+  // Row tiles of a unit see from new_pos to new_pos + T slots.  Where that is not much the same for all, an XCD (an eighth of the units)
+  // takes the longest of several units first, so that the launch ends in short ones.
+  p.group = 1;
+  // (8 x 32 heads x 2048 tokens 383 -> 363 us, one sequence of them 66 -> 59; 16 or 32 units at a time 378, 396.)
+  if (p.splits == 1 && p.tiles >= 8 && uniform && new_pos < T)
+    for (int k = 8; k > 1; k /= 2)
+      if ((int64_t)B * Hkv % (8 * k) == 0) { p.group = k; break; }
   return p;
 }
 // (any T' <= T, any length, either type: items x splits <= kAtItems where there are splits)
@@ -804,19 +814,27 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   a.part = reinterpret_cast<float4*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
-  const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, uniform ? (int64_t)new_pos + T : layer->capacity, !uniform);
+  const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, new_pos, layer->capacity, uniform);
   a.near = 8.f / a.scale;
   a.group_m = 0xffffffffu / (uint32_t)a.c.g + 1;
-  a.tiles = p.tiles; a.splits = p.splits;
-  // Row tiles of a unit see from new_pos to new_pos + T slots.  Where that is not much the same for all, an XCD (an eighth of the units)
-  // takes the longest of several units first, so that the launch ends in short ones.
-  a.group = 1;
-  // (8 x 32 heads x 2048 tokens 383 -> 363 us, one sequence of them 66 -> 59; 16 or 32 units at a time 378, 396.)
-  if (p.splits == 1 && p.tiles >= 8 && uniform && new_pos < T)
-    for (int k = 8; k > 1; k /= 2)
-      if ((int64_t)B * Hkv % (8 * k) == 0) { a.group = k; break; }
+  a.tiles = p.tiles; a.splits = p.splits; a.group = p.group;
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dt == SQA_F32) return D == 64 ? sqa::launch_attention<float, 64>(p.rw, a, st) : sqa::launch_attention<float, 128>(p.rw, a, st);
   return D == 64 ? sqa::launch_attention<sqa::bf16_t, 64>(p.rw, a, st) : sqa::launch_attention<sqa::bf16_t, 128>(p.rw, a, st);
+}
+
+extern "C" sqa_status sqa_chunk_plan(const sqa_layer_cache* layer, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                                     const sqa_batch_opts* opts, sqa_chunk_plan_info* info) {
+  if (!layer || !info) return SQA_ERR_NULL;
+  if (dt != SQA_F32 && dt != SQA_BF16) return SQA_ERR_DTYPE;
+  if (sqa::bad_chunk_shape(B, T, Hq, Hkv, D, new_pos, opts)) return SQA_ERR_SHAPE;
+  const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
+  if (layer->capacity < 1 || (uniform && (int64_t)new_pos + T > layer->capacity)) return SQA_ERR_CAPACITY;
+  const sqa::AttentionPlan p = sqa::attention_plan(dt, B, T, Hq, Hkv, D, new_pos, layer->capacity, uniform);
+  info->rows = 32 * p.rw; info->row_tiles = p.tiles; info->slot_splits = p.splits; info->units_in_turn = p.group;
+  info->rounded_probs = dt == SQA_BF16 && p.rw == 4;
+  const sqa::ScoresPlan q = sqa::scores_plan(dt, B, T, Hq, Hkv, D, new_pos, layer->capacity, uniform);
+  info->score_slots = q.slots; info->score_slot_tiles = q.tiles; info->score_row_splits = q.splits;
+  return SQA_OK;
 }

@@ -294,11 +294,15 @@ __global__ __launch_bounds__(kScoreThreads, sizeof(T) == 2 && D == 64 ? 3 : 2) v
   if (tid == 0 && tile == 0) a.c.L.unit_state[(int64_t)u * SQA_ST_WORDS + SQA_ST_EVICT_HINT] = -2;   // what was decided by the old scores
 }
 
-static int scores_splits(int B, int T, int Hq, int Hkv, int tiles) {
-  const int64_t items = (int64_t)B * Hkv * tiles, row_tiles = ((int64_t)T * (Hq / Hkv) + kScoreRows - 1) / kScoreRows;
+ScoresPlan scores_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos, int32_t capacity, bool uniform) {
+  ScoresPlan p;
+  p.slots = dt == SQA_F32 || D == 64 ? score_slots<float, 64>() : score_slots<bf16_t, 128>();
+  p.tiles = (int)(((uniform ? (int64_t)new_pos + T : capacity) + p.slots - 1) / p.slots);
+  const int64_t items = (int64_t)B * Hkv * p.tiles, row_tiles = ((int64_t)T * (Hq / Hkv) + kScoreRows - 1) / kScoreRows;
   int64_t s = kScoreItems / items;
   s = s > row_tiles ? row_tiles : s;
-  return s < 1 ? 1 : (int)s;
+  p.splits = s < 1 ? 1 : (int)s;
+  return p;
 }
 // (any length: items x splits <= kScoreItems where there are splits)
 size_t chunk_scores_scratch() { return (size_t)kScoreItems * kScoreSlotsMost * sizeof(float); }
@@ -334,12 +338,10 @@ extern "C" sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtyp
   a.count = static_cast<int32_t*>(workspace);
   a.part = reinterpret_cast<float2*>(static_cast<char*>(workspace) + sqa::kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
-  const int64_t slots = uniform ? (int64_t)new_pos + T : layer->capacity;
-  const int per = dt == SQA_F32 || D == 64 ? sqa::score_slots<float, 64>() : sqa::score_slots<sqa::bf16_t, 128>();
-  const int64_t tiles = (slots + per - 1) / per;
-  if ((int64_t)B * Hkv > (INT32_MAX - 8) / tiles) return SQA_ERR_SHAPE;
-  a.tiles = (int)tiles;
-  a.splits = sqa::scores_splits(B, T, Hq, Hkv, a.tiles);
+  const sqa::ScoresPlan p = sqa::scores_plan(dt, B, T, Hq, Hkv, D, new_pos, layer->capacity, uniform);
+  if ((int64_t)B * Hkv > (INT32_MAX - 8) / p.tiles) return SQA_ERR_SHAPE;
+  a.tiles = p.tiles;
+  a.splits = p.splits;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dt == SQA_F32) return D == 64 ? sqa::launch_scores<float, 64>(a, st) : sqa::launch_scores<float, 128>(a, st);
   return D == 64 ? sqa::launch_scores<sqa::bf16_t, 64>(a, st) : sqa::launch_scores<sqa::bf16_t, 128>(a, st);
