@@ -62,6 +62,7 @@ class BatchOptsStruct(C.Structure):
     """Mirror of sqa_batch_opts."""
     _fields_ = [("prompt_len", C.c_void_p), ("budget_seq", C.c_void_p), ("new_pos_seq", C.c_void_p),
                 ("status", C.c_void_p), ("order", C.c_int32)]
+    tensors, devices, entries = (), frozenset(), None      # (of batch_opts: what is kept alive, where it is, the entries of its shortest array)
 
 
 class TokenRowsStruct(C.Structure):
@@ -189,6 +190,8 @@ def batch_opts(prompt_len: Optional[torch.Tensor] = None, budget_seq: Optional[t
             raise TypeError("per-sequence arrays are contiguous int32 tensors")
     o = BatchOptsStruct(_ptr(prompt_len), _ptr(budget_seq), _ptr(new_pos_seq), _ptr(status), ORDER[order])
     o.tensors = (prompt_len, budget_seq, new_pos_seq, status)
+    o.devices = frozenset(t.get_device() for t in o.tensors if t is not None)
+    o.entries = min((t.numel() for t in o.tensors[:3] if t is not None), default=None)
     return o
 
 
@@ -628,6 +631,18 @@ def _check_device(devices) -> None:
         raise ValueError("a tensor is not on the current device")
 
 
+def _opts_at(opts: Optional[BatchOptsStruct], B: int, dev: int) -> Optional[int]:
+    """Address of the options, after a look at whether their arrays are on the call's device and hold its sequences."""
+    if opts is None:
+        return None
+    if opts.entries is not None and opts.entries < B:
+        raise TypeError("per-sequence arrays hold an entry for each sequence")
+    for at in opts.devices:
+        if at != dev:
+            raise ValueError("a tensor is not on the current device")
+    return C.addressof(opts)
+
+
 def _prep(prep: Optional[HeadPrepStruct], dtype: torch.dtype, D: int, dev: int):
     if prep is None:
         return None
@@ -680,10 +695,10 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: 
         raise TypeError("an output without its input")
     rows = array("q", rows)
     at = rows.buffer_info()[0]
-    how = _prep(prep, dtype, D, dev)
+    how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
     _check_device(devices)
     code = _lib.sqa_qk_norm_rope(None if q is None else at, None if k is None else at if q is None else at + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos,
-                                 q_to, k_to, _stream(), None if opts is None else C.addressof(opts))
+                                 q_to, k_to, _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_qk_norm_rope")
     return q_out, k_out
@@ -731,11 +746,11 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
         q_to = q_out.data_ptr()
         devices += (q.get_device(), q_out.get_device())
         rows = array("q", (k.data_ptr(), k_seq, k_row, v.data_ptr(), v_seq, v_row, q.data_ptr(), seq, row))
-    how = _prep(prep, dtype, D, dev)
+    how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
     _check_device(devices)
     first = rows.buffer_info()[0]                            # sqa_token_rows one after the other: keys, values, queries
     code = _lib.sqa_chunk_append(None if q is None else first + 2 * _ROWS_BYTES, first, first + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq,
-                                 Hkv, D, how, new_pos, q_to, at, _stream(), None if opts is None else C.addressof(opts))
+                                 Hkv, D, how, new_pos, q_to, at, _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_chunk_append")
     return q_out
@@ -779,9 +794,10 @@ def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer:
         _check_out(lse, (B, Hq, T), torch.float32)
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
+    extra = _opts_at(opts, B, dev)
     _check_device([dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
     code = _lib.sqa_chunk_attention(q.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, out.data_ptr(), lse.data_ptr(),
-                                    workspace.data_ptr(), workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
+                                    workspace.data_ptr(), workspace.nbytes, _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_chunk_attention")
     return out, lse
@@ -800,8 +816,9 @@ def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "Laye
         raise TypeError("lse is a contiguous fp32 tensor [B, Hq, T]")
     if workspace is None:
         workspace = chunk_workspace(caches, Hq, T, layer)
+    extra = _opts_at(opts, B, dev)
     _check_device([dev, lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
     code = _lib.sqa_chunk_scores(q.data_ptr(), lse.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, workspace.data_ptr(),
-                                 workspace.nbytes, _stream(), None if opts is None else C.addressof(opts))
+                                 workspace.nbytes, _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_chunk_scores")
