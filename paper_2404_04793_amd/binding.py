@@ -631,6 +631,12 @@ def _check_device(devices) -> None:
         raise ValueError("a tensor is not on the current device")
 
 
+def _check_position(new_pos: int, where: str) -> None:
+    """(ctypes would cut it off to 32 bits: another position.)"""
+    if not -1 << 31 <= new_pos < 1 << 31:
+        raise SqaError(2, where)
+
+
 def _opts_at(opts: Optional[BatchOptsStruct], B: int, dev: int) -> Optional[int]:
     """Address of the options, after a look at whether their arrays are on the call's device and hold its sequences."""
     if opts is None:
@@ -697,6 +703,7 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: 
     at = rows.buffer_info()[0]
     how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
     _check_device(devices)
+    _check_position(new_pos, "sqa_qk_norm_rope")
     code = _lib.sqa_qk_norm_rope(None if q is None else at, None if k is None else at if q is None else at + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos,
                                  q_to, k_to, _stream(), extra)
     if code != SQA_OK:
@@ -748,6 +755,7 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
         rows = array("q", (k.data_ptr(), k_seq, k_row, v.data_ptr(), v_seq, v_row, q.data_ptr(), seq, row))
     how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
     _check_device(devices)
+    _check_position(new_pos, "sqa_chunk_append")
     first = rows.buffer_info()[0]                            # sqa_token_rows one after the other: keys, values, queries
     code = _lib.sqa_chunk_append(None if q is None else first + 2 * _ROWS_BYTES, first, first + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq,
                                  Hkv, D, how, new_pos, q_to, at, _stream(), extra)
@@ -770,6 +778,7 @@ def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> t
 def chunk_plan(capacity: int, B: int, T: int, Hq: int, Hkv: int, D: int, dtype: str, new_pos: int = 0, ragged: bool = False) -> dict:
     """sqa_chunk_plan: how chunk_attention and chunk_scores would lay a chunk out (host arithmetic, no GPU).  dtype: "bf16" or "f32"; ragged: with
     prompt_len or new_pos_seq."""
+    _check_position(new_pos, "sqa_chunk_plan")
     layer, opts, info = LayerCacheStruct(capacity=capacity), BatchOptsStruct(prompt_len=0x1000 if ragged else None), ChunkPlanInfo()
     _check(_lib.sqa_chunk_plan(C.byref(layer), {"f32": 0, "bf16": 1}[dtype], B, T, Hq, Hkv, D, new_pos, C.byref(opts), C.byref(info)), "sqa_chunk_plan")
     return {f: int(getattr(info, f)) for f, _ in ChunkPlanInfo._fields_}
@@ -796,6 +805,7 @@ def chunk_attention(q: torch.Tensor, new_pos: int, caches: "LayerCaches", layer:
         workspace = chunk_workspace(caches, Hq, T, layer)
     extra = _opts_at(opts, B, dev)
     _check_device([dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
+    _check_position(new_pos, "sqa_chunk_attention")
     code = _lib.sqa_chunk_attention(q.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, out.data_ptr(), lse.data_ptr(),
                                     workspace.data_ptr(), workspace.nbytes, _stream(), extra)
     if code != SQA_OK:
@@ -818,6 +828,7 @@ def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "Laye
         workspace = chunk_workspace(caches, Hq, T, layer)
     extra = _opts_at(opts, B, dev)
     _check_device([dev, lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
+    _check_position(new_pos, "sqa_chunk_scores")
     code = _lib.sqa_chunk_scores(q.data_ptr(), lse.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, workspace.data_ptr(),
                                  workspace.nbytes, _stream(), extra)
     if code != SQA_OK:

@@ -35,3 +35,25 @@ def test_arrays_of_another_device():
     assert sqa._opts_at(opts, 2, 0) == sqa.C.addressof(opts)
     opts = sqa.batch_opts(prompt_len=ints(2), budget_seq=torch.zeros(3, 2, dtype=torch.int32), status=ints(1))
     assert sqa._opts_at(opts, 2, -1) == sqa.C.addressof(opts)
+
+
+def test_positions_beyond_32_bits(monkeypatch):
+    """Refused, not cut off to another position.  (Before the library is called: its symbols are replaced.)"""
+    class Library:
+        def __getattr__(self, name):
+            if name == "sqa_status_str":
+                return lib.sqa_status_str
+            return lambda *args: 0 if name != "sqa_chunk_workspace_bytes" else 1 << 20
+    lib = sqa._lib
+    monkeypatch.setattr(sqa, "_lib", Library())
+    monkeypatch.setattr(sqa, "_check_device", lambda devices: None)
+    monkeypatch.setattr(sqa, "_stream", lambda: None)
+    for new_pos in (1 << 31, 1 << 32, (1 << 32) + 5, -(1 << 31) - 1):
+        for call in (lambda c, x, q, ws: sqa.qk_norm_rope(x, x, new_pos), lambda c, x, q, ws: sqa.chunk_append(x, x, new_pos, c),
+                     lambda c, x, q, ws: sqa.chunk_attention(q, new_pos, c, workspace=ws),
+                     lambda c, x, q, ws: sqa.chunk_scores(q, torch.zeros(2, 4, 3), new_pos, c, workspace=ws),
+                     lambda c, x, q, ws: sqa.chunk_plan(8, 2, 3, 4, 4, 64, "f32", new_pos)):
+            with pytest.raises(sqa.SqaError) as e:
+                call(sqa.LayerCaches([8], [8], 2, 4, 64, torch.float32, "cpu", True), torch.zeros(2, 3, 4, 64), torch.zeros(2, 4, 3, 64),
+                     torch.zeros(1 << 20, dtype=torch.uint8))
+            assert e.value.code == 2
