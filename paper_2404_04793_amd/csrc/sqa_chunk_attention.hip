@@ -121,7 +121,7 @@ template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
   ChunkUnit unit;
   bool held_slots;
 
-  uint32_t group_m;                                 // (division by g: rows are less than 2^31 / 64)
+  uint32_t group_m;                                 // (division by g: for rows below 2^31 the quotient is one too large at most, and place() puts it right)
 
   // Where the work is; false: there is none.  Nothing is known yet of what the unit holds, but its first `end` slots can be read where
   // held_slots is true.
@@ -152,8 +152,8 @@ template <typename T, int D, int NT, int M, int KT> struct AttentionWork {
     last_row = min(row0 + M, rows) - 1;
     int t, head;
     place(last_row, t, head);
-    end = __builtin_amdgcn_readfirstlane((int)min(pos + t + 1, (int64_t)INT32_MAX));
     held_slots = pos + n <= unit.slots;
+    end = __builtin_amdgcn_readfirstlane(held_slots ? (int)pos + t + 1 : 1);          // (positions may be any up to 2^31: 1 for a unit that is refused)
     const int nt = (end + KT - 1) / KT, per = (nt + a.splits - 1) / a.splits;
     parts = (nt + per - 1) / per;
     tile0 = split * per;

@@ -26,3 +26,22 @@ def test_large_keys_in_slots_that_a_row_does_not_see(sqa, dtype, D, B, T, first,
             assert R.same([out[:, :t].contiguous(), lse[..., :t].contiguous()], [got[:, :t].contiguous(), got_lse[..., :t].contiguous()]), (t, size)
             assert not torch.equal(lse[..., t], got_lse[..., t])
         keys[:, :, first + t] = old
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv", [(3, 5, 8, 2), (40, 64, 16, 16), (8, 150, 64, 32), (4, 300, 8, 2)])
+def test_positions_up_to_the_last(sqa, B, T, Hq, Hkv):  # noqa: F811
+    """A sequence whose position lies far beyond its unit's slots, up to 2^31 - 1: rows of zeros, whatever the form; the others as ever."""
+    dt, _, c, q, _, status = setup(sqa, "bf16", 64, "dense", B, T, [100] * B, Hq, Hkv, [T] * B, 43)
+    good, good_lse = sqa.chunk_attention(q, 0, c, opts=sqa.batch_opts(new_pos_seq=torch.full((B,), 100, dtype=torch.int32, device=q.device)))
+    for far in (2 ** 31 - 1, 2 ** 31 - T, 2 ** 31 - 63, 2 ** 30, 101 + T):
+        pos = torch.full((B,), 100, dtype=torch.int32, device=q.device)
+        pos[B - 1] = far
+        status.zero_()
+        opts = sqa.batch_opts(new_pos_seq=pos, status=status)
+        out, lse = sqa.chunk_attention(q, 0, c, opts=opts)
+        assert int(status) == 8 and bool((out[B - 1] == 0).all()) and bool((lse[B - 1] == -float("inf")).all()), far
+        assert R.same([good[:B - 1], good_lse[:B - 1]], [out[:B - 1], lse[:B - 1]])
+        score0 = c.score[0].clone()
+        status.zero_()
+        sqa.chunk_scores(q, good_lse, 0, c, opts=opts)
+        assert int(status) == 8 and R.same([score0[B - 1]], [c.score[0][B - 1]])
