@@ -18,7 +18,7 @@
  *   blocks (sqa_layer_cache.block_table) the host free list sqa_block_pool_*.
  *   Between a model's projections and these calls: sqa_qk_norm_rope, and for prompts
  *   that come in chunks (or drafts of a few tokens) sqa_chunk_append,
- *   sqa_chunk_attention and sqa_chunk_scores.
+ *   sqa_chunk_attention and sqa_chunk_scores (sqa_chunk_plan: how they would be launched).
  *
  * Conventions
  *   - "DEVICE" pointers are HIP device memory owned by the caller and borrowed
@@ -491,8 +491,10 @@ size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int
  *   out : DEVICE [B][T][Hq][D], dtype dt (what an output projection takes)
  *   lse : DEVICE float [B][Hq][T] or NULL: ln sum_{j <= new_pos + t} exp(q . K_j / sqrt(D)), the row_lse of
  *         sqa_prefill_scores_lse and sqa_chunk_scores
- * The softmax is in fp32.  In bf16 the product with V takes probabilities that are right to 2^-15 of each; where a workgroup has 128 rows (long
- * chunks: sqa_chunk_plan) they are rounded to bf16 for it, as sqa_decode_step does for 4 or 8 query heads per KV head at D = 128.  Slots that a token may not see do not change its row, whatever they hold (NaN and infinities too).
+ * The softmax is in fp32.  In bf16 the product with V takes probabilities that are right to 2^-15 of each; where a workgroup
+ * has 128 rows (long chunks: sqa_chunk_plan) they are rounded to bf16 for it, as sqa_decode_step does for 4 or 8 query heads
+ * per KV head at D = 128.  Slots that a token may not see do not change its row by a bit, whatever they hold (NaN and
+ * infinities too).
  * A unit that does not hold the chunk (too few tokens, a ring that has turned, another token in the chunk's last slot) gets rows of
  * zeros and lse -inf, status SQA_ERR_STATE (a block number outside the pools: SQA_ERR_SHAPE).  That is not a search for evicted tokens:
  * the call belongs between the append and the first eviction after it.  Results are the same from run to run. */
@@ -506,14 +508,17 @@ sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, int T, int Hq
  * After the last chunk of a prompt score_acc is what sqa_prefill_scores gives for the whole prompt (to rounding), and K, V and
  * score_acc of a dense layer are the inputs of sqa_prefill_compress (P = capacity, opts->prompt_len).
  *   q, lse : as for sqa_chunk_attention; layer->score_acc required.  A wrong lse gives wrong scores, not an error
+ * What a token has given stays: an append at a smaller position takes its slot back, not its share of earlier slots'
+ * scores.  So a draft is scored once it is known which of its tokens stay (opts->prompt_len).
  * A unit that does not hold the chunk is left untouched, status as above.  Results are the same from run to run. */
 sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D,
                             int32_t new_pos, const sqa_layer_cache* layer,
                             void* workspace, size_t ws_bytes, void* stream, const sqa_batch_opts* opts);
 
-/* How sqa_chunk_attention and sqa_chunk_scores would lay a chunk out on the chip (host arithmetic, no GPU call): for logs, for telling which form's
- * precision a call has, and so that it can be checked without a GPU that a shape reaches a form.  Of `layer` only capacity is read, of opts
- * whether prompt_len and new_pos_seq are NULL.  Refuses the shapes that those calls refuse. */
+/* How sqa_chunk_attention and sqa_chunk_scores would lay a chunk out on the chip (host arithmetic, no GPU call): for logs,
+ * for telling which form's precision a call has, and so that it can be checked without a GPU which form a shape reaches.
+ * Of `layer` only capacity is read, of opts whether prompt_len and new_pos_seq are NULL.  Refuses the shapes that those
+ * calls refuse. */
 typedef struct sqa_chunk_plan_info {
   int32_t rows;             /* attention: query rows (tokens x query heads of a KV head) of a workgroup: 32, 64 or 128     */
   int32_t row_tiles;        /* workgroups that the rows of a unit take                                             */

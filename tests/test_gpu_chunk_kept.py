@@ -77,3 +77,32 @@ def test_append_writes_nothing_but_its_slots(sqa, dtype, D, layout):  # noqa: F8
                     assert c.state[0][b, h].tolist() == [first[b] + n[b], 0, -2, 0]
                     c.state[0][b, h] = before[4][b, h]
         assert R.same(before, R.snapshot(c)), (B, T)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+def test_a_draft_is_scored_by_what_stays_of_it(sqa, dtype, D):  # noqa: F811
+    """Five drafted tokens, two of which are accepted: scored with prompt_len = 2 and written over by the next append, the layer is the one to which only
+    those two were ever appended."""
+    dt, gen, B, Hq, Hkv, T, first = R.DT[dtype], generator(23), 2, 8, 2, 5, [600, 37]
+    layers = [R.fill(R.make_cache(sqa, "blocked", B, Hkv, D, dt, [620, 620]), first, generator(24)) for _ in range(2)]
+    x = torch.randn(B, T, Hq + 2 * Hkv, D, generator=gen, device=DEV).to(dt)
+    y = torch.randn(B, T, Hq + 2 * Hkv, D, generator=gen, device=DEV).to(dt)
+    y[:, :2] = x[:, :2]
+    two, three = ints([2, 2]), ints([3, 3])
+    for drafted, c in zip((True, False), layers):
+        opts = sqa.batch_opts(prompt_len=ints([T, T]) if drafted else two, new_pos_seq=ints(first))
+        q = sqa.chunk_append(x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:], 0, c, q=x[:, :, :Hq], opts=opts)
+        _, lse = sqa.chunk_attention(q, 0, c, opts=opts)
+        sqa.chunk_scores(q, lse, 0, c, opts=sqa.batch_opts(prompt_len=two, new_pos_seq=ints(first)))
+        z = y[:, 2:].contiguous()
+        later = sqa.batch_opts(prompt_len=three, new_pos_seq=ints([f + 2 for f in first]))
+        q = sqa.chunk_append(z[:, :, Hq:Hq + Hkv], z[:, :, Hq + Hkv:], 0, c, q=z[:, :, :Hq], opts=later)
+        _, lse = sqa.chunk_attention(q, 0, c, opts=later)
+        sqa.chunk_scores(q, lse, 0, c, opts=later)
+    for b in range(B):
+        n = first[b] + 5
+        for h in range(Hkv):
+            a, c = (l.unit(0, b, h) for l in layers)
+            assert all(torch.equal(p, q) for p, q in zip(R.rows_of(layers[0], b, h, n), R.rows_of(layers[1], b, h, n)))
+            assert torch.equal(a[2][:n], c[2][:n]) and torch.equal(a[3][:n], c[3][:n])
+    assert torch.equal(layers[0].state[0], layers[1].state[0])
