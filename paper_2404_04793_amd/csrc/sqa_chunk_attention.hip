@@ -2,15 +2,18 @@
 //   out_t = sum_j exp(s_tj - m_t) V_j / l_t,  s_tj = q_t.K_j / sqrt(D),  l_t = sum_j exp(s_tj - m_t),  j <= position of t
 // One pass over the slots with a running maximum m and sum l per row.  The g query heads of a KV head and the chunk's tokens
 // are one list of rows, row r = token r / g, head r % g: K and V are read once for all of them.  A workgroup of 4
-// waves takes 32 RW of these rows, RW = 4, 2 or 1 by their number; with RW < 4 the 4 / RW waves of the same rows share
+// waves takes 32 RW of these rows, RW = 4, 2 or 1: by their number, and fewer while that leaves workgroups short and each would have less
+// than 512 slots (attention_plan).  With RW < 4 the 4 / RW waves of the same rows share
 // out the slots of a tile and join at the end.  Few rows against many slots are shared out over workgroups too; their
 // (m, l, sums) go through the workspace and the last one to arrive joins them, in order.
 //   S^T = K.Q^T  a lane holds 16 of 32 slots of one row: maximum and sum need one exchange between the two lane halves, and
 //                the probabilities are the next product's operand as they are
 //   O^T = V^T.P^T  a row's sums lie in the two lanes of its column: rescaling is a multiplication by a lane's own number
 // K and V tiles go from global memory straight to LDS, two buffers, in an order without bank conflicts (TileRows).
-// Few rows are bound by memory (16 x 1-5 tokens of 32 heads over 8, up to 4095 slots, bf16: 44 us, 4.6 TB/s), many by the vector
-// instructions beside the products (8 x 2048 tokens of 32 heads 350 us, 785 TFLOP/s; 512 of 64 heads over 8 after 7680 140 us, 950) and, where
+// Few rows are bound by how tiles of K and V arrive: two stages of 64 KB, one workgroup per CU, a barrier a tile.  16 x 1-5 tokens of 32 heads over 8, up
+// to 4095 slots, bf16, 202 MB: 58 us with caches from HBM, as a model of many layers finds them (3.5 TB/s; a read reaches 6.3 to 7.1), 47 us where the
+// last-level cache holds them (4.3 TB/s).  Many rows are bound by the vector
+// instructions beside the products (8 x 2048 tokens of 32 heads 350 us, 785 TFLOP/s; 512 of 64 heads over 8 after 7680 141 us, 945) and, where
 // those run long enough, by power (2048 of 32 heads over 8 after 30000 930 to 1010 us from card to card, 1120 to 1030 TFLOP/s).
 #include "sqa_chunk_mma.h"
 #include <type_traits>
@@ -738,14 +741,19 @@ static AttentionPlan attention_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv,
     // as many as run at a time (tiles of few rows fill half a CU's LDS or all of it); twice that where sequences differ in length: five
     // tokens of 16 sequences over 4095 slots 48 us (57 with twice as many), over 2048 to 4095 slots 51 (46 with twice as many)
     s = (p.rw == 4 || ragged ? kAtItems : kAtItems / 2) / items;
-    // a join costs what some hundred slots do: short units are shared out by rows first
+    // a join costs what some hundred slots do: short units are shared out by rows first.  With 256, 512 and 1024 slots in place of kAtJoin: 128 tokens
+    // of 32 heads over 8 after 1000 20.3, 15.1, 15.1 us, 64 after 4000 25.1, 21.3, 21.3, 256 after 1500 26.4, 26.7, 27.4
     if (p.rw == least || s <= 1 || slots / s >= kAtJoin) break;
   }
-  const int few = dt == SQA_BF16 ? 384 : 128;        // (fp32 products take 8 times as long)
+  // The least slots of a workgroup, so that a join is worth its time (fp32 products take 8 times as long).  With twice as many 1 token of 32 heads
+  // over 8 after 2000 takes 17.2 in place of 12.9 us, 5 of 8 heads of 128 after 1000 in fp32 34 in place of 21; with half as many 10.9 and 18.3.  From
+  // 4000 slots on, or 16 sequences of 4000, it makes no difference (46 us).
+  const int few = dt == SQA_BF16 ? 384 : 128;
   s = s > slots / few ? slots / few : s;
   p.splits = s < 1 ? 1 : (int)s;
   // Row tiles of a unit see from new_pos to new_pos + T slots.  Where that is not much the same for all, an XCD (an eighth of the units)
-  // takes the longest of several units first, so that the launch ends in short ones.
+  // takes the longest of several units first, so that the launch ends in short ones.  (An eighth of the units has to be a whole number of such groups;
+  // other numbers of units are taken one after the other.)
   p.group = 1;
   // (8 x 32 heads x 2048 tokens 383 -> 363 us, one sequence of them 66 -> 59; 16 or 32 units at a time 378, 396.)
   if (p.splits == 1 && p.tiles >= 8 && uniform && new_pos < T)

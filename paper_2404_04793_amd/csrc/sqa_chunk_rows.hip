@@ -2,7 +2,8 @@
 // keys and values, written into the slots of a layer cache (sqa_chunk_append).
 //   y = x / sqrt(mean(x^2) + eps) * w ;  (a, b) <- (a cos - b sin, b cos + a sin) over the leading rot_dim elements
 // Bound by memory: every element is read once and written once, the angles come from a table of rot_dim floats per position.
-// (4 x 2048 tokens of 32 + 8 heads of 128, bf16: 34.4 us, 4.9 TB/s, a large copy's 5.1; 8 x 512 into blocks after 2048 23.8 us, 4.3 TB/s.)
+// (4 x 2048 tokens of 32 + 8 heads of 128, bf16: 34.4 us, 4.9 TB/s, a large copy's 5.1; 8 x 512 into blocks after 2048 23.8 us, 4.3 TB/s: with what a
+// projection has just written still in the last-level cache.  From HBM 45 and 30 us.)
 // A row of one head is 16 bytes per lane (8 to 32 lanes); a wave takes as many heads as fit side by side and U tokens of them, all
 // requested before the first is used: what it writes is U consecutive rows of each head.  The sum of squares and the rotation's
 // partners (rot_dim / 2 elements away: a whole number of lanes) stay inside a row's lanes.  fp32 throughout, rounded once.
@@ -234,7 +235,9 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   const int64_t groups = (int64_t)a.c.B * (a.q_groups + a.kv_groups);
   constexpr int waves = kRowsThreads / SQA_WAVE;
   // two tokens per wave where that leaves every SIMD a wave, otherwise one.  (4 x 2048 tokens of 32 + 8 heads: 35.7 us with two, 39.1
-  // with four, 42.3 with one; rows stored non-temporally 34.7, but what reads them next is slower by more.)
+  // with four, 42.3 with one; rows stored non-temporally 34.7, but what reads them next is slower by more.  From a quarter as many waves on or
+  // only from four times as many on, in us against this rule: 64 tokens 4.8 and 4.1 against 4.9, 4 x 64 appended 6.7 and 6.1 against 6.7, 2 x 512
+  // 8.1 either way.)
   const bool two = groups * ((a.c.T + 1) / 2) >= 1024;
   a.t_blocks = two ? (a.c.T + 1) / 2 : a.c.T;
   const int64_t blocks = (groups * a.t_blocks + waves - 1) / waves;

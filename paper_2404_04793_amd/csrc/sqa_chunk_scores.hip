@@ -18,8 +18,9 @@ namespace sqa {
 constexpr int kScoreThreads = 256;
 constexpr int kScoreRows = 64;                      // of a tile in LDS
 // slots of a wave in blocks of 32: two in bf16 with D = 128 (each row read from LDS feeds both), else one: in fp32 the products bound it
-// either way; with D = 64 in bf16 three workgroups fit a CU then (8 x 2048 tokens of 16 heads 105 -> 83 us, 512 of 64 heads over 8
-// after 7680 65 -> 68; with D = 128 201 against 219 and 89 against 85, 4096 tokens of 32 heads over 8 117 against 95)
+// either way; with D = 64 in bf16 a wave then needs 114 registers, four workgroups fit a CU, and 8 x 2048 tokens of 16 heads take 83 in place of 105 us
+// (512 of 64 heads over 8 after 7680 68 in place of 65; with D = 128 201 against 219 and 89 against 85, 4096 tokens of 32 heads over 8 117
+// against 95).  Whether the compiler is told of two, three or four workgroups changes neither registers nor time (83 to 84 us)
 template <typename T, int D> constexpr int score_blocks() { return sizeof(T) == 2 && D == 128 ? 2 : 1; }
 template <typename T, int D> constexpr int score_slots() { return 4 * 32 * score_blocks<T, D>(); }
 constexpr int kScoreSlotsMost = 256;
