@@ -12,8 +12,8 @@
 // K and V tiles go from global memory straight to LDS, two buffers, in an order without bank conflicts (TileRows).
 // Few rows are bound by how tiles of K and V arrive: two stages of 64 KB, one workgroup per CU, a barrier a tile.  16 x 1-5 tokens of 32 heads over 8, up
 // to 4095 slots, bf16, 202 MB: 58 us with caches from HBM, as a model of many layers finds them (3.5 TB/s; a read reaches 6.3 to 7.1), 47 us where the
-// last-level cache holds them (4.3 TB/s).  Many rows are bound by the vector
-// instructions beside the products (8 x 2048 tokens of 32 heads 350 us, 785 TFLOP/s; 512 of 64 heads over 8 after 7680 141 us, 945) and, where
+// last-level cache holds them (4.3 TB/s).  Many rows are bound by how far products and vector instructions of a SIMD's two waves overlap (8 x 2048
+// tokens of 32 heads 350 us, 785 TFLOP/s, busy 0.39 and 0.46; 512 of 64 heads over 8 after 7680 141 us, 945, 0.46 and 0.43) and, where
 // those run long enough, by power (2048 of 32 heads over 8 after 30000 930 to 1010 us from card to card, 1120 to 1030 TFLOP/s).
 #include "sqa_chunk_mma.h"
 #include <type_traits>

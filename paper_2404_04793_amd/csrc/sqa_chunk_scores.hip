@@ -6,8 +6,8 @@
 //   S^T = K.Q^T  a lane holds 16 of 32 slots of one row and adds up each by itself, over its rows: one normaliser per lane and
 //                block, and no sum across lanes before the end.  The exponentials of one block of rows are independent of the next
 //                one's products and are taken meanwhile
-// Bound by the vector instructions of a logit (multiply-add, exp2, add) beside its product: 32 heads over 8, 2048 tokens after 30000
-// 1050 TFLOP/s; 64 over 8, 512 after 7680 80 us, 830 (what a workgroup does before its first product weighs).
+// Bound by how far a logit's vector instructions (multiply-add, exp2, add) and its product overlap: 32 heads over 8, 2048 tokens after 30000
+// 1050 TFLOP/s; 64 over 8, 512 after 7680 80 us, 830, busy 0.47 and 0.36 (what a workgroup does before its first product weighs).
 // One workgroup owns a slot, so nothing is added atomically; where there are few slots the rows are shared out over workgroups
 // whose sums go through the workspace, and the last one to arrive adds them in order.
 #include "sqa_chunk_mma.h"
