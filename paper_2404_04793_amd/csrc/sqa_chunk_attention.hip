@@ -41,13 +41,13 @@ struct AttentionArgs {
 
 // Two probabilities as two bf16 each, high + low = p to 2^-15 of it: few rows leave the matrix cores idle, so that V is multiplied by both and the
 // caller's bf16 values meet probabilities as good as in fp32 (rms error of 16 x 1-5 tokens of 32 heads over 8 against 64 bits 1.66e-3, all of it
-// the output's rounding; with p rounded to one bf16 2.10e-3; 45.8 -> 47.1 us).  The high part is cut off and the low part is
-// p (1 + 2^-23) - high, so neither is 0 unless p is: 0 x inf would spoil a sum that is infinite.
+// the output's rounding; with p rounded to one bf16 2.10e-3; 45.8 -> 47.1 us).  The high part is cut off, the low part is what is left, but not below
+// the smallest normal number or p itself: neither is 0 unless p is, since 0 x inf would spoil a sum that is infinite.
 struct Halves { uint32_t high, low; };
 __device__ __forceinline__ Halves halves(float x, float y) {
   const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-  constexpr float c = 1.f + FLT_EPSILON;
-  return {__builtin_amdgcn_perm(b, a, 0x07060302u), pair(fmaf(x, c, -__uint_as_float(a & 0xffff0000u)), fmaf(y, c, -__uint_as_float(b & 0xffff0000u)))};
+  auto low = [](float p, uint32_t w) { return __builtin_amdgcn_fmed3f(p - __uint_as_float(w & 0xffff0000u), p, FLT_MIN); };
+  return {__builtin_amdgcn_perm(b, a, 0x07060302u), pair(low(x, a), low(y, b))};
 }
 
 // the halves of a pair of bf16 that are not finite, as a mask

@@ -2,7 +2,7 @@
 p = high + low, so that what is left is the output's own rounding and not one of the probabilities.
 
 Bound: that of chunk_reference.attention with 2^-15 in place of a rounding of the probabilities.  high is p cut off to 8 bits, so low < 2^-7 p, rounded to
-bf16: 2^-7 2^-8 p; the 2^-23 p that low is too large by counts as 2 u more."""
+bf16: 2^-7 2^-8 p; the 2^-126 that low is at least is far below 2 u of a row's sum."""
 import math
 
 import pytest
@@ -61,3 +61,20 @@ def test_infinite_values_that_a_row_sees_stay_infinite(sqa):  # noqa: F811
                 hit[1::7] = True
                 assert bool((got[..., hit] == bad).all()), (T, slot, bad)
                 assert R.same([out[..., ~hit].contiguous(), lse], [got[..., ~hit].contiguous(), lse2])
+
+
+def test_infinite_values_at_the_smallest_probabilities(sqa):  # noqa: F811
+    """exp(-d) for d up to 87 is not 0 in fp32, and times an infinite value it is that infinity.  64 slots of as many probabilities, each with an
+    infinite value in a column of its own."""
+    D, T, first = 64, 3, 500
+    for d in (0.0, 0.5, 10.0, 70.0, 78.0, 82.0, 85.0, 86.0):
+        _, _, c, q, _, _ = setup(sqa, "bf16", D, "dense", 1, T, [first], 4, 2, None, 9)
+        q.zero_()
+        q[..., :2] = 8.0                                   # s = K[0] + K[1] in every row: 8 / sqrt(64)
+        c.K[0][:, :, :first + T, :2] = 0.0
+        for j in range(D):
+            c.K[0][:, :, 3 * j, 0] = -d
+            c.K[0][:, :, 3 * j, 1] = -j / 64.0
+            c.V[0][:, :, 3 * j, j] = math.inf
+        out, _ = sqa.chunk_attention(q, first, c)
+        assert bool((out == math.inf).all()), (d, (out != math.inf).nonzero()[:5].tolist())
