@@ -464,6 +464,25 @@ sqa_status sqa_qk_norm_rope(const sqa_token_rows* q, const sqa_token_rows* k, sq
                             int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
                             void* q_out, void* k_out, void* stream, const sqa_batch_opts* opts);
 
+/* Positions on several axes (time, height and width of an image or a video, say): each token has one on every axis, and each pair of
+ * elements goes by one axis.  Pair i still takes column i of the table, whatever frequencies its columns hold.  The first
+ * pairs[0] pairs go by axis 0, the next pairs[1] by axis 1, and so on; or (turns = 1) the axes take turns, pair by pair, each
+ * as long as it has pairs left.  With equal positions on all axes both are the plain rotation. */
+enum { SQA_MAX_ROPE_AXES = 4 };
+typedef struct sqa_rope_axes {    /* HOST */
+  const int32_t* pos;             /* DEVICE [n_axes][B][T]; those of padding are not read.  An entry outside 0 .. n_pos - 1
+                                     is taken as the nearest of them, status SQA_ERR_SHAPE          */
+  int32_t n_axes;                 /* 1 .. SQA_MAX_ROPE_AXES                                         */
+  int32_t pairs[SQA_MAX_ROPE_AXES]; /* not negative; the first n_axes add up to rot_dim / 2         */
+  int32_t turns;                  /* 0 or 1, see above                                              */
+} sqa_rope_axes;
+
+/* The same with positions on several axes; prep->rope is required then.  new_pos and opts->new_pos_seq no longer say how a token is
+ * rotated (a negative one still leaves its sequence out).  axes NULL: sqa_qk_norm_rope. */
+sqa_status sqa_qk_norm_rope_ex(const sqa_token_rows* q, const sqa_token_rows* k, sqa_dtype dt,
+                               int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
+                               void* q_out, void* k_out, void* stream, const sqa_batch_opts* opts, const sqa_rope_axes* axes);
+
 /* Appends a chunk to one layer's cache (Eq. 2-3 for T tokens; nothing is evicted): the token at position p goes to slot p
  * of each of its sequence's units, its key normalised and rotated on the way, its value as it is, its score 0.
  * Sets unit_state to {new_pos + tokens, 0, -2, 0}: what lay behind is dropped, so a draft that was rejected
@@ -479,6 +498,12 @@ sqa_status sqa_qk_norm_rope(const sqa_token_rows* q, const sqa_token_rows* k, sq
 sqa_status sqa_chunk_append(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt,
                             int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
                             void* q_out, const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts);
+
+/* The same, rotated by positions on several axes: new_pos and opts->new_pos_seq say which slots the tokens go to. */
+sqa_status sqa_chunk_append_ex(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt,
+                               int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos,
+                               void* q_out, const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts,
+                               const sqa_rope_axes* axes);
 
 /* Scratch of the two calls below for chunks of up to T tokens: work on few rows is shared out over the slots and joined.
  * DEVICE, 256-byte aligned, zero-filled once before its first use (sqa_decode_workspace_init) and not shared with other calls
@@ -531,6 +556,103 @@ typedef struct sqa_chunk_plan_info {
 } sqa_chunk_plan_info;
 sqa_status sqa_chunk_plan(const sqa_layer_cache* layer, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
                           const sqa_batch_opts* opts, sqa_chunk_plan_info* info);
+
+/* ---- a layer's cache in 4 bits ----------------------------------------------
+ * The same tokens in a quarter of the memory (136 bytes a token and KV head at D = 128, against 512 in bf16), for serving without
+ * scores: the sliding and StreamingLLM policies of Sec. 2.2 with the layer's own budget, or every token.
+ *
+ * Numbers.  32 neighbouring elements of a row (a group) share a power of two 2^e, the smallest with max |x| <= 7 * 2^e, -125 <= e <=
+ * 125; each is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it (ties to the even code), what is larger as 6.  A code is
+ * 8 * (sign) + its place in that list; two share a byte, the element with the even number in the low half.  The group's byte is e +
+ * 127.  A group with a number that is not finite is held as byte 255 and stands for 32 NaN.  (This is OCP's MXFP4 with a power one
+ * larger where max |x| > 7 * 2^e, so that the largest is off by no more than the grid's widest half step; it is what the matrix cores
+ * take.)
+ *
+ * Slots.  The token of position p of a sequence lies in slot p of its units while p < capacity; from then on the first n_sink slots
+ * stay and the others are a ring: slot n_sink + (p - n_sink) % (capacity - n_sink).  So the positions say all that there is to know
+ * of a unit: nothing is stored beside the rows, and a cache is empty when the next append is at position 0.  Every call trusts
+ * the positions it is given: slots that were never written are read as they are.
+ *
+ * opts, as for the chunk calls above: prompt_len, new_pos_seq, status, and budget_seq [B] (n_sink < budget <= capacity): the slots
+ * that the sequence uses in place of capacity.  A sequence whose entries are out of range is left out, status SQA_ERR_SHAPE
+ * (prompt_len) or SQA_ERR_BUDGET. */
+typedef struct sqa_q4_cache {
+  void* K;                    /* DEVICE, rows of D/2 bytes, 16-byte aligned: [B][Hkv][capacity], or with block_table a pool
+                                 [n_blocks][SQA_BLOCK_SLOTS]                                        */
+  void* V;                    /* the same                                                          */
+  uint8_t* K_scale;           /* DEVICE, rows of D/32 bytes, laid out like K, 4-byte aligned       */
+  uint8_t* V_scale;           /* the same                                                          */
+  const int32_t* block_table; /* NULL or DEVICE int32 [B*Hkv][blocks_per_unit]: unit u's slots 16i .. 16i+15 are block
+                                 block_table[u][i] of the pools (as in sqa_layer_cache; sqa_block_assign fills such tables) */
+  int32_t capacity;           /* slots of a unit = the layer's budget, at most 2^30                 */
+  int32_t n_sink;             /* 0 .. capacity - 1                                                 */
+  int32_t blocks_per_unit;    /* row length of block_table, >= ceil(capacity / SQA_BLOCK_SLOTS), at most SQA_MAX_BLOCKS_PER_UNIT */
+  int32_t n_blocks;           /* blocks in each pool                                               */
+} sqa_q4_cache;
+
+/* A chunk into the cache: sqa_chunk_append for 4 bits.  Keys are normalised and rotated in fp32 and rounded once, to 4 bits.
+ *   slot_map : DEVICE int32 [B][Hkv][T] or NULL: the row (of the pools, or of all units' rows) that each token goes to, -1 = nowhere,
+ *              as sqa_slot_map makes it once for the layers that share a table; positions then only say how tokens are rotated
+ *   axes     : HOST or NULL: positions on several axes (sqa_rope_axes)
+ * A sequence that brings more than capacity - n_sink tokens past its capacity would overwrite its own: its keys and values are left
+ * out, status SQA_ERR_CAPACITY.  Tokens whose block lies outside the pools (or whose row outside the cache) are left out, status
+ * SQA_ERR_SHAPE. */
+sqa_status sqa_q4_append(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt,
+                         int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out,
+                         const sqa_q4_cache* layer, void* stream, const sqa_batch_opts* opts, const sqa_rope_axes* axes,
+                         const int32_t* slot_map);
+
+/* Slots first_slot .. first_slot + T - 1 of every unit as the numbers they stand for (exact in either type).  With opts, new_pos_seq is
+ * the sequence's first slot and prompt_len how many are wanted.
+ *   k_out, v_out : DEVICE [B][Hkv][T][D], dtype dt; either may be NULL.  Rows of slots that the unit does not have are left as they
+ *                  were, status SQA_ERR_CAPACITY (a block outside the pools: SQA_ERR_SHAPE) */
+sqa_status sqa_q4_read(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, int Hkv, int D, int32_t first_slot,
+                       void* k_out, void* v_out, void* stream, const sqa_batch_opts* opts);
+
+/* Scratch of sqa_q4_attention for chunks of up to T tokens.  DEVICE, 256-byte aligned, zero-filled once before its first use
+ * (sqa_decode_workspace_init); calls that share one must not overlap in time.  0 for arguments that the call refuses. */
+size_t sqa_q4_workspace_bytes(const sqa_q4_cache* layer, int B, int T, int Hq, int Hkv, int D);
+
+/* Causal attention of a chunk that has been appended (T = 1: a decode step) over the tokens that the cache still holds:
+ *   out[b][t][h] = sum_j softmax_j(q . K_j / sqrt(D)) V_j  over the slots j whose token's position is at most new_pos + t
+ *   q   : DEVICE [B][Hq][T][D], dtype dt
+ *   out : DEVICE [B][T][Hq][D], dtype dt;  lse : DEVICE float [B][Hq][T] or NULL, as for sqa_chunk_attention
+ * With the positions, lengths and budgets of the append.  A token whose own slot was taken again by the chunk's later ones cannot be (see
+ * sqa_q4_append): such a sequence gets rows of zeros and lse -inf, status SQA_ERR_CAPACITY; so does a unit one of whose blocks lies
+ * outside the pools, status SQA_ERR_SHAPE (tokens that see nothing of that block may have their rows all the same).  Queries, probabilities and sums keep fp32's precision (bf16: queries exactly, probabilities
+ * to 2^-16; where a workgroup has 128 rows they are rounded to bf16 for the product with V).  A slot that a token may not see does not
+ * change its row by a bit.  Results are the same from run to run. */
+sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                            const sqa_q4_cache* layer, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream,
+                            const sqa_batch_opts* opts);
+
+/* ---- block tables and slot maps on the GPU -----------------------------------
+ * For loops whose lengths live on the GPU (or that are captured into a graph): tables of either kind of cache are brought up to
+ * date from the sequences' lengths, blocks taken from and given back to a free list in device memory.
+ *   block_table : DEVICE [B*Hkv][blocks_per_unit], blocks_per_unit >= ceil(capacity / SQA_BLOCK_SLOTS)
+ *   tokens      : DEVICE [B]: how many tokens each sequence is to have room for (those beyond capacity need none); 0: it has left,
+ *                 < 0: it stays as it is
+ *   held        : DEVICE [B]: blocks that each of the sequence's units has, in the first entries of its row; brought up to date
+ *   free_ids    : DEVICE [n_blocks], free_count DEVICE [1]: the free blocks are the first *free_count entries
+ *   status      : DEVICE [1] or NULL
+ * In this order: sequences that hold more than they need give the rest back -- to the end of the list, by sequence, head and
+ * entry; the entries become -1 --, then the others take what they lack from the end of the list, in the same order.  A sequence that
+ * the list is too short for gets nothing, and none behind it does: held stays, status SQA_ERR_CAPACITY.  held outside
+ * 0 .. blocks_per_unit: that sequence is left alone, status SQA_ERR_STATE; a list with more blocks than it has room for: nothing is
+ * done, status SQA_ERR_STATE.  One workgroup; B <= SQA_MAX_ASSIGN. */
+enum { SQA_MAX_ASSIGN = 8192 };
+sqa_status sqa_block_assign(int32_t* block_table, int B, int Hkv, int32_t blocks_per_unit, int32_t capacity, const int32_t* tokens,
+                            int32_t* held, int32_t* free_ids, int32_t* free_count, int32_t n_blocks, int32_t* status, void* stream);
+
+/* The row of the pools that each of T new tokens of each unit goes to, -1 for padding, for sequences that take no part and
+ * where the table has no block (an entry < 0):
+ *   slot of position p: p, and from capacity on n_sink + (p - n_sink) % (capacity - n_sink);  row = block_table[u][slot / 16] * 16 + slot % 16
+ *   block_table : NULL: rows of units one after the other, u * capacity + slot
+ *   map         : DEVICE int32 [B][Hkv][T]
+ * opts: prompt_len, new_pos_seq, budget_seq, status as above.  A sequence that would overwrite its own tokens (sqa_q4_append) gets -1,
+ * status SQA_ERR_CAPACITY; rows from 2^31 on are given as -1, status SQA_ERR_SHAPE. */
+sqa_status sqa_slot_map(const int32_t* block_table, int B, int T, int Hkv, int32_t blocks_per_unit, int32_t capacity, int32_t n_sink,
+                        int32_t new_pos, int32_t* map, void* stream, const sqa_batch_opts* opts);
 
 /* ---- free list for blocked K/V allocation (host only) ----------------------
  * Book-keeping for the block numbers of ONE pool pair (the K and V pools of one layer share numbers, see

@@ -76,6 +76,18 @@ class HeadPrepStruct(C.Structure):
                 ("n_pos", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
+class RopeAxesStruct(C.Structure):
+    """Mirror of sqa_rope_axes."""
+    _fields_ = [("pos", C.c_void_p), ("n_axes", C.c_int32), ("pairs", C.c_int32 * 4), ("turns", C.c_int32)]
+    tensor, device, shape = None, None, None               # (of rope_axes: what is kept alive, where it is, [n_axes, B, T])
+
+
+class Q4CacheStruct(C.Structure):
+    """Mirror of sqa_q4_cache."""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p), ("block_table", C.c_void_p),
+                ("capacity", C.c_int32), ("n_sink", C.c_int32), ("blocks_per_unit", C.c_int32), ("n_blocks", C.c_int32)]
+
+
 class ChunkPlanInfo(C.Structure):
     """Mirror of sqa_chunk_plan_info."""
     _fields_ = [(f, C.c_int32) for f in ("rows", "row_tiles", "slot_splits", "units_in_turn", "rounded_probs", "score_slots",
@@ -137,8 +149,24 @@ _lib.sqa_decode_plan_waves.restype = C.c_int32
 _lib.sqa_decode_plan_waves.argtypes = [_LCp, _i, _i, _i, _i, _i, _i, _i]
 _lib.sqa_qk_norm_rope.restype = _i
 _lib.sqa_qk_norm_rope.argtypes = [_vp, _vp, _i, _i, _i, _i, _i, _i, _vp, C.c_int32, _vp, _vp, _vp, _vp]
+_lib.sqa_qk_norm_rope_ex.restype = _i
+_lib.sqa_qk_norm_rope_ex.argtypes = _lib.sqa_qk_norm_rope.argtypes + [_vp]
 _lib.sqa_chunk_append.restype = _i
 _lib.sqa_chunk_append.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, C.c_int32, _vp, _vp, _vp, _vp]
+_lib.sqa_chunk_append_ex.restype = _i
+_lib.sqa_chunk_append_ex.argtypes = _lib.sqa_chunk_append.argtypes + [_vp]
+_lib.sqa_q4_append.restype = _i
+_lib.sqa_q4_append.argtypes = _lib.sqa_chunk_append.argtypes + [_vp, _vp]
+_lib.sqa_q4_read.restype = _i
+_lib.sqa_q4_read.argtypes = [_vp, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp]
+_lib.sqa_q4_workspace_bytes.restype = _sz
+_lib.sqa_q4_workspace_bytes.argtypes = [_vp, _i, _i, _i, _i, _i]
+_lib.sqa_q4_attention.restype = _i
+_lib.sqa_q4_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+_lib.sqa_block_assign.restype = _i
+_lib.sqa_block_assign.argtypes = [_vp, _i, _i, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp]
+_lib.sqa_slot_map.restype = _i
+_lib.sqa_slot_map.argtypes = [_vp, _i, _i, _i, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, _vp]
 _lib.sqa_chunk_workspace_bytes.restype = _sz
 _lib.sqa_chunk_workspace_bytes.argtypes = [_vp, _i, _i, _i, _i, _i]
 _lib.sqa_chunk_attention.restype = _i
@@ -612,6 +640,20 @@ def head_prep(q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.
     return p
 
 
+def rope_axes(pos: torch.Tensor, pairs: Sequence[int], turns: bool = False) -> RopeAxesStruct:
+    """sqa_rope_axes: pos int32 [n_axes, B, T] (device; kept alive with the result), pairs: how many pairs of elements go by each axis,
+    one axis after the other or (turns) the axes in turn."""
+    if pos.dim() != 3 or pos.dtype != torch.int32 or not pos.is_contiguous():
+        raise TypeError("positions are a contiguous int32 tensor [n_axes, B, T]")
+    if len(pairs) != pos.shape[0] or not 1 <= len(pairs) <= 4:
+        raise TypeError("one number of pairs for each of 1 to 4 axes")
+    if any(not 0 <= int(n) < 1 << 31 for n in pairs):
+        raise SqaError(2, "sqa_rope_axes")
+    a = RopeAxesStruct(pos.data_ptr(), len(pairs), (C.c_int32 * 4)(*[int(n) for n in pairs]), int(turns))
+    a.tensor, a.device, a.shape = pos, pos.get_device(), tuple(pos.shape)
+    return a
+
+
 # (The calls below are kept short, their checks among them: in a model that makes them once per layer, the host's part of a small
 # chunk's call is longer than its kernel.)
 
@@ -659,11 +701,21 @@ def _prep(prep: Optional[HeadPrepStruct], dtype: torch.dtype, D: int, dev: int):
     return C.addressof(prep)
 
 
+def _axes_at(axes: Optional[RopeAxesStruct], B: int, T: int, dev: int) -> Optional[int]:
+    if axes is None:
+        return None
+    if axes.shape is not None and axes.shape[1:] != (B, T):
+        raise TypeError("positions [n_axes, B, T] of the call's tokens")
+    if axes.device is not None and axes.device != dev:
+        raise ValueError("a tensor is not on the current device")
+    return C.addressof(axes)
+
+
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: int, prep: Optional[HeadPrepStruct] = None,
                  q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
-                 opts: Optional[BatchOptsStruct] = None):
+                 opts: Optional[BatchOptsStruct] = None, axes: Optional[RopeAxesStruct] = None):
     """q [B, T, Hq, D], k [B, T, Hkv, D] (either may be None) at positions new_pos .. -> q [B, Hq, T, D], k [B, Hkv, T, D],
-    normalised and rotated."""
+    normalised and rotated (by positions on several axes: rope_axes)."""
     some = q if q is not None else k
     if some is None:
         raise TypeError("queries or keys")
@@ -702,10 +754,11 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], new_pos: 
     rows = array("q", rows)
     at = rows.buffer_info()[0]
     how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
+    turn = None if axes is None else _axes_at(axes, B, T, dev)
     _check_device(devices)
     _check_position(new_pos, "sqa_qk_norm_rope")
-    code = _lib.sqa_qk_norm_rope(None if q is None else at, None if k is None else at if q is None else at + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos,
-                                 q_to, k_to, _stream(), extra)
+    code = _lib.sqa_qk_norm_rope_ex(None if q is None else at, None if k is None else at if q is None else at + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how,
+                                    new_pos, q_to, k_to, _stream(), extra, turn)
     if code != SQA_OK:
         raise SqaError(code, "sqa_qk_norm_rope")
     return q_out, k_out
@@ -720,21 +773,18 @@ def _layer_at(caches: "LayerCaches", layer: int, dtype: torch.dtype, B: int, Hkv
     return C.addressof(caches.table) + layer * _LC_BYTES
 
 
-def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0,
-                 prep: Optional[HeadPrepStruct] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
-                 opts: Optional[BatchOptsStruct] = None) -> Optional[torch.Tensor]:
-    """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
-    way; with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
+def _append(where: str, call, k: torch.Tensor, v: torch.Tensor, new_pos: int, at: int, pool: torch.Tensor, prep, q, q_out, opts, axes,
+            more: tuple) -> Optional[torch.Tensor]:
+    """chunk_append and q4_append: to the layer at address `at`, whose keys are `pool`; `more`: the call's last arguments."""
     B, T, Hkv, D = k.shape
     dtype, dev, Hq, q_to = k.dtype, k.get_device(), Hkv, None
-    at = _layer_at(caches, layer, dtype, B, Hkv, D)
     if v.shape != k.shape or v.dtype != dtype:
         raise TypeError("keys and values of one shape and dtype")
     k_seq, k_row, k_head, k_one = k.stride()
     v_seq, v_row, v_head, v_one = v.stride()
     if k_one != 1 or v_one != 1 or (k_head != D or v_head != D) and Hkv != 1:
         raise TypeError(_ARRAY)
-    devices = [dev, v.get_device(), caches.K[layer].get_device()]
+    devices = [dev, v.get_device(), pool.get_device()]
     if q is None:
         if q_out is not None:
             raise TypeError("an output without its input")
@@ -754,14 +804,25 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
         devices += (q.get_device(), q_out.get_device())
         rows = array("q", (k.data_ptr(), k_seq, k_row, v.data_ptr(), v_seq, v_row, q.data_ptr(), seq, row))
     how, extra = _prep(prep, dtype, D, dev), _opts_at(opts, B, dev)
+    turn = None if axes is None else _axes_at(axes, B, T, dev)
     _check_device(devices)
-    _check_position(new_pos, "sqa_chunk_append")
+    _check_position(new_pos, where)
     first = rows.buffer_info()[0]                            # sqa_token_rows one after the other: keys, values, queries
-    code = _lib.sqa_chunk_append(None if q is None else first + 2 * _ROWS_BYTES, first, first + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq,
-                                 Hkv, D, how, new_pos, q_to, at, _stream(), extra)
+    code = call(None if q is None else first + 2 * _ROWS_BYTES, first, first + _ROWS_BYTES, _DT.get(dtype, -1), B, T, Hq, Hkv, D, how, new_pos,
+                q_to, at, _stream(), extra, turn, *more)
     if code != SQA_OK:
-        raise SqaError(code, "sqa_chunk_append")
+        raise SqaError(code, where)
     return q_out
+
+
+def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerCaches", layer: int = 0,
+                 prep: Optional[HeadPrepStruct] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 opts: Optional[BatchOptsStruct] = None, axes: Optional[RopeAxesStruct] = None) -> Optional[torch.Tensor]:
+    """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
+    way (by positions on several axes: rope_axes); with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
+    B, T, Hkv, D = k.shape
+    at = _layer_at(caches, layer, k.dtype, B, Hkv, D)
+    return _append("sqa_chunk_append", _lib.sqa_chunk_append_ex, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes, ())
 
 
 def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> torch.Tensor:
@@ -833,3 +894,176 @@ def chunk_scores(q: torch.Tensor, lse: torch.Tensor, new_pos: int, caches: "Laye
                                  workspace.nbytes, _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_chunk_scores")
+
+
+# ---- a layer's cache in 4 bits, block tables on the GPU ----
+
+class Q4Caches:
+    """Device memory of the caches in 4 bits of a range of layers, plus the sqa_q4_cache records."""
+
+    def __init__(self, capacities: Sequence[int], B: int, Hkv: int, D: int, device, n_sink: int = 0, blocked: bool = False,
+                 block_seed: Optional[int] = 0, spare_blocks: int = 3, n_blocks: Optional[int] = None):
+        """capacities[l]: slots of a unit of layer l, its budget (every token: the longest length).  blocked: K and V are pools of
+        16-row blocks, dealt out to the units in a seeded random order (block_seed; None = in order) with a few to spare; with
+        n_blocks the pools have that many and the tables are empty (-1): block_assign fills them."""
+        self.L, self.B, self.Hkv, self.D, self.n_sink, self.blocked = len(capacities), B, Hkv, D, n_sink, blocked
+        self.capacities = list(capacities)
+        self.K, self.V, self.K_scale, self.V_scale = [], [], [], []
+        self.block_table: List[Optional[torch.Tensor]] = []
+        self.table = (Q4CacheStruct * self.L)()
+        for i, cap in enumerate(capacities):
+            per = blocks = 0
+            tbl = None
+            if blocked:
+                per = (cap + SQA_BLOCK_SLOTS - 1) // SQA_BLOCK_SLOTS
+                if n_blocks is not None:
+                    blocks, tbl = n_blocks, torch.full((B * Hkv, per), -1, dtype=torch.int32, device=device)
+                else:
+                    blocks = B * Hkv * per + spare_blocks
+                    order = torch.arange(blocks) if block_seed is None else \
+                        torch.randperm(blocks, generator=torch.Generator().manual_seed(block_seed + 7919 * i))
+                    tbl = order[:B * Hkv * per].to(torch.int32).view(B * Hkv, per).contiguous().to(device)
+                rows = (blocks, SQA_BLOCK_SLOTS)
+            else:
+                rows = (B, Hkv, cap)
+            self.block_table.append(tbl)
+            for to, width in ((self.K, D // 2), (self.V, D // 2), (self.K_scale, D // 32), (self.V_scale, D // 32)):
+                to.append(torch.zeros(*rows, width, dtype=torch.uint8, device=device))
+            t = self.table[i]
+            t.K, t.V, t.K_scale, t.V_scale = (x[i].data_ptr() for x in (self.K, self.V, self.K_scale, self.V_scale))
+            t.block_table = _ptr(tbl)
+            t.capacity, t.n_sink, t.blocks_per_unit, t.n_blocks = int(cap), int(n_sink), int(per), int(blocks)
+
+
+_Q4_BYTES = C.sizeof(Q4CacheStruct)
+
+
+def _q4_at(caches: Q4Caches, layer: int, B: int, Hkv: int, D: int) -> int:
+    """Address of a layer's record, after a look at whether the call's tensors fit the cache."""
+    if not 0 <= layer < caches.L:
+        raise IndexError("layer outside the table")
+    if B != caches.B or D != caches.D or Hkv != caches.Hkv:
+        raise TypeError("the cache has another batch, heads or head size")
+    return C.addressof(caches.table) + layer * _Q4_BYTES
+
+
+def q4_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: Q4Caches, layer: int = 0, prep: Optional[HeadPrepStruct] = None,
+              q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None,
+              axes: Optional[RopeAxesStruct] = None, slot_map: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """chunk_append into a cache in 4 bits.  slot_map int32 [B, Hkv, T] (sqa_slot_map): the row that each token goes to."""
+    B, T, Hkv, D = k.shape
+    at, rows = _q4_at(caches, layer, B, Hkv, D), None
+    if slot_map is not None:
+        _check_out(slot_map, (B, Hkv, T), torch.int32)
+        _check_device([slot_map.get_device()])
+        rows = slot_map.data_ptr()
+    return _append("sqa_q4_append", _lib.sqa_q4_append, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes, (rows,))
+
+
+def q4_read(caches: Q4Caches, first_slot: int, n: int, dtype: torch.dtype, layer: int = 0, k_out: Optional[torch.Tensor] = None,
+            v_out: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Slots first_slot .. first_slot + n - 1 of every unit as the numbers they stand for: K, V [B, Hkv, n, D] (without outputs given, rows
+    that are not read are 0)."""
+    shape, device = (caches.B, caches.Hkv, n, caches.D), caches.K[layer].device
+    if k_out is None:
+        k_out = torch.zeros(shape, dtype=dtype, device=device)
+    if v_out is None:
+        v_out = torch.zeros(shape, dtype=dtype, device=device)
+    _check_out(k_out, shape, dtype)
+    _check_out(v_out, shape, dtype)
+    at, dev = _q4_at(caches, layer, caches.B, caches.Hkv, caches.D), caches.K[layer].get_device()
+    extra = _opts_at(opts, caches.B, dev)
+    _check_device([dev, k_out.get_device(), v_out.get_device()])
+    _check_position(first_slot, "sqa_q4_read")
+    code = _lib.sqa_q4_read(at, _DT.get(dtype, -1), caches.B, n, caches.Hkv, caches.D, first_slot, k_out.data_ptr(), v_out.data_ptr(), _stream(), extra)
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_q4_read")
+    return k_out, v_out
+
+
+def q4_workspace(caches: Q4Caches, Hq: int, T: int, layer: int = 0) -> torch.Tensor:
+    """Scratch of q4_attention for chunks of up to T tokens, zero-filled."""
+    need = _lib.sqa_q4_workspace_bytes(_q4_at(caches, layer, caches.B, caches.Hkv, caches.D), caches.B, T, Hq, caches.Hkv, caches.D)
+    if need == 0:
+        raise SqaError(2, "sqa_q4_workspace_bytes")
+    ws = torch.empty(need, dtype=torch.uint8, device=caches.K[0].device)
+    _check(_lib.sqa_decode_workspace_init(_ptr(ws), need, _stream()), "sqa_decode_workspace_init")
+    return ws
+
+
+def q4_attention(q: torch.Tensor, new_pos: int, caches: Q4Caches, layer: int = 0, out: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 opts: Optional[BatchOptsStruct] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """q [B, Hq, T, D] of a chunk that q4_append has taken -> (out [B, T, Hq, D], lse [B, Hq, T] fp32)."""
+    B, Hq, T, D = q.shape
+    dtype, dev, Hkv = q.dtype, q.get_device(), caches.Hkv
+    if not q.is_contiguous():
+        raise TypeError("a chunk's queries are a contiguous tensor [B, Hq, T, D]")
+    at = _q4_at(caches, layer, B, Hkv, D)
+    if out is None:
+        out = torch.empty((B, T, Hq, D), dtype=dtype, device=q.device)
+    else:
+        _check_out(out, (B, T, Hq, D), dtype)
+    if lse is None:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device)
+    else:
+        _check_out(lse, (B, Hq, T), torch.float32)
+    if workspace is None:
+        workspace = q4_workspace(caches, Hq, T, layer)
+    extra = _opts_at(opts, B, dev)
+    _check_device([dev, out.get_device(), lse.get_device(), workspace.get_device(), caches.K[layer].get_device()])
+    _check_position(new_pos, "sqa_q4_attention")
+    code = _lib.sqa_q4_attention(q.data_ptr(), _DT.get(dtype, -1), B, T, Hq, Hkv, D, new_pos, at, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+                                 workspace.nbytes, _stream(), extra)
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_q4_attention")
+    return out, lse
+
+
+def _int32(*tensors: torch.Tensor) -> None:
+    for t in tensors:
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise TypeError("tables, lengths and lists are contiguous int32 tensors")
+
+
+def block_assign(block_table: torch.Tensor, tokens: torch.Tensor, held: torch.Tensor, free_ids: torch.Tensor, free_count: torch.Tensor,
+                 capacity: int, status: Optional[torch.Tensor] = None) -> None:
+    """Brings block_table [B * Hkv, blocks_per_unit], held [B] and the free list (free_ids [n_blocks], free_count [1]) up to date: room for
+    tokens[b] tokens in each unit of sequence b (0: it has left, < 0: as it is).  All int32, on the device, in place."""
+    _int32(block_table, tokens, held, free_ids, free_count, *(() if status is None else (status,)))
+    B, (units, per) = tokens.numel(), block_table.shape
+    if B < 1 or units % B or held.numel() != B or free_count.numel() != 1:
+        raise TypeError("block_table [B * Hkv, blocks_per_unit], tokens and held [B], free_count [1]")
+    _check_device([t.get_device() for t in (block_table, tokens, held, free_ids, free_count)] + ([] if status is None else [status.get_device()]))
+    code = _lib.sqa_block_assign(block_table.data_ptr(), B, units // B, per, capacity, tokens.data_ptr(), held.data_ptr(), free_ids.data_ptr(),
+                                 free_count.data_ptr(), free_ids.numel(), _ptr(status), _stream())
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_block_assign")
+
+
+def slot_map(block_table: Optional[torch.Tensor], capacity: int, T: int, new_pos: int = 0, n_sink: int = 0, B: Optional[int] = None,
+             Hkv: Optional[int] = None, out: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None) -> torch.Tensor:
+    """The row that each of T new tokens of each unit goes to, int32 [B, Hkv, T] (-1: nowhere); block_table [B * Hkv, blocks_per_unit], or
+    None: units one after the other.  B and Hkv from `out` where it is given."""
+    if out is None:
+        if B is None or Hkv is None:
+            raise TypeError("B and Hkv, or out")
+        if block_table is None:
+            raise TypeError("a table or an output says which device")
+        out = torch.empty((B, Hkv, T), dtype=torch.int32, device=block_table.device)
+    B, Hkv = out.shape[:2]
+    _check_out(out, (B, Hkv, T), torch.int32)
+    per, devices = 0, [out.get_device()]
+    if block_table is not None:
+        _int32(block_table)
+        if block_table.dim() != 2 or block_table.shape[0] != B * Hkv:
+            raise TypeError("block_table [B * Hkv, blocks_per_unit]")
+        per = block_table.shape[1]
+        devices.append(block_table.get_device())
+    extra = _opts_at(opts, B, devices[0])
+    _check_device(devices)
+    _check_position(new_pos, "sqa_slot_map")
+    code = _lib.sqa_slot_map(_ptr(block_table), B, T, Hkv, per, capacity, n_sink, new_pos, out.data_ptr(), _stream(), extra)
+    if code != SQA_OK:
+        raise SqaError(code, "sqa_slot_map")
+    return out

@@ -7,11 +7,10 @@
 // A row of one head is 16 bytes per lane (8 to 32 lanes); a wave takes as many heads as fit side by side and U tokens of them, all
 // requested before the first is used: what it writes is U consecutive rows of each head.  The sum of squares and the rotation's
 // partners (rot_dim / 2 elements away: a whole number of lanes) stay inside a row's lanes.  fp32 throughout, rounded once.
-#include "sqa_chunk.h"
+#include "sqa_rows.h"
 
 namespace sqa {
 
-constexpr int kRowsThreads = 256;
 enum { kQuery = 0, kKeyOut = 1, kKeyValue = 2 };    // what a wave's heads are: queries, keys to k_out, keys and values to the cache
 
 struct RowsArgs {
@@ -20,39 +19,9 @@ struct RowsArgs {
   void* q_out;
   void* k_out;                                      // NULL: to the cache
   sqa_head_prep prep;
+  AxesArgs axes;
   int q_groups, kv_groups, t_blocks;                // items of a sequence: head groups x blocks of U tokens
 };
-
-template <typename T> struct Piece;                 // 16 bytes of a row as floats
-template <> struct Piece<float> {
-  static constexpr int E = 4;
-  static __device__ __forceinline__ void open(uint4 w, float* x) {
-    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
-  }
-  static __device__ __forceinline__ uint4 close(const float* x) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  }
-};
-template <> struct Piece<bf16_t> {
-  static constexpr int E = 8;
-  static __device__ __forceinline__ void open(uint4 w, float* x) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(v[i]); x[2 * i + 1] = bf16_hi(v[i]); }
-  }
-  static __device__ __forceinline__ uint4 close(const float* x) {
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
-    return make_uint4(v[0], v[1], v[2], v[3]);
-  }
-};
-
-// the value of the lane half a row away, rows of LPR lanes: where a whole head is rotated
-template <int LPR> __device__ __forceinline__ float half_row_away(float v) {
-  if constexpr (LPR == 16) return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true));      // row_ror:8
-  else return __shfl_xor(v, LPR / 2, LPR);
-}
 
 // May a unit take the chunk?  What its LPR lanes (lane c of them) have to know is asked for before the rows are worked on, all at
 // once, and judged afterwards.  Other waves of the launch may have set the unit's state meanwhile: what is asked holds before and
@@ -95,8 +64,8 @@ __device__ __forceinline__ int judge_unit(const ChunkArgs& a, const UnitAsked& k
   return bad ? SQA_ERR_STATE : (outside ? SQA_ERR_SHAPE : 0);
 }
 
-template <typename T, int D, int U>
-__global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs a) {
+// AXES: rotated by positions on several axes
+template <typename T, int D, int U, bool AXES> __device__ __forceinline__ void rows_work(const RowsArgs& a) {
   constexpr int E = Piece<T>::E, LPR = D / E, HPW = SQA_WAVE / LPR;
   const int lane = threadIdx.x & (SQA_WAVE - 1), c = lane % LPR;
   const int64_t item = (int64_t)blockIdx.x * (kRowsThreads / SQA_WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SQA_WAVE);
@@ -109,7 +78,7 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
   const int t0 = tb * U;
   if (t0 >= s.n) return;
   const bool turn = a.prep.rope != nullptr;
-  if (turn && s.pos + s.n > a.prep.n_pos) {
+  if (!AXES && turn && s.pos + s.n > a.prep.n_pos) {
     if (group == 0 && tb == 0 && lane == 0 && a.c.status) *a.c.status = SQA_ERR_SHAPE;
     return;
   }
@@ -134,55 +103,70 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
   if (kind == kKeyValue) asked = ask_unit(a.c, b, u, s, c);
 
   // ---- norm and rotation
-  const void* wp = kind == kQuery ? a.prep.q_weight : a.prep.k_weight;
-  float w[E];
-  if (wp) Piece<T>::open(ld16(static_cast<const T*>(wp) + c * E), w);
-  const int half = a.prep.rot_dim / 2, e0 = c * E, step = a.prep.interleaved ? 0 : half / E;
-  const bool mine = turn && e0 < a.prep.rot_dim, first = e0 < half;
-  const int partner = mine ? (first ? lane + step : lane - step) : lane;
+  const int e0 = c * E;
+  if constexpr (AXES) {
+    RowPrep<T, D, true> how(a.prep, kind == kQuery ? a.prep.q_weight : a.prep.k_weight, lane);
+    how.set_axes(a.axes);
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    float y[E];
-    Piece<T>::open(x[i], y);
-    if (wp) {
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
-#pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
-      const float r = 1.f / sqrtf(ss * (1.f / D) + a.prep.eps);
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
+    for (int i = 0; i < U; ++i) {
+      float y[E];
+      Piece<T>::open(x[i], y);
+      const AxisPos at = axes_of(a.axes, a.c, a.prep.n_pos, b, t0 + min(i, nt - 1), group == 0 && lane == 0);
+      how.normalise(y);
+      how.rotate(y, at);
+      x[i] = Piece<T>::close(y);
     }
-    if (turn) {
-      const float* row = a.prep.rope + (s.pos + t0 + min(i, nt - 1)) * a.prep.rot_dim;
-      if (a.prep.interleaved) {
-        if (mine) {
+  } else {
+    const void* wp = kind == kQuery ? a.prep.q_weight : a.prep.k_weight;
+    float w[E];
+    if (wp) Piece<T>::open(ld16(static_cast<const T*>(wp) + c * E), w);
+    const int half = a.prep.rot_dim / 2, step = a.prep.interleaved ? 0 : half / E;
+    const bool mine = turn && e0 < a.prep.rot_dim, first = e0 < half;
+    const int partner = mine ? (first ? lane + step : lane - step) : lane;
 #pragma unroll
-          for (int e = 0; e < E; e += 2) {
-            const float cs = row[(e0 + e) / 2], sn = row[half + (e0 + e) / 2];
-            const float p = y[e], q = y[e + 1];
-            y[e] = p * cs - q * sn;
-            y[e + 1] = q * cs + p * sn;
+    for (int i = 0; i < U; ++i) {
+      float y[E];
+      Piece<T>::open(x[i], y);
+      if (wp) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
+        const float r = 1.f / sqrtf(ss * (1.f / D) + a.prep.eps);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
+      }
+      if (turn) {
+        const float* row = a.prep.rope + (s.pos + t0 + min(i, nt - 1)) * a.prep.rot_dim;
+        if (a.prep.interleaved) {
+          if (mine) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              const float cs = row[(e0 + e) / 2], sn = row[half + (e0 + e) / 2];
+              const float p = y[e], q = y[e + 1];
+              y[e] = p * cs - q * sn;
+              y[e + 1] = q * cs + p * sn;
+            }
+          }
+        } else {
+          float cs[E], sn[E];
+          const float* from = row + (mine ? (first ? e0 : e0 - half) : 0);
+#pragma unroll
+          for (int e = 0; e < E; e += 4) {
+            *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
+            *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
+          }
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
+            const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
+            y[e] = mine ? z : y[e];
           }
         }
-      } else {
-        float cs[E], sn[E];
-        const float* from = row + (mine ? (first ? e0 : e0 - half) : 0);
-#pragma unroll
-        for (int e = 0; e < E; e += 4) {
-          *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
-          *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
-          const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
-          y[e] = mine ? z : y[e];
-        }
       }
+      if (wp || turn) x[i] = Piece<T>::close(y);
     }
-    if (wp || turn) x[i] = Piece<T>::close(y);
   }
 
   // ---- where they go
@@ -216,16 +200,8 @@ __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs
     *reinterpret_cast<int4*>(a.c.L.unit_state + (int64_t)u * SQA_ST_WORDS) = make_int4((int)(s.pos + s.n), 0, -2, 0);
 }
 
-static bool bad_rows(const sqa_token_rows& r, int B, int T, size_t es) {
-  const int64_t per16 = (int64_t)(16 / es);
-  return !aligned16(r.data) || (B > 1 && (r.seq_stride < 0 || r.seq_stride % per16)) || (T > 1 && (r.row_stride < 0 || r.row_stride % per16));
-}
-
-static bool rows_overlap(const sqa_token_rows* r, int B, int T, int H, int D, size_t es, const void* p, size_t n) {
-  if (!r) return false;
-  const int64_t last = (B > 1 ? (int64_t)(B - 1) * r->seq_stride : 0) + (T > 1 ? (int64_t)(T - 1) * r->row_stride : 0) + (int64_t)H * D;
-  return overlap(r->data, (size_t)last * es, p, n);
-}
+template <typename T, int D, int U> __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs a) { rows_work<T, D, U, false>(a); }
+template <typename T, int D, int U> __global__ __launch_bounds__(kRowsThreads) void axis_rows_kernel(const RowsArgs a) { rows_work<T, D, U, true>(a); }
 
 template <typename T, int D>
 static void launch_rows(RowsArgs& a, hipStream_t st) {
@@ -241,13 +217,18 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   const bool two = groups * ((a.c.T + 1) / 2) >= 1024;
   a.t_blocks = two ? (a.c.T + 1) / 2 : a.c.T;
   const int64_t blocks = (groups * a.t_blocks + waves - 1) / waves;
+  if (a.axes.n) {
+    if (two) axis_rows_kernel<T, D, 2><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
+    else axis_rows_kernel<T, D, 1><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
+    return;
+  }
   if (two) chunk_rows_kernel<T, D, 2><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
   else chunk_rows_kernel<T, D, 1><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
 }
 
 static sqa_status rows_call(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt, int B, int T, int Hq,
                             int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out, void* k_out,
-                            const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts) {
+                            const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts, const sqa_rope_axes* axes) {
   if ((q != nullptr) != (q_out != nullptr) || (q && !q->data) || (k && !k->data) || (v && !v->data)) return SQA_ERR_NULL;
   if (dt != SQA_F32 && dt != SQA_BF16) return SQA_ERR_DTYPE;
   if (bad_chunk_shape(B, T, Hq, Hkv, D, new_pos, opts)) return SQA_ERR_SHAPE;
@@ -256,14 +237,12 @@ static sqa_status rows_call(const sqa_token_rows* q, const sqa_token_rows* k, co
   if (!aligned16(q_out) || !aligned16(k_out)) return SQA_ERR_SHAPE;
   RowsArgs a{};
   if (prep) {
-    if (!aligned16(prep->q_weight) || !aligned16(prep->k_weight) || !aligned16(prep->rope)) return SQA_ERR_SHAPE;
-    if ((prep->q_weight || prep->k_weight) && !(prep->eps >= 0.f)) return SQA_ERR_SHAPE;
-    if (prep->rope && (prep->n_pos < 1 || prep->rot_dim < 16 || prep->rot_dim % 16 || prep->rot_dim > D ||
-                       (prep->interleaved != 0 && prep->interleaved != 1) ||
-                       (!(opts && opts->new_pos_seq) && !(opts && opts->prompt_len) && (int64_t)new_pos + T > prep->n_pos)))
-      return SQA_ERR_SHAPE;
+    const sqa_status bad = check_prep(*prep, D, axes, new_pos, T, opts);
+    if (bad) return bad;
     a.prep = *prep;
   }
+  sqa_status why;
+  if (axes && !axes_args(axes, prep, &a.axes, &why)) return why;
   // (where every sequence brings T tokens at new_pos, the host sees whether they fit)
   if (layer && !(opts && (opts->prompt_len || opts->new_pos_seq)) &&
       (int64_t)new_pos + T > (layer->budget < layer->capacity ? layer->budget : layer->capacity))
@@ -293,18 +272,30 @@ static sqa_status rows_call(const sqa_token_rows* q, const sqa_token_rows* k, co
 
 }  // namespace sqa
 
+extern "C" sqa_status sqa_qk_norm_rope_ex(const sqa_token_rows* q, const sqa_token_rows* k, sqa_dtype dt, int B, int T, int Hq, int Hkv,
+                                          int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out, void* k_out, void* stream,
+                                          const sqa_batch_opts* opts, const sqa_rope_axes* axes) {
+  if ((!q && !k) || (k != nullptr) != (k_out != nullptr)) return SQA_ERR_NULL;
+  return sqa::rows_call(q, k, nullptr, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, k_out, nullptr, stream, opts, axes);
+}
+
 extern "C" sqa_status sqa_qk_norm_rope(const sqa_token_rows* q, const sqa_token_rows* k, sqa_dtype dt, int B, int T, int Hq, int Hkv,
                                        int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out, void* k_out, void* stream,
                                        const sqa_batch_opts* opts) {
-  if ((!q && !k) || (k != nullptr) != (k_out != nullptr)) return SQA_ERR_NULL;
-  return sqa::rows_call(q, k, nullptr, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, k_out, nullptr, stream, opts);
+  return sqa_qk_norm_rope_ex(q, k, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, k_out, stream, opts, nullptr);
+}
+
+extern "C" sqa_status sqa_chunk_append_ex(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt, int B,
+                                          int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out,
+                                          const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts, const sqa_rope_axes* axes) {
+  if (!k || !v || !layer) return SQA_ERR_NULL;
+  sqa_status why;
+  if (sqa::bad_layer(*layer, &why)) return why;
+  return sqa::rows_call(q, k, v, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, nullptr, layer, stream, opts, axes);
 }
 
 extern "C" sqa_status sqa_chunk_append(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt, int B,
                                        int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out,
                                        const sqa_layer_cache* layer, void* stream, const sqa_batch_opts* opts) {
-  if (!k || !v || !layer) return SQA_ERR_NULL;
-  sqa_status why;
-  if (sqa::bad_layer(*layer, &why)) return why;
-  return sqa::rows_call(q, k, v, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, nullptr, layer, stream, opts);
+  return sqa_chunk_append_ex(q, k, v, dt, B, T, Hq, Hkv, D, prep, new_pos, q_out, layer, stream, opts, nullptr);
 }
