@@ -17,7 +17,11 @@
 namespace sqa {
 
 constexpr int kQ4Slots = 32;                        // slots of a tile
-constexpr int kQ4Records = 16384;                   // rows of sums that the workspace has room for
+typedef __attribute__((address_space(1))) const uint8_t g_u8_t;
+typedef __attribute__((address_space(3))) v4u_t lds_v4u_t;
+
+constexpr int kQ4Splits = 64;                       // workgroups that share out a unit's slots: a lane each when they are joined
+constexpr int kQ4Records = 256 * 16;                // rows of sums that the workspace has room for: no more workgroups than 256 are joined
 
 struct Q4AttentionArgs {
   Q4Args a;
@@ -28,10 +32,17 @@ struct Q4AttentionArgs {
   float4* part;                                     // [items][splits][rows][D / 4 + 1]: sums, then (m, l, bad)
   float scale;                                      // log2(e) / sqrt(D)
   float near;                                       // 8 / scale: logits that close to a row's reference do not move it
-  uint32_t group_m;                                 // 2^32 / g, for divisions by g
+  uint32_t group_m, heads_m, tiles_m, splits_m;     // 2^32 / g, / Hkv, / tiles, / splits: for divisions by them
   int tiles, splits;
 };
 
+// q = x / d and what is left, for 0 <= x < 2^31 and m = 2^32 / d rounded up: the high product is one too large at most
+__device__ __forceinline__ void divide(int x, int d, uint32_t m, int& q, int& r) {
+  q = d > 1 ? (int)__umulhi((uint32_t)x, m) : x;
+  r = x - q * d;
+  if (r < 0) { --q; r += d; }
+}
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }           // (the same in all lanes)
 __device__ __forceinline__ float lanes16_max(float v) { v = fmaxf(v, __shfl_xor(v, 16, SQA_WAVE)); return fmaxf(v, __shfl_xor(v, 32, SQA_WAVE)); }
 __device__ __forceinline__ float lanes16_sum(float v) { v += __shfl_xor(v, 16, SQA_WAVE); return v + __shfl_xor(v, 32, SQA_WAVE); }
 
@@ -68,7 +79,7 @@ template <typename T, int D> struct Q4Tile {
 };
 
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4AttentionArgs a) {
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_kernel(const Q4AttentionArgs a) {
   using C = Q4Tile<T, D>;
   constexpr int M = 16, NE = C::NE, NL = C::NL, NP = C::NP, NV = C::NV, KD = C::KD, PP = D / 4, REC = PP + 1, NT = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // V tiles of the waves, at the end their sums; then the table
@@ -83,28 +94,37 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
   const uint32_t total = (uint32_t)(a.a.c.B * a.a.c.Hkv) * (uint32_t)(a.tiles * a.splits);
   const uint32_t per8 = (total + 7) / 8, work = (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);
   if (blockIdx.x >> 3 >= per8 || work >= total) return;
-  const int split = (int)(work % (uint32_t)a.splits);
-  const uint32_t item = work / (uint32_t)a.splits;
-  const int u = (int)(item / (uint32_t)a.tiles), tile = a.tiles - 1 - (int)(item % (uint32_t)a.tiles);      // (the longest first)
-  const int b = u / a.a.c.Hkv, h = u - b * a.a.c.Hkv, g = a.a.c.g;
-  const Q4Seq s = q4_seq(a.a, b, tid == 0 && h == 0 && tile == 0 && split == 0);
+  int split, tile, h, item, u, b;
+  divide((int)work, a.splits, a.splits_m, item, split);
+  divide(item, a.tiles, a.tiles_m, u, tile);
+  tile = a.tiles - 1 - tile;                        // (the longest first)
+  divide(u, a.a.c.Hkv, a.heads_m, b, h);
+  const int g = a.a.c.g;
+  Q4Seq s = q4_seq(a.a, b, tid == 0 && h == 0 && tile == 0 && split == 0);
+  s.n = scalar(s.n); s.slots = scalar(s.slots); s.why = scalar(s.why);
+  s.pos = (int64_t)scalar((int)s.pos);              // (positions are 32-bit numbers)
   const int rows = s.n * g, row0 = tile * M;
   if (row0 >= rows) return;
   const int last_row = min(row0 + M, rows) - 1;
   auto place = [&](int r, int& t, int& head) {
-    t = g > 1 ? (int)__umulhi((uint32_t)r, a.group_m) : r;
-    int x = r - t * g;
-    if (x < 0) { --t; x += g; }
+    int x;
+    divide(r, g, a.group_m, t, x);
     head = h * g + x;
   };
   int t_first, t_last, any;
   place(row0, t_first, any);
   place(last_row, t_last, any);
+  t_first = scalar(t_first); t_last = scalar(t_last);
   const bool turned = s.end() > s.slots;
   const int len = s.why ? 1 : s.len();
   const int end = turned ? len : min((int)s.pos + t_last + 1, len);                      // slots that the rows see lie before it
   const int whole = turned ? (s.n == 1 ? len : 0) : min((int)s.pos + t_first + 1, len);   // ... that all rows see
-  const int nt = (end + kQ4Slots - 1) / kQ4Slots, per = (nt + a.splits - 1) / a.splits, parts = (nt + per - 1) / per;
+  const int nt = (int)((uint32_t)(end + kQ4Slots - 1) / kQ4Slots);
+  int per = nt, parts = 1, rest;
+  if (a.splits > 1) {
+    divide(nt + a.splits - 1, a.splits, a.splits_m, per, rest);
+    parts = (int)((uint32_t)(nt + per - 1) / (uint32_t)per);
+  }
   const int tile0 = split * per, tile1 = min(tile0 + per, nt);
   if (split >= parts) return;
 
@@ -128,11 +148,12 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
   place(min(row0 + i, last_row), t, head);
   const int back = s.n - 1 - t;                     // a slot of the ring is seen when its token is at least so far behind the newest
   const int newest = s.slot(s.end() - 1);           // ... and it lies here
-  const int fixed = turned ? s.sink : 0, ring = s.slots - s.sink;
+  const int fixed = turned ? s.sink : 0, ring = turned ? s.slots - s.sink : 0;
+  // (without branches: they are not faster, and where a value was set to -inf behind && and || some lanes have been seen to keep theirs)
   auto sees = [&](int slot) {
     int behind = newest - slot;
-    if (turned && behind < 0) behind += ring;
-    return slot < len && (slot < fixed || behind >= back);
+    behind += behind < 0 ? ring : 0;
+    return (bool)((int)(slot < len) & ((int)(slot < fixed) | (int)(behind >= back)));
   };
   // its elements 8 KD j .. of step x: 8 (KD j + x) ..
   uint4 qp[NP][KD];
@@ -165,28 +186,47 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
     }
     bad = __syncthreads_or(bad);
   }
+  // ---- rows of 16 neighbouring slots lie one after the other; slots behind the last one are read as that one again
   const int64_t unit_row = (int64_t)u * L.capacity;
-  auto row_of = [&](int slot) {                     // (slots behind the last: that one again)
-    slot = min(slot, end - 1);
-    return L.block_table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS - 2 * tile0] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit_row + slot;
+  auto row_of = [&](int slot) {                     // (the same in all lanes)
+    return L.block_table ? (int64_t)__builtin_amdgcn_readfirstlane(s_table[slot / SQA_BLOCK_SLOTS - 2 * tile0]) * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS
+                         : unit_row + slot;
   };
-
-  struct Loaded { uint32_t k[2][KD]; uint4 v[NL]; uint32_t kp[2], vp[NL]; };
-  auto fetch = [&](int tl, Loaded& x) {
+  struct At { int64_t row[2]; int last[2]; };       // of a tile's halves: the first row, and the last that there is behind it
+  auto locate = [&](int tl) {
+    const int slot = tl * kQ4Slots;
+    At x;
+    x.row[0] = row_of(slot); x.last[0] = min(end - 1 - slot, 15);
+    const bool two = end - slot > 16;               // (a half without a slot: the first half again)
+    x.row[1] = two ? row_of(slot + 16) : x.row[0]; x.last[1] = two ? min(end - 17 - slot, 15) : x.last[0];
+    return x;
+  };
+  struct Codes { uint32_t k[2][KD], kp[2], vp[NL]; uint4 v[NL]; } now;
+  auto fetch_keys = [&](const At& x, Codes& to) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const int64_t row = row_of(tl * kQ4Slots + 16 * kb + i);
-      const char* at = static_cast<const char*>(L.K) + row * C::RB + 4 * KD * j;
-      if constexpr (KD == 4) { const uint4 w = ld16(at); x.k[kb][0] = w.x; x.k[kb][1] = w.y; x.k[kb][2] = w.z; x.k[kb][3] = w.w; }
-      else { const uint2 w = *reinterpret_cast<const uint2*>(at); x.k[kb][0] = w.x; x.k[kb][1] = w.y; }
-      x.kp[kb] = L.K_scale[row * C::GPR + KD * j / 4];
+      const uint32_t r = (uint32_t)min(i, x.last[kb]);
+      const char* at = uniform(static_cast<const char*>(L.K) + x.row[kb] * C::RB) + (r * C::RB + 4 * KD * j);
+      if constexpr (KD == 4) { const uint4 w = ld16(at); to.k[kb][0] = w.x; to.k[kb][1] = w.y; to.k[kb][2] = w.z; to.k[kb][3] = w.w; }
+      else { const v2u_t w = *(const g_v2u_t*)at; to.k[kb][0] = w.x; to.k[kb][1] = w.y; }
+      to.kp[kb] = *(const g_u8_t*)(uniform(reinterpret_cast<const char*>(L.K_scale) + x.row[kb] * C::GPR) + (r * C::GPR + KD * j / 4));
     }
+  };
+  auto fetch_values = [&](const At& x, Codes& to) {
 #pragma unroll
     for (int y = 0; y < NL; ++y) {
-      const int vr = D == 128 ? 16 * y + (lane >> 2) : lane >> 1, vc = D == 128 ? lane & 3 : lane & 1;
-      const int64_t row = row_of(tl * kQ4Slots + vr);
-      x.v[y] = ld16(static_cast<const char*>(L.V) + row * C::RB + 16 * vc);
-      x.vp[y] = L.V_scale[row * C::GPR + vc];
+      const int half = D == 128 ? y : lane >> 5;    // (rows of 64: 32 of them in one load)
+      const uint32_t r = D == 128 ? (uint32_t)min(lane >> 2, x.last[y]) : (uint32_t)min((lane >> 1) & 15, half ? x.last[1] : x.last[0]);
+      const uint32_t c = D == 128 ? lane & 3 : lane & 1;
+      const char* codes = uniform(static_cast<const char*>(L.V) + x.row[D == 128 ? y : 0] * C::RB);
+      const char* powers = uniform(reinterpret_cast<const char*>(L.V_scale) + x.row[D == 128 ? y : 0] * C::GPR);
+      if constexpr (D == 64) {
+        const char* const c1 = uniform(static_cast<const char*>(L.V) + x.row[1] * C::RB);
+        const char* const p1 = uniform(reinterpret_cast<const char*>(L.V_scale) + x.row[1] * C::GPR);
+        codes = half ? c1 : codes; powers = half ? p1 : powers;
+      }
+      to.v[y] = ld16_nt(codes + (r * C::RB + 16 * c));
+      to.vp[y] = *(const g_u8_t*)(powers + (r * C::GPR + c));
     }
   };
 
@@ -194,32 +234,39 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
 #pragma unroll
   for (int e = 0; e < NE; ++e) o[e] = f32x4_t{};
   float m = -FLT_MAX, l = 0.f;
-  char* const Vt = s_stage + wave * C::VB;
+  // the lane's places in the wave's tile of V: of its first row's pieces (the others by exclusive or), of its column's rows
+  const int put_row = D == 128 ? lane >> 2 : lane >> 1, put_piece = D == 128 ? 4 * (lane & 3) : 4 * (lane & 1), get_row = 4 * j + i / 4;
+  const uint32_t tile_at = lds_at(s_stage) + wave * C::VB;
+  uint32_t put = tile_at + put_row * (2 * D) + ((put_piece ^ C::swizzle(put_row)) << 4);
+  uint32_t get = tile_at + get_row * (2 * D) + ((((i & 3) >> 1) ^ C::swizzle(get_row)) << 4) + (i & 1) * 8;
 
-  Loaded now{}, next{};
-  if (tile0 + wave < tile1) fetch(tile0 + wave, now);
+  if (tile0 + wave < tile1) {
+    const At x = locate(tile0 + wave);
+    fetch_keys(x, now);
+    fetch_values(x, now);
+  }
 #pragma unroll 1
   for (int tl = tile0 + wave; tl < tile1; tl += NW) {
-    if (tl + NW < tile1) fetch(tl + NW, next);
+    asm volatile("" : "+v"(put), "+v"(get));        // (their exclusive ors take an instruction each, not registers of their own)
+    // (the last one again where there are no more: a load under a condition would have the compiler wait for all loads before the next use)
+    const At ahead = locate(tl + NW < tile1 ? tl + NW : tl);
     // ---- s[kb][r]: slot 32 tl + 16 kb + 4 j + r of row i
-    f32x4_t sc[2];
+    f32x4_t sc[2] = {f32x4_t{}, f32x4_t{}};
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      sc[kb] = f32x4_t{};
-      const float power = __uint_as_float(now.kp[kb] << 23);
+    for (int x = 0; x < KD; ++x) {
 #pragma unroll
-      for (int x = 0; x < KD; ++x) {
-        const bf16x8_t k = __builtin_bit_cast(bf16x8_t, q4_open(now.k[kb][x], power));
+      for (int kb = 0; kb < 2; ++kb) {
+        const bf16x8_t k = __builtin_bit_cast(bf16x8_t, q4_open(now.k[kb][x], __uint_as_float(now.kp[kb] << 23)));
 #pragma unroll
         for (int p = 0; p < NP; ++p) sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8_t, qp[p][x]), sc[kb], 0, 0, 0);
       }
     }
+    fetch_keys(ahead, now);               // (into registers that have just been used)
     // ---- V to LDS as bf16
     const bool edge = (tl + 1) * kQ4Slots > whole;
     uint64_t odd[NL] = {};                          // (lanes whose group is not finite, where not every row sees it)
 #pragma unroll
     for (int y = 0; y < NL; ++y) {
-      const int row = D == 128 ? 16 * y + (lane >> 2) : lane >> 1, first = D == 128 ? 4 * (lane & 3) : 4 * (lane & 1);
       uint4 w = now.v[y];
       uint32_t power = now.vp[y];
       if (edge) {
@@ -230,8 +277,9 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
       const uint32_t c[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int p = 0; p < 4; ++p)
-        *reinterpret_cast<uint4*>(Vt + row * (2 * D) + (((first + p) ^ C::swizzle(row)) << 4)) = q4_open(c[p], vs);
+        *(lds_v4u_t*)(uintptr_t)((put ^ (p << 4)) + y * (32 * D)) = __builtin_bit_cast(v4u_t, q4_open(c[p], vs));
     }
+    fetch_values(ahead, now);
     asm volatile("" ::: "memory");                  // (a wave's LDS accesses are done in order)
     // ---- softmax
     if (edge) {
@@ -239,7 +287,7 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (!sees(tl * kQ4Slots + 16 * kb + 4 * j + r)) sc[kb][r] = -INFINITY;
+          sc[kb][r] = sees(tl * kQ4Slots + 16 * kb + 4 * j + r) ? sc[kb][r] : -INFINITY;
     }
     float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
     if (__any(top > m + a.near)) {                  // the reference of a row moves when one of its logits is 2^8 times beyond it
@@ -262,19 +310,23 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
 #pragma unroll
         for (int k = 0; k < NV; ++k) pw[k][2 * kb + r / 2] = w[k];
       }
-    // ---- O^T += V^T.P^T
+    // ---- O^T += V^T.P^T, four blocks of 16 elements at a time
 #pragma unroll
-    for (int e = 0; e < NE; ++e) {
-      s16x4_t half[2];
+    for (int e0 = 0; e0 < NE; e0 += 4) {
+      bf16x8_t v[4];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int row = 16 * kb + 4 * j + i / 4, piece = (2 * e + ((i & 3) >> 1)) ^ C::swizzle(row);
-        half[kb] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(Vt + row * (2 * D) + piece * 16 + (i & 1) * 8));
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t at = get ^ ((e0 + e) << 5);
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)at);
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)(at + 32 * D));
+        v[e] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
-      const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, make_uint4(pw[k][0], pw[k][1], pw[k][2], pw[k][3])), o[e], 0, 0, 0);
+      for (int k = 0; k < NV; ++k) {
+        const bf16x8_t pk = __builtin_bit_cast(bf16x8_t, make_uint4(pw[k][0], pw[k][1], pw[k][2], pw[k][3]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e], pk, o[e0 + e], 0, 0, 0);
+      }
     }
     // the groups that are not finite, to the rows that see them
 #pragma unroll
@@ -288,7 +340,6 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
         for (int e = 0; e < NE; ++e) o[e] += e / 2 == group ? add : 0.f;
       }
     asm volatile("" ::: "memory");
-    now = next;
   }
 
   // ---- the waves' sums joined, each row's pieces of 16 bytes in an order without bank conflicts
@@ -296,7 +347,7 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
   if (j == 0) { s_m[wave][i] = m; s_l[wave][i] = l; }
   __syncthreads();
   float top = s_m[0][i];
-#pragma unroll
+#pragma unroll 2
   for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][i]);
   const float keep = exp2_fast((m - top) * a.scale);
   float4* const mine = reinterpret_cast<float4*>(s_stage) + (wave * M + i) * PP;
@@ -305,15 +356,15 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
   __syncthreads();
   auto joined = [&](int row, float& mm, float& ll) {
     mm = s_m[0][row];
-#pragma unroll
+#pragma unroll 2
     for (int w = 1; w < NW; ++w) mm = fmaxf(mm, s_m[w][row]);
     ll = 0.f;
-#pragma unroll
+#pragma unroll 2
     for (int w = 0; w < NW; ++w) ll += s_l[w][row] * exp2_fast((s_m[w][row] - mm) * a.scale);
   };
   auto piece4 = [&](int row, int p) {
     float4 v = reinterpret_cast<const float4*>(s_stage)[row * PP + (p ^ row)];
-#pragma unroll
+#pragma unroll 2
     for (int w = 1; w < NW; ++w) {
       const float4 x = reinterpret_cast<const float4*>(s_stage)[(w * M + row) * PP + (p ^ row)];
       v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
@@ -354,58 +405,129 @@ __global__ __launch_bounds__(64 * NW) void q4_attention_kernel(const Q4Attention
     rec.put(refs + split * M + row, make_float4(mm, ll, (float)bad, 0.f));
   }
   if (!last_to_arrive(a.count + item, parts, &s_word)) return;
-  bad = 0;
-  for (int x = tid; x < parts; x += NT) bad |= rec.get(refs + x * M).z != 0.f;
-  if (__syncthreads_or(bad)) { refuse(SQA_ERR_SHAPE); return; }
-  for (int x = tid; x < live; x += NT) {
-    const int row = x / (PP / 2), p = x % (PP / 2);
-    float mm = -FLT_MAX, ll = 0.f;
-    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int k0 = 0; k0 < parts; k0 += 4) {
-      float4 ml[4], w4[4][2];
+  // ---- all workgroups' sums.  Few records: a thread asks for all that it needs at once.
+  if (parts <= 8) {
+    bad = 0;
+    for (int x = tid; x < live; x += NT) {
+      const int row = x / (PP / 2), p = x % (PP / 2);
+      float4 ml[8], w4[8][2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t from = (uint32_t)(min(k0 + k, parts - 1) * M + row);
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t from = (uint32_t)(min(k, parts - 1) * M + row);
         ml[k] = rec.get(refs + from); w4[k][0] = rec.get(from * PP + 2 * p); w4[k][1] = rec.get(from * PP + 2 * p + 1);
       }
+      float mm = ml[0].x, ll = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k0 + k < parts) {
-          const float to = fmaxf(mm, ml[k].x), w0 = exp2_fast((mm - to) * a.scale), w1 = exp2_fast((ml[k].x - to) * a.scale);
-          mm = to;
-          ll = fmaf(ll, w0, ml[k].y * w1);
+      for (int k = 1; k < 8; ++k) mm = fmaxf(mm, ml[k].x);
+      float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k >= parts) break;
+        const float w = exp2_fast((ml[k].x - mm) * a.scale);
+        ll = fmaf(w, ml[k].y, ll);
+        bad |= ml[k].z != 0.f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
+      }
+      if (bad) break;
+      store8(row, p, v, mm, ll);
+    }
+    if (__syncthreads_or(bad)) refuse(SQA_ERR_SHAPE);
+    return;
+  }
+  // Many: each one's weight per row first, then the weighted pieces, the records shared out among groups of threads.
+  float* const s_weight = reinterpret_cast<float*>(s_stage);                             // [parts][M], then the groups' sums
+  const int live_rows = last_row + 1 - row0;
+  bad = 0;
+  for (int row = wave; row < live_rows; row += NW) {                                     // a lane per record (there are 64 at most)
+    const float4 ml = rec.get(refs + (uint32_t)(min(lane, parts - 1) * M + row));
+    const bool there = lane < parts;
+    bad |= there && ml.z != 0.f;
+    float mm = there ? ml.x : -FLT_MAX;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o, SQA_WAVE));
+    const float w = exp2_fast((ml.x - mm) * a.scale);
+    const float ll = wave_sum(there ? w * ml.y : 0.f);
+    if (there) s_weight[lane * M + row] = w;
+    if (lane == 0) { s_m[0][row] = mm; s_l[0][row] = ll; }
+  }
+  if (__syncthreads_or(bad)) { refuse(SQA_ERR_SHAPE); return; }
+  int groups = 1;
+  while (groups * 2 * live <= NT && groups < parts) groups *= 2;
+  float4* const s_sum = reinterpret_cast<float4*>(s_stage + kQ4Splits * M * 4);
+  const int per_group = groups * live;
+  for (int x0 = 0; x0 < live; x0 += NT) {            // (once, but for more pieces than threads: one group then)
+    const int x = x0 + tid % (groups > 1 ? live : NT), grp = groups > 1 ? tid / live : 0;
+    if (x >= live || (groups > 1 && tid >= per_group)) { if (groups == 1) continue; else break; }
+    const int row = x / (PP / 2), p = x % (PP / 2);
+    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+    for (int k0 = grp; k0 < parts; k0 += 8 * groups) {
+      float4 w4[8][2];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t from = (uint32_t)(min(k0 + k * groups, parts - 1) * M + row) * PP + 2 * p;
+        w4[k][0] = rec.get(from); w4[k][1] = rec.get(from + 1);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k0 + k * groups < parts) {
+          const float w = s_weight[(k0 + k * groups) * M + row];
 #pragma unroll
           for (int y = 0; y < 2; ++y)
-            v[y] = make_float4(fmaf(v[y].x, w0, w4[k][y].x * w1), fmaf(v[y].y, w0, w4[k][y].y * w1), fmaf(v[y].z, w0, w4[k][y].z * w1), fmaf(v[y].w, w0, w4[k][y].w * w1));
+            v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
         }
     }
-    store8(row, p, v, mm, ll);
+    if (groups == 1) store8(row, p, v, s_m[0][row], s_l[0][row]);
+    else { s_sum[2 * (grp * live + x)] = v[0]; s_sum[2 * (grp * live + x) + 1] = v[1]; }
+  }
+  if (groups == 1) return;
+  __syncthreads();
+  if (tid < live) {
+    const int row = tid / (PP / 2), p = tid % (PP / 2);
+    float4 v[2] = {s_sum[2 * tid], s_sum[2 * tid + 1]};
+    for (int k = 1; k < groups; ++k)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float4 x = s_sum[2 * (k * live + tid) + y];
+        v[y].x += x.x; v[y].y += x.y; v[y].z += x.z; v[y].w += x.w;
+      }
+    store8(row, p, v, s_m[0][row], s_l[0][row]);
   }
 }
 
-struct Q4Plan { int tiles, splits; };
-static Q4Plan q4_plan(int B, int T, int Hq, int Hkv, int D, int32_t new_pos, int32_t capacity, bool uniform) {
+struct Q4Plan { int waves, tiles, splits; };         // waves of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
+static Q4Plan q4_plan(int B, int T, int Hq, int Hkv, int32_t new_pos, int32_t capacity, bool uniform) {
   Q4Plan p;
   const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity;
   p.tiles = (T * (Hq / Hkv) + 15) / 16;
   const int64_t items = (int64_t)B * Hkv * p.tiles;
-  int64_t s = items > kChunkCounters ? 1 : 1024 / items;
-  s = std::min(s, slots / 256);
-  s = std::min<int64_t>(s, kQ4Records / 16 / items);
+  // A join through the workspace costs 5 us, one inside a workgroup 1: units are shared out among waves before workgroups, and among these
+  // only until every CU has one.  (256 units of 1000 slots: 8 waves 12.2 us, 4 with 3 workgroups a unit 14.0; 8 units of 30000: 32
+  // workgroups of 8 waves each 19.2, 64 22.8, 64 of 4 waves 24.6; 512 units of 1000: 4 waves 18.7, 8 20.0; 2048 of 571: 2 waves 31.2, 4 36.5, 8 44.)
+  p.waves = items >= 1024 ? 2 : (items >= 512 ? 4 : 8);
+  int64_t s = 256 / items;
+  s = std::min(s, slots / 256);                     // (8 tiles at least: a wave each)
+  s = std::min<int64_t>(s, kQ4Splits);
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }
 
-template <typename T, int D> static sqa_status launch_q4(const Q4AttentionArgs& a, hipStream_t st) {
-  constexpr int NW = 4;
+template <typename T, int D, int NW> static sqa_status start_q4(const Q4AttentionArgs& a, hipStream_t st) {
   auto fn = q4_attention_kernel<T, D, NW>;
-  size_t lds = NW * Q4Tile<T, D>::VB;
+  using C = Q4Tile<T, D>;
+  size_t lds = NW * C::VB;
   if (a.a.L.block_table) lds += (size_t)(a.a.L.blocks_per_unit + 3) / 4 * 16 + 16;
   SQA_HIP_CHECK(allow_dynamic_lds(reinterpret_cast<const void*>(fn), lds));
   const int64_t work = (int64_t)a.a.c.B * a.a.c.Hkv * a.tiles * a.splits;
   fn<<<(unsigned)xcd_grid(work), 64 * NW, lds, st>>>(a);
   SQA_HIP_CHECK(hipGetLastError());
   return SQA_OK;
+}
+template <typename T, int D> static sqa_status launch_q4(int waves, const Q4AttentionArgs& a, hipStream_t st) {
+  if (waves == 2) return start_q4<T, D, 2>(a, st);
+  return waves == 8 ? start_q4<T, D, 8>(a, st) : start_q4<T, D, 4>(a, st);
 }
 
 }  // namespace sqa
@@ -431,7 +553,7 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   if (uniform && (int64_t)new_pos + T > layer->capacity && T > layer->capacity - layer->n_sink) return SQA_ERR_CAPACITY;
   const size_t es = dt == SQA_F32 ? 4 : 2, qb = (size_t)B * Hq * T * D * es, lb = (size_t)B * Hq * T * sizeof(float);
   if (overlap(q, qb, out, qb) || (lse && (overlap(lse, lb, q, qb) || overlap(lse, lb, out, qb)))) return SQA_ERR_SHAPE;
-  const Q4Plan p = q4_plan(B, T, Hq, Hkv, D, new_pos, layer->capacity, uniform);
+  const Q4Plan p = q4_plan(B, T, Hq, Hkv, new_pos, layer->capacity, uniform);
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   Q4AttentionArgs a{};
   a.a = q4_args(layer, B, T, Hq, Hkv, new_pos, opts);
@@ -440,9 +562,10 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   a.part = reinterpret_cast<float4*>(static_cast<char*>(workspace) + kChunkCounterBytes);
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   a.near = 8.f / a.scale;
-  a.group_m = 0xffffffffu / (uint32_t)a.a.c.g + 1;
+  auto reciprocal = [](int d) { return 0xffffffffu / (uint32_t)d + 1; };
+  a.group_m = reciprocal(a.a.c.g); a.heads_m = reciprocal(Hkv); a.tiles_m = reciprocal(p.tiles); a.splits_m = reciprocal(p.splits);
   a.tiles = p.tiles; a.splits = p.splits;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dt == SQA_F32) return D == 64 ? launch_q4<float, 64>(a, st) : launch_q4<float, 128>(a, st);
-  return D == 64 ? launch_q4<bf16_t, 64>(a, st) : launch_q4<bf16_t, 128>(a, st);
+  if (dt == SQA_F32) return D == 64 ? launch_q4<float, 64>(p.waves, a, st) : launch_q4<float, 128>(p.waves, a, st);
+  return D == 64 ? launch_q4<bf16_t, 64>(p.waves, a, st) : launch_q4<bf16_t, 128>(p.waves, a, st);
 }
