@@ -620,11 +620,23 @@ size_t sqa_q4_workspace_bytes(const sqa_q4_cache* layer, int B, int T, int Hq, i
  * With the positions, lengths and budgets of the append.  A token whose own slot was taken again by the chunk's later ones cannot be (see
  * sqa_q4_append): such a sequence gets rows of zeros and lse -inf, status SQA_ERR_CAPACITY; so does a unit one of whose blocks lies
  * outside the pools, status SQA_ERR_SHAPE (tokens that see nothing of that block may have their rows all the same).  Queries, probabilities and sums keep fp32's precision (bf16: queries exactly, probabilities
- * to 2^-16; where a workgroup has 128 rows they are rounded to bf16 for the product with V).  A slot that a token may not see does not
+ * to 2^-15; where a workgroup has 128 rows (sqa_q4_plan) they are rounded to bf16 for the product with V).  A slot that a token may not see does not
  * change its row by a bit.  Results are the same from run to run. */
 sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
                             const sqa_q4_cache* layer, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream,
                             const sqa_batch_opts* opts);
+
+/* How sqa_q4_attention would lay a chunk out on the chip (host arithmetic, no GPU call).  Of `layer` only capacity is read, of opts
+ * whether prompt_len and new_pos_seq are NULL. */
+typedef struct sqa_q4_plan_info {
+  int32_t rows;             /* query rows (tokens x query heads of a KV head) of a workgroup: 16 or 128              */
+  int32_t waves;            /* waves of 64 threads of a workgroup; with 16 rows they share out its slots             */
+  int32_t row_tiles;        /* workgroups that the rows of a unit take                                               */
+  int32_t slot_splits;      /* k > 1: k workgroups share out the slots of the same rows, and the last one joins them */
+  int32_t rounded_probs;    /* 1: probabilities are rounded to bf16 for the product with V                            */
+} sqa_q4_plan_info;
+sqa_status sqa_q4_plan(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                       const sqa_batch_opts* opts, sqa_q4_plan_info* info);
 
 /* ---- block tables and slot maps on the GPU -----------------------------------
  * For loops whose lengths live on the GPU (or that are captured into a graph): tables of either kind of cache are brought up to

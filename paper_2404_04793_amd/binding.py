@@ -88,6 +88,11 @@ class Q4CacheStruct(C.Structure):
                 ("capacity", C.c_int32), ("n_sink", C.c_int32), ("blocks_per_unit", C.c_int32), ("n_blocks", C.c_int32)]
 
 
+class Q4PlanInfo(C.Structure):
+    """Mirror of sqa_q4_plan_info."""
+    _fields_ = [(f, C.c_int32) for f in ("rows", "waves", "row_tiles", "slot_splits", "rounded_probs")]
+
+
 class ChunkPlanInfo(C.Structure):
     """Mirror of sqa_chunk_plan_info."""
     _fields_ = [(f, C.c_int32) for f in ("rows", "row_tiles", "slot_splits", "units_in_turn", "rounded_probs", "score_slots",
@@ -163,6 +168,8 @@ _lib.sqa_q4_workspace_bytes.restype = _sz
 _lib.sqa_q4_workspace_bytes.argtypes = [_vp, _i, _i, _i, _i, _i]
 _lib.sqa_q4_attention.restype = _i
 _lib.sqa_q4_attention.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+_lib.sqa_q4_plan.restype = _i
+_lib.sqa_q4_plan.argtypes = [_vp, _i, _i, _i, _i, _i, _i, C.c_int32, _vp, _vp]
 _lib.sqa_block_assign.restype = _i
 _lib.sqa_block_assign.argtypes = [_vp, _i, _i, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp, C.c_int32, _vp, _vp]
 _lib.sqa_slot_map.restype = _i
@@ -989,6 +996,15 @@ def q4_workspace(caches: Q4Caches, Hq: int, T: int, layer: int = 0) -> torch.Ten
     ws = torch.empty(need, dtype=torch.uint8, device=caches.K[0].device)
     _check(_lib.sqa_decode_workspace_init(_ptr(ws), need, _stream()), "sqa_decode_workspace_init")
     return ws
+
+
+def q4_plan(capacity: int, B: int, T: int, Hq: int, Hkv: int, D: int, dtype: str, new_pos: int = 0, ragged: bool = False) -> dict:
+    """sqa_q4_plan: how q4_attention would lay a chunk out (host arithmetic, no GPU).  dtype: "bf16" or "f32"; ragged: with prompt_len or
+    new_pos_seq."""
+    _check_position(new_pos, "sqa_q4_plan")
+    layer, opts, info = Q4CacheStruct(capacity=capacity), BatchOptsStruct(prompt_len=0x1000 if ragged else None), Q4PlanInfo()
+    _check(_lib.sqa_q4_plan(C.addressof(layer), {"f32": 0, "bf16": 1}[dtype], B, T, Hq, Hkv, D, new_pos, C.addressof(opts), C.addressof(info)), "sqa_q4_plan")
+    return {f: int(getattr(info, f)) for f, _ in Q4PlanInfo._fields_}
 
 
 def q4_attention(q: torch.Tensor, new_pos: int, caches: Q4Caches, layer: int = 0, out: Optional[torch.Tensor] = None,

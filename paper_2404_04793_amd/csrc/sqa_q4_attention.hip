@@ -17,11 +17,12 @@
 namespace sqa {
 
 constexpr int kQ4Slots = 32;                        // slots of a tile
+constexpr float kQ4FarLogit = 64.f;                 // in powers of two: below it the rounding is 2e-6 at most
 typedef __attribute__((address_space(1))) const uint8_t g_u8_t;
 typedef __attribute__((address_space(3))) v4u_t lds_v4u_t;
 
 constexpr int kQ4Splits = 64;                       // workgroups that share out a unit's slots: a lane each when they are joined
-constexpr int kQ4Records = 256 * 16;                // rows of sums that the workspace has room for: no more workgroups than 256 are joined
+constexpr int kQ4WideRows = 128;                    // rows of a unit from which on a workgroup may take 128 of them (bf16)
 
 struct Q4AttentionArgs {
   Q4Args a;
@@ -78,57 +79,106 @@ template <typename T, int D> struct Q4Tile {
   static __device__ __forceinline__ int swizzle(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 };
 
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_kernel(const Q4AttentionArgs a) {
-  using C = Q4Tile<T, D>;
-  constexpr int M = 16, NE = C::NE, NL = C::NL, NP = C::NP, NV = C::NV, KD = C::KD, PP = D / 4, REC = PP + 1, NT = 64 * NW;
-  extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // V tiles of the waves, at the end their sums; then the table
-  __shared__ float s_m[NW][M], s_l[NW][M];
-  __shared__ int s_word;
-  int* const s_table = reinterpret_cast<int*>(s_stage + NW * C::VB);
-  const sqa_q4_cache& L = a.a.L;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i = lane & 15, j = lane >> 4;
+// threadIdx.x anew: what is derived from it takes no registers from here back to its first use
+__device__ __forceinline__ int late_tid() {
+  int x = threadIdx.x;
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
-  // ---- where the work is
-  const uint32_t total = (uint32_t)(a.a.c.B * a.a.c.Hkv) * (uint32_t)(a.tiles * a.splits);
-  const uint32_t per8 = (total + 7) / 8, work = (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);
-  if (blockIdx.x >> 3 >= per8 || work >= total) return;
-  int split, tile, h, item, u, b;
-  divide((int)work, a.splits, a.splits_m, item, split);
-  divide(item, a.tiles, a.tiles_m, u, tile);
-  tile = a.tiles - 1 - tile;                        // (the longest first)
-  divide(u, a.a.c.Hkv, a.heads_m, b, h);
-  const int g = a.a.c.g;
-  Q4Seq s = q4_seq(a.a, b, tid == 0 && h == 0 && tile == 0 && split == 0);
-  s.n = scalar(s.n); s.slots = scalar(s.slots); s.why = scalar(s.why);
-  s.pos = (int64_t)scalar((int)s.pos);              // (positions are 32-bit numbers)
-  const int rows = s.n * g, row0 = tile * M;
-  if (row0 >= rows) return;
-  const int last_row = min(row0 + M, rows) - 1;
-  auto place = [&](int r, int& t, int& head) {
-    int x;
-    divide(r, g, a.group_m, t, x);
-    head = h * g + x;
-  };
-  int t_first, t_last, any;
-  place(row0, t_first, any);
-  place(last_row, t_last, any);
-  t_first = scalar(t_first); t_last = scalar(t_last);
-  const bool turned = s.end() > s.slots;
-  const int len = s.why ? 1 : s.len();
-  const int end = turned ? len : min((int)s.pos + t_last + 1, len);                      // slots that the rows see lie before it
-  const int whole = turned ? (s.n == 1 ? len : 0) : min((int)s.pos + t_first + 1, len);   // ... that all rows see
-  const int nt = (int)((uint32_t)(end + kQ4Slots - 1) / kQ4Slots);
-  int per = nt, parts = 1, rest;
-  if (a.splits > 1) {
-    divide(nt + a.splits - 1, a.splits, a.splits_m, per, rest);
-    parts = (int)((uint32_t)(nt + per - 1) / (uint32_t)per);
+// A barrier, and whether x is true in any thread (__syncthreads_or keeps the packed thread numbers in a register until its last use)
+template <int NT> __device__ __forceinline__ bool any_thread(bool x, int* s_flags /*[NT / 64]*/) {
+  s_flags[threadIdx.x >> 6] = __any(x);
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int k = 0; k < NT / 64; ++k) all |= s_flags[k];
+  return scalar(all) != 0;
+}
+
+// What a workgroup of NT threads works on: M rows of one unit and a run of its slots, in tiles of KT.
+template <typename T, int D, int NT, int M, int KT> struct Q4Work {
+  static constexpr int PP = D / 4, REC = PP + 1;    // 16-byte pieces of a row of sums; and its (m, l, bad)
+  Q4Seq s;
+  int item, split, u, b, h, g, row0, last_row, parts, tile0, tile1;
+  int len, end, whole;                              // slots that hold tokens, that the workgroup's rows see, that all of its rows see lie before them
+  int newest, fixed, ring;
+  bool turned;
+  uint32_t group_m;
+
+  // false: there is nothing to do.  (All of it the same in all lanes.)
+  __device__ __forceinline__ bool locate(const Q4AttentionArgs& a) {
+    const uint32_t total = (uint32_t)(a.a.c.B * a.a.c.Hkv) * (uint32_t)(a.tiles * a.splits);
+    const uint32_t per8 = (total + 7) / 8, work = (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);                // (one run of items per XCD, see xcd_item)
+    if (blockIdx.x >> 3 >= per8 || work >= total) return false;
+    int tile;
+    divide((int)work, a.splits, a.splits_m, item, split);
+    divide(item, a.tiles, a.tiles_m, u, tile);
+    tile = a.tiles - 1 - tile;                      // (the longest first)
+    divide(u, a.a.c.Hkv, a.heads_m, b, h);
+    g = a.a.c.g; group_m = a.group_m;
+    s = q4_seq(a.a, b, threadIdx.x == 0 && h == 0 && tile == 0 && split == 0);
+    s.n = scalar(s.n); s.slots = scalar(s.slots); s.why = scalar(s.why);
+    s.pos = (int64_t)scalar((int)s.pos);            // (positions are 32-bit numbers)
+    const int rows = s.n * g;
+    row0 = tile * M;
+    if (row0 >= rows) return false;
+    last_row = min(row0 + M, rows) - 1;
+    int t_first, t_last, any;
+    place(row0, t_first, any);
+    place(last_row, t_last, any);
+    t_first = scalar(t_first); t_last = scalar(t_last);
+    turned = s.end() > s.slots;
+    len = s.why ? 1 : s.len();
+    end = turned ? len : min((int)s.pos + t_last + 1, len);
+    whole = turned ? (s.n == 1 ? len : 0) : min((int)s.pos + t_first + 1, len);
+    newest = s.why ? 0 : scalar(s.slot(s.end() - 1));
+    fixed = turned ? s.sink : 0; ring = turned ? s.slots - s.sink : 0;
+    const int nt = (int)((uint32_t)(end + KT - 1) / KT);
+    int per = nt, rest;
+    parts = 1;
+    if (a.splits > 1) {
+      divide(nt + a.splits - 1, a.splits, a.splits_m, per, rest);
+      per = scalar(per);
+      parts = scalar((int)((uint32_t)(nt + per - 1) / (uint32_t)per));
+    }
+    tile0 = scalar(split * per); tile1 = scalar(min(tile0 + per, nt));
+    len = scalar(len); end = scalar(end); whole = scalar(whole); fixed = scalar(fixed); ring = scalar(ring);
+    if (split >= parts) return false;
+    if (s.why) {
+      if (split == 0) refuse(a, s.why);
+      return false;
+    }
+    return true;
   }
-  const int tile0 = split * per, tile1 = min(tile0 + per, nt);
-  if (split >= parts) return;
-
-  auto refuse = [&](int why) {
+  __device__ __forceinline__ void place(int r, int& t, int& head) const {
+    int x;
+    divide(r, g, group_m, t, x);
+    head = h * g + x;
+  }
+  // Does a row whose token is `back` tokens before the newest see a slot?  The newest lies at `newest`, the others of the ring before it.
+  // (Without branches: where a value was set to -inf behind && and || some lanes have been seen to keep theirs.)
+  __device__ __forceinline__ bool sees(int slot, int back) const {
+    int behind = newest - slot;
+    behind += behind < 0 ? ring : 0;
+    return (bool)((int)(slot < len) & ((int)(slot < fixed) | (int)(behind >= back)));
+  }
+  // block numbers of this workgroup's slots to LDS; does one of them lie outside the pools?
+  __device__ __forceinline__ bool stage_blocks(const sqa_q4_cache& L, int* s_table, int* s_flags) const {
+    if (!L.block_table) return false;
+    constexpr int BPT = KT / SQA_BLOCK_SLOTS;
+    const int32_t* table = L.block_table + (int64_t)u * L.blocks_per_unit;
+    bool bad = false;
+    for (int x = threadIdx.x; x < BPT * (tile1 - tile0); x += NT) {
+      const int e = BPT * tile0 + x;
+      int blk = e * SQA_BLOCK_SLOTS < end ? table[e] : 0;
+      if ((unsigned)blk >= (unsigned)L.n_blocks) { bad = true; blk = 0; }
+      s_table[x] = blk;
+    }
+    return any_thread<NT>(bad, s_flags);
+  }
+  __device__ __forceinline__ void refuse(const Q4AttentionArgs& a, int why) const {
+    const int tid = threadIdx.x;
     if (tid == 0 && a.a.c.status) *a.a.c.status = why;
     constexpr int E = 16 / (int)sizeof(T), PPR = D / E;
     for (int x = tid; x < (last_row + 1 - row0) * PPR; x += NT) {
@@ -137,28 +187,181 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
       st16(static_cast<T*>(a.out) + (((int64_t)b * a.a.c.T + t) * a.a.c.Hq + head) * D + x % PPR * E, make_uint4(0, 0, 0, 0));
       if (a.lse && x % PPR == 0) a.lse[((int64_t)b * a.a.c.Hq + head) * a.a.c.T + t] = -INFINITY;
     }
-  };
-  if (s.why) {
-    if (split == 0) refuse(s.why);
-    return;
+  }
+  // pieces 2 p and 2 p + 1 of a row of sums
+  __device__ __forceinline__ void store8(const Q4AttentionArgs& a, int row, int p, const float4 (&v)[2], float mm, float ll) const {
+    int t, head;
+    place(row0 + row, t, head);
+    const float inv = 1.f / ll;
+    T* dst = static_cast<T*>(a.out) + (((int64_t)b * a.a.c.T + t) * a.a.c.Hq + head) * D + 8 * p;
+    if constexpr (sizeof(T) == 2)
+      st16(dst, make_uint4(pair(v[0].x * inv, v[0].y * inv), pair(v[0].z * inv, v[0].w * inv), pair(v[1].x * inv, v[1].y * inv), pair(v[1].z * inv, v[1].w * inv)));
+    else
+#pragma unroll
+      for (int k = 0; k < 2; ++k) reinterpret_cast<float4*>(dst)[k] = make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv);
+    if (p == 0 && a.lse) a.lse[((int64_t)b * a.a.c.Hq + head) * a.a.c.T + t] = 0.6931471805599453f * fmaf(mm, a.scale, log2f(ll));
   }
 
+  // The sums of KW waves for each row (in s_stage, [KW][M] rows of pieces, piece p of row r at place p ^ (r & 15); references and sums in s_m and
+  // s_l) joined, those of the workgroups of the same rows too, and stored.
+  template <int KW>
+  __device__ __forceinline__ void finish(const Q4AttentionArgs& a, char* s_stage, float (*s_m)[M], float (*s_l)[M], int* s_word, int* s_flags, bool bad) const {
+    const int tid = late_tid(), lane = tid & 63, wave = tid >> 6;
+    auto joined = [&](int row, float& mm, float& ll) {
+      mm = s_m[0][row];
+#pragma unroll 2
+      for (int w = 1; w < KW; ++w) mm = fmaxf(mm, s_m[w][row]);
+      ll = 0.f;
+#pragma unroll 2
+      for (int w = 0; w < KW; ++w) ll += s_l[w][row] * exp2_fast((s_m[w][row] - mm) * a.scale);
+    };
+    auto piece4 = [&](int row, int p) {
+      float4 v = reinterpret_cast<const float4*>(s_stage)[row * PP + (p ^ (row & 15))];
+#pragma unroll 2
+      for (int w = 1; w < KW; ++w) {
+        const float4 x = reinterpret_cast<const float4*>(s_stage)[(w * M + row) * PP + (p ^ (row & 15))];
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+      }
+      return v;
+    };
+    const int live = (last_row + 1 - row0) * (PP / 2);
+    if (parts == 1) {
+      if (bad) { refuse(a, SQA_ERR_SHAPE); return; }
+      for (int x = tid; x < live; x += NT) {
+        const int row = x / (PP / 2), p = x % (PP / 2);
+        float mm, ll;
+        joined(row, mm, ll);
+        const float4 v[2] = {piece4(row, 2 * p), piece4(row, 2 * p + 1)};
+        store8(a, row, p, v, mm, ll);
+      }
+      return;
+    }
+    const char* const base = uniform(reinterpret_cast<const char*>(a.part + (int64_t)item * a.splits * (M * REC)));
+    const HandOver rec(reinterpret_cast<float4*>(const_cast<char*>(base)), (uint32_t)(a.splits * (M * REC * 16)));
+    const uint32_t refs = (uint32_t)(a.splits * M * PP);                                   // all rows' sums, then all rows' (m, l, bad)
+    for (int x = tid; x < 2 * live; x += NT) rec.put((uint32_t)(split * M * PP + x), piece4(x / PP, x % PP));
+    for (int row = tid; row <= last_row - row0; row += NT) {
+      float mm, ll;
+      joined(row, mm, ll);
+      rec.put(refs + split * M + row, make_float4(mm, ll, bad ? 1.f : 0.f, 0.f));
+    }
+    if (!last_to_arrive(a.count + item, parts, s_word)) return;
+    // ---- all workgroups' sums.  Few records: a thread asks for all that it needs at once.
+    if (parts <= 4) {
+      bad = false;
+      for (int x = tid; x < live; x += NT) {
+        const int row = x / (PP / 2), p = x % (PP / 2);
+        float4 ml[4], w4[4][2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t from = (uint32_t)(min(k, parts - 1) * M + row);
+          ml[k] = rec.get(refs + from); w4[k][0] = rec.get(from * PP + 2 * p); w4[k][1] = rec.get(from * PP + 2 * p + 1);
+        }
+        float mm = ml[0].x, ll = 0.f;
+#pragma unroll
+        for (int k = 1; k < 4; ++k) mm = fmaxf(mm, ml[k].x);
+        float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (k >= parts) break;
+          const float w = exp2_fast((ml[k].x - mm) * a.scale);
+          ll = fmaf(w, ml[k].y, ll);
+          bad |= ml[k].z != 0.f;
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
+        }
+        if (bad) break;
+        store8(a, row, p, v, mm, ll);
+      }
+      if (any_thread<NT>(bad, s_flags)) refuse(a, SQA_ERR_SHAPE);
+      return;
+    }
+    // Many: each one's weight per row first, then the weighted pieces, the records shared out among groups of threads.
+    float* const s_weight = reinterpret_cast<float*>(s_stage);                             // [parts][M], then the groups' sums
+    const int live_rows = last_row + 1 - row0;
+    bad = false;
+    for (int row = wave; row < live_rows; row += NT / 64) {                                     // a lane per record (there are 64 at most)
+      const float4 ml = rec.get(refs + (uint32_t)(min(lane, parts - 1) * M + row));
+      const bool there = lane < parts;
+      bad |= there && ml.z != 0.f;
+      float mm = there ? ml.x : -FLT_MAX;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o, SQA_WAVE));
+      const float w = exp2_fast((ml.x - mm) * a.scale);
+      const float ll = wave_sum(there ? w * ml.y : 0.f);
+      if (there) s_weight[lane * M + row] = w;
+      if (lane == 0) { s_m[0][row] = mm; s_l[0][row] = ll; }
+    }
+    if (any_thread<NT>(bad, s_flags)) { refuse(a, SQA_ERR_SHAPE); return; }
+    int groups = 1;
+    while (groups * 2 * live <= NT && groups < parts) groups *= 2;
+    float4* const s_sum = reinterpret_cast<float4*>(s_stage + kQ4Splits * M * 4);
+    const int per_group = groups * live;
+    for (int x0 = 0; x0 < live; x0 += NT) {            // (once, but for more pieces than threads: one group then)
+      const int x = x0 + tid % (groups > 1 ? live : NT), grp = groups > 1 ? tid / live : 0;
+      if (x >= live || (groups > 1 && tid >= per_group)) { if (groups == 1) continue; else break; }
+      const int row = x / (PP / 2), p = x % (PP / 2);
+      float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+      for (int k0 = grp; k0 < parts; k0 += 8 * groups) {
+        float4 w4[8][2];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t from = (uint32_t)(min(k0 + k * groups, parts - 1) * M + row) * PP + 2 * p;
+          w4[k][0] = rec.get(from); w4[k][1] = rec.get(from + 1);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k0 + k * groups < parts) {
+            const float w = s_weight[(k0 + k * groups) * M + row];
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
+          }
+      }
+      if (groups == 1) store8(a, row, p, v, s_m[0][row], s_l[0][row]);
+      else { s_sum[2 * (grp * live + x)] = v[0]; s_sum[2 * (grp * live + x) + 1] = v[1]; }
+    }
+    if (groups == 1) return;
+    __syncthreads();
+    if (tid < live) {
+      const int row = tid / (PP / 2), p = tid % (PP / 2);
+      float4 v[2] = {s_sum[2 * tid], s_sum[2 * tid + 1]};
+      for (int k = 1; k < groups; ++k)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const float4 x = s_sum[2 * (k * live + tid) + y];
+          v[y].x += x.x; v[y].y += x.y; v[y].z += x.z; v[y].w += x.w;
+        }
+      store8(a, row, p, v, s_m[0][row], s_l[0][row]);
+    }
+  }
+};
+
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_kernel(const Q4AttentionArgs a) {
+  using C = Q4Tile<T, D>;
+  constexpr int M = 16, NE = C::NE, NL = C::NL, NP = C::NP, NV = C::NV, KD = C::KD, PP = D / 4, NT = 64 * NW;
+  extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // V tiles of the waves, at the end their sums; then the table
+  __shared__ float s_m[NW][M], s_l[NW][M];
+  __shared__ int s_word, s_flags[NW];
+  int* const s_table = reinterpret_cast<int*>(s_stage + NW * C::VB);
+  const sqa_q4_cache& L = a.a.L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int i = lane & 15, j = lane >> 4;
+
+  Q4Work<T, D, NT, M, kQ4Slots> w;
+  if (!w.locate(a)) return;
+  const int tile0 = w.tile0, tile1 = w.tile1, end = w.end;
   // ---- this lane's query row
   int t, head;
-  place(min(row0 + i, last_row), t, head);
-  const int back = s.n - 1 - t;                     // a slot of the ring is seen when its token is at least so far behind the newest
-  const int newest = s.slot(s.end() - 1);           // ... and it lies here
-  const int fixed = turned ? s.sink : 0, ring = turned ? s.slots - s.sink : 0;
-  // (without branches: they are not faster, and where a value was set to -inf behind && and || some lanes have been seen to keep theirs)
-  auto sees = [&](int slot) {
-    int behind = newest - slot;
-    behind += behind < 0 ? ring : 0;
-    return (bool)((int)(slot < len) & ((int)(slot < fixed) | (int)(behind >= back)));
-  };
+  w.place(min(w.row0 + i, w.last_row), t, head);
+  const int back = w.s.n - 1 - t;                   // tokens of the chunk behind it
   // its elements 8 KD j .. of step x: 8 (KD j + x) ..
   uint4 qp[NP][KD];
   {
-    const T* src = static_cast<const T*>(a.q) + (((int64_t)b * a.a.c.Hq + head) * a.a.c.T + t) * D + 8 * KD * j;
+    const T* src = static_cast<const T*>(a.q) + (((int64_t)w.b * a.a.c.Hq + head) * a.a.c.T + t) * D + 8 * KD * j;
 #pragma unroll
     for (int x = 0; x < KD; ++x) {
       if constexpr (sizeof(T) == 2) qp[0][x] = ld16(src + 8 * x);
@@ -174,20 +377,9 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
     }
   }
 
-  // ---- block numbers of this workgroup's slots
-  int bad = 0;
-  if (L.block_table) {
-    const int32_t* table = L.block_table + (int64_t)u * L.blocks_per_unit;
-    for (int x = tid; x < 2 * (tile1 - tile0); x += NT) {
-      const int e = 2 * tile0 + x;
-      int blk = e * SQA_BLOCK_SLOTS < end ? table[e] : 0;
-      if ((unsigned)blk >= (unsigned)L.n_blocks) { bad = 1; blk = 0; }
-      s_table[x] = blk;
-    }
-    bad = __syncthreads_or(bad);
-  }
+  const bool bad = w.stage_blocks(L, s_table, s_flags);
   // ---- rows of 16 neighbouring slots lie one after the other; slots behind the last one are read as that one again
-  const int64_t unit_row = (int64_t)u * L.capacity;
+  const int64_t unit_row = (int64_t)w.u * L.capacity;
   auto row_of = [&](int slot) {                     // (the same in all lanes)
     return L.block_table ? (int64_t)__builtin_amdgcn_readfirstlane(s_table[slot / SQA_BLOCK_SLOTS - 2 * tile0]) * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS
                          : unit_row + slot;
@@ -263,7 +455,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
     }
     fetch_keys(ahead, now);               // (into registers that have just been used)
     // ---- V to LDS as bf16
-    const bool edge = (tl + 1) * kQ4Slots > whole;
+    const bool edge = (tl + 1) * kQ4Slots > w.whole;
     uint64_t odd[NL] = {};                          // (lanes whose group is not finite, where not every row sees it)
 #pragma unroll
     for (int y = 0; y < NL; ++y) {
@@ -287,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          sc[kb][r] = sees(tl * kQ4Slots + 16 * kb + 4 * j + r) ? sc[kb][r] : -INFINITY;
+          sc[kb][r] = w.sees(tl * kQ4Slots + 16 * kb + 4 * j + r, back) ? sc[kb][r] : -INFINITY;
     }
     float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
     if (__any(top > m + a.near)) {                  // the reference of a row moves when one of its logits is 2^8 times beyond it
@@ -335,7 +527,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
         const int from = __builtin_ctzll(odd[y]);
         odd[y] &= odd[y] - 1;
         const int slot = tl * kQ4Slots + (D == 128 ? 16 * y + (from >> 2) : from >> 1), group = D == 128 ? from & 3 : from & 1;
-        const float add = sees(slot) ? NAN : 0.f;
+        const float add = w.sees(slot, back) ? NAN : 0.f;
 #pragma unroll
         for (int e = 0; e < NE; ++e) o[e] += e / 2 == group ? add : 0.f;
       }
@@ -354,180 +546,257 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
 #pragma unroll
   for (int e = 0; e < NE; ++e) mine[(4 * e + j) ^ i] = make_float4(o[e][0] * keep, o[e][1] * keep, o[e][2] * keep, o[e][3] * keep);
   __syncthreads();
-  auto joined = [&](int row, float& mm, float& ll) {
-    mm = s_m[0][row];
-#pragma unroll 2
-    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, s_m[w][row]);
-    ll = 0.f;
-#pragma unroll 2
-    for (int w = 0; w < NW; ++w) ll += s_l[w][row] * exp2_fast((s_m[w][row] - mm) * a.scale);
-  };
-  auto piece4 = [&](int row, int p) {
-    float4 v = reinterpret_cast<const float4*>(s_stage)[row * PP + (p ^ row)];
-#pragma unroll 2
-    for (int w = 1; w < NW; ++w) {
-      const float4 x = reinterpret_cast<const float4*>(s_stage)[(w * M + row) * PP + (p ^ row)];
-      v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-    }
-    return v;
-  };
-  auto store8 = [&](int row, int p, const float4 (&v)[2], float mm, float ll) {          // pieces 2 p and 2 p + 1
-    int tt, hh;
-    place(row0 + row, tt, hh);
-    const float inv = 1.f / ll;
-    T* dst = static_cast<T*>(a.out) + (((int64_t)b * a.a.c.T + tt) * a.a.c.Hq + hh) * D + 8 * p;
-    if constexpr (sizeof(T) == 2)
-      st16(dst, make_uint4(pair(v[0].x * inv, v[0].y * inv), pair(v[0].z * inv, v[0].w * inv), pair(v[1].x * inv, v[1].y * inv), pair(v[1].z * inv, v[1].w * inv)));
-    else
-#pragma unroll
-      for (int k = 0; k < 2; ++k) reinterpret_cast<float4*>(dst)[k] = make_float4(v[k].x * inv, v[k].y * inv, v[k].z * inv, v[k].w * inv);
-    if (p == 0 && a.lse) a.lse[((int64_t)b * a.a.c.Hq + hh) * a.a.c.T + tt] = 0.6931471805599453f * fmaf(mm, a.scale, log2f(ll));
-  };
-  const int live = (last_row + 1 - row0) * (PP / 2);
-  if (parts == 1) {
-    if (bad) { refuse(SQA_ERR_SHAPE); return; }
-    for (int x = tid; x < live; x += NT) {
-      const int row = x / (PP / 2), p = x % (PP / 2);
-      float mm, ll;
-      joined(row, mm, ll);
-      const float4 v[2] = {piece4(row, 2 * p), piece4(row, 2 * p + 1)};
-      store8(row, p, v, mm, ll);
-    }
-    return;
-  }
-  const char* const base = uniform(reinterpret_cast<const char*>(a.part + (int64_t)item * a.splits * (M * REC)));
-  const HandOver rec(reinterpret_cast<float4*>(const_cast<char*>(base)), (uint32_t)(a.splits * (M * REC * 16)));
-  const uint32_t refs = (uint32_t)(a.splits * M * PP);                                   // all rows' sums, then all rows' (m, l, bad)
-  for (int x = tid; x < 2 * live; x += NT) rec.put((uint32_t)(split * M * PP + x), piece4(x / PP, x % PP));
-  for (int row = tid; row <= last_row - row0; row += NT) {
-    float mm, ll;
-    joined(row, mm, ll);
-    rec.put(refs + split * M + row, make_float4(mm, ll, (float)bad, 0.f));
-  }
-  if (!last_to_arrive(a.count + item, parts, &s_word)) return;
-  // ---- all workgroups' sums.  Few records: a thread asks for all that it needs at once.
-  if (parts <= 8) {
-    bad = 0;
-    for (int x = tid; x < live; x += NT) {
-      const int row = x / (PP / 2), p = x % (PP / 2);
-      float4 ml[8], w4[8][2];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t from = (uint32_t)(min(k, parts - 1) * M + row);
-        ml[k] = rec.get(refs + from); w4[k][0] = rec.get(from * PP + 2 * p); w4[k][1] = rec.get(from * PP + 2 * p + 1);
-      }
-      float mm = ml[0].x, ll = 0.f;
-#pragma unroll
-      for (int k = 1; k < 8; ++k) mm = fmaxf(mm, ml[k].x);
-      float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (k >= parts) break;
-        const float w = exp2_fast((ml[k].x - mm) * a.scale);
-        ll = fmaf(w, ml[k].y, ll);
-        bad |= ml[k].z != 0.f;
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
-      }
-      if (bad) break;
-      store8(row, p, v, mm, ll);
-    }
-    if (__syncthreads_or(bad)) refuse(SQA_ERR_SHAPE);
-    return;
-  }
-  // Many: each one's weight per row first, then the weighted pieces, the records shared out among groups of threads.
-  float* const s_weight = reinterpret_cast<float*>(s_stage);                             // [parts][M], then the groups' sums
-  const int live_rows = last_row + 1 - row0;
-  bad = 0;
-  for (int row = wave; row < live_rows; row += NW) {                                     // a lane per record (there are 64 at most)
-    const float4 ml = rec.get(refs + (uint32_t)(min(lane, parts - 1) * M + row));
-    const bool there = lane < parts;
-    bad |= there && ml.z != 0.f;
-    float mm = there ? ml.x : -FLT_MAX;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o, SQA_WAVE));
-    const float w = exp2_fast((ml.x - mm) * a.scale);
-    const float ll = wave_sum(there ? w * ml.y : 0.f);
-    if (there) s_weight[lane * M + row] = w;
-    if (lane == 0) { s_m[0][row] = mm; s_l[0][row] = ll; }
-  }
-  if (__syncthreads_or(bad)) { refuse(SQA_ERR_SHAPE); return; }
-  int groups = 1;
-  while (groups * 2 * live <= NT && groups < parts) groups *= 2;
-  float4* const s_sum = reinterpret_cast<float4*>(s_stage + kQ4Splits * M * 4);
-  const int per_group = groups * live;
-  for (int x0 = 0; x0 < live; x0 += NT) {            // (once, but for more pieces than threads: one group then)
-    const int x = x0 + tid % (groups > 1 ? live : NT), grp = groups > 1 ? tid / live : 0;
-    if (x >= live || (groups > 1 && tid >= per_group)) { if (groups == 1) continue; else break; }
-    const int row = x / (PP / 2), p = x % (PP / 2);
-    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 1
-    for (int k0 = grp; k0 < parts; k0 += 8 * groups) {
-      float4 w4[8][2];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t from = (uint32_t)(min(k0 + k * groups, parts - 1) * M + row) * PP + 2 * p;
-        w4[k][0] = rec.get(from); w4[k][1] = rec.get(from + 1);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k0 + k * groups < parts) {
-          const float w = s_weight[(k0 + k * groups) * M + row];
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-            v[y] = make_float4(fmaf(w4[k][y].x, w, v[y].x), fmaf(w4[k][y].y, w, v[y].y), fmaf(w4[k][y].z, w, v[y].z), fmaf(w4[k][y].w, w, v[y].w));
-        }
-    }
-    if (groups == 1) store8(row, p, v, s_m[0][row], s_l[0][row]);
-    else { s_sum[2 * (grp * live + x)] = v[0]; s_sum[2 * (grp * live + x) + 1] = v[1]; }
-  }
-  if (groups == 1) return;
-  __syncthreads();
-  if (tid < live) {
-    const int row = tid / (PP / 2), p = tid % (PP / 2);
-    float4 v[2] = {s_sum[2 * tid], s_sum[2 * tid + 1]};
-    for (int k = 1; k < groups; ++k)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const float4 x = s_sum[2 * (k * live + tid) + y];
-        v[y].x += x.x; v[y].y += x.y; v[y].z += x.z; v[y].w += x.w;
-      }
-    store8(row, p, v, s_m[0][row], s_l[0][row]);
-  }
+  w.template finish<NW>(a, s_stage, s_m, s_l, &s_word, s_flags, bad);
 }
 
-struct Q4Plan { int waves, tiles, splits; };         // waves of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
-static Q4Plan q4_plan(int B, int T, int Hq, int Hkv, int32_t new_pos, int32_t capacity, bool uniform) {
+// The same for many rows in bf16: 128 rows and tiles of 64 slots, two workgroups per CU.  A tile is opened once for all four waves: K and V of the
+// next ones are on their way in 4 bits in registers (16 bytes of each a thread) and go to LDS as bf16 between a tile's products and
+// the barrier.  V^T.P^T of a tile follows K.Q^T of the next one.  Probabilities are rounded to one bf16, as in sqa_chunk_attention's form for many
+// rows: the products bound these calls.
+template <int D> struct Q4Wide {
+  using R = TileRows<bf16_t, D>;
+  static constexpr int Slots = 64, Rows = 128, TILE = Slots * R::RB;
+  static constexpr int STAGE = 4 * TILE > Rows * D * 4 + 8192 ? 4 * TILE : Rows * D * 4 + 8192;            // K, K', V, V'; at the end all rows' sums
+  // piece p of row r of V lies at place p ^ v_swizzle(r): 64 bytes of each of 4 rows are read at a time, 8 lanes write 2 or 4 rows
+  static __device__ __forceinline__ int v_swizzle(int r) { return R::PPR == 8 ? 4 * ((r >> 1) & 1) : 5 * (r & 3); }
+};
+
+template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_kernel(const Q4AttentionArgs a) {
+  using T = bf16_t;
+  using C = Q4Wide<D>;
+  using R = TileRows<T, D>;
+  constexpr int NB = D / 32, NS = Frag<T, D>::NS, TILE = C::TILE, KT = C::Slots, GPR = D / kGroup, KD = D / 32;
+  extern __shared__ __attribute__((aligned(1024))) char s_stage[];
+  __shared__ float s_m[1][C::Rows], s_l[1][C::Rows];
+  __shared__ __attribute__((aligned(16))) uint8_t s_odd[2][256];                         // of a tile of V: is a thread's part not finite, and left out?
+  __shared__ int s_word, s_flags[4];
+  int* const s_table = reinterpret_cast<int*>(s_stage + C::STAGE);
+  Q4Work<T, D, 256, C::Rows, KT> w;
+  if (!w.locate(a)) return;
+  const sqa_q4_cache& L = a.a.L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = scalar(tid >> 6), col = lane & 31, half = lane >> 5;
+
+  // ---- this lane's query row
+  int t, head;
+  w.place(min(w.row0 + 32 * wave + col, w.last_row), t, head);
+  const int back = w.s.n - 1 - t;
+  Frag<T, D> q;
+  {
+    const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (((int64_t)w.b * a.a.c.Hq + head) * a.a.c.T + t) * D);
+#pragma unroll
+    for (int x = 0; x < NS; ++x) q.p[x] = ld16(src + (2 * x + half) * 16);
+  }
+  const bool bad = w.stage_blocks(L, s_table, s_flags);
+
+  // ---- a thread's part of a tile: 8 KD numbers of row tid / 4
+  const int row = tid >> 2, part = tid & 3;
+  const int64_t unit_row = (int64_t)w.u * L.capacity;
+  auto row_of = [&](int j) {                        // (slots behind the last one: that one again)
+    const int slot = min((w.tile0 + j) * KT + row, w.end - 1);
+    return L.block_table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS - KT / SQA_BLOCK_SLOTS * w.tile0] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit_row + slot;
+  };
+  struct Codes { uint32_t c[KD], power; };
+  auto fetch = [&](const void* codes, const uint8_t* powers, int64_t at) {
+    Codes x;
+    const char* from = static_cast<const char*>(codes) + at * (D / 2) + 4 * KD * part;
+    if constexpr (KD == 4) { const uint4 v = ld16(from); x.c[0] = v.x; x.c[1] = v.y; x.c[2] = v.z; x.c[3] = v.w; }
+    else { const v2u_t v = *(const g_v2u_t*)from; x.c[0] = v.x; x.c[1] = v.y; }
+    x.power = *(const g_u8_t*)(powers + at * GPR + KD * part / 4);
+    return x;
+  };
+  const uint32_t lds0 = lds_at(s_stage);
+  auto put = [&](const Codes& x, uint32_t tile, int swizzle) {
+    const float power = __uint_as_float(x.power << 23);
+#pragma unroll
+    for (int p = 0; p < KD; ++p)
+      *(lds_v4u_t*)(uintptr_t)(lds0 + tile + row * R::RB + (((KD * part + p) ^ swizzle) << 4)) = __builtin_bit_cast(v4u_t, q4_open(x.c[p], power));
+  };
+  auto is_edge = [&](int j) { return (w.tile0 + j + 1) * KT > w.whole; };                // not all rows of the workgroup see all of the tile
+  auto put_keys = [&](const Codes& x, int j) { put(x, (j & 1) * TILE, R::k_swizzle(row)); };
+  auto put_values = [&](Codes x, int j) {
+    if (is_edge(j)) {                               // a slot that a row does not see has probability 0, but 0 x NaN is NaN: see values()
+      const bool odd = x.power > 252u;
+      s_odd[j & 1][tid] = odd;
+#pragma unroll
+      for (int p = 0; p < KD; ++p) x.c[p] = odd ? 0u : x.c[p];
+      x.power = odd ? 127u : x.power;
+    }
+    put(x, (2 + (j & 1)) * TILE, C::v_swizzle(row));
+  };
+
+  // ---- the lane's places in a tile of K and of V
+  int k_at[NS], v_at[NB];
+#pragma unroll
+  for (int x = 0; x < NS; ++x) k_at[x] = col * R::RB + (((2 * x + half) ^ R::k_swizzle(col)) << 4);
+  {
+    const int r = 4 * half + (lane & 15) / 4;
+#pragma unroll
+    for (int e = 0; e < NB; ++e) v_at[e] = r * R::RB + (((4 * e + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::v_swizzle(r)) << 4) + (lane & 1) * 8;
+  }
+
+  f32x16_t o[NB], sc[2];
+  bf16x8_t p[4];
+#pragma unroll
+  for (int e = 0; e < NB; ++e) o[e] = f32x16_t{};
+  float m = -FLT_MAX, l = 0.f;                       // m: a reference that a row's largest logit is near, not always that logit
+
+  auto keys = [&](int j) {                           // sc = K.Q^T of tile j
+    const char* const Kt = s_stage + (j & 1) * TILE;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      uint4 k[NS];
+#pragma unroll
+      for (int x = 0; x < NS; ++x) k[x] = *reinterpret_cast<const uint4*>(Kt + k_at[x] + 32 * kb * R::RB);
+      sc[kb] = f32x16_t{};
+#pragma unroll
+      for (int x = 0; x < NS; ++x) mma_piece<T>(k[x], q.p[x], sc[kb]);
+    }
+  };
+  auto values = [&](int j) {                         // o += V^T.P^T of tile j
+    const char* const Vt = s_stage + (2 + (j & 1)) * TILE;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int e = 0; e < NB; ++e) {
+        const char* at = Vt + v_at[e] + 16 * ks * R::RB;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * R::RB));
+        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[ks], o[e], 0, 0, 0);
+      }
+    if (is_edge(j)) {                               // the groups that are not finite, to the rows that see them
+      uint64_t odd = __ballot(reinterpret_cast<const uint32_t*>(s_odd[j & 1])[lane] != 0);            // (a lane per slot)
+      while (odd) {
+        const int r = __builtin_ctzll(odd);
+        odd &= odd - 1;
+        const float add = w.sees((w.tile0 + j) * KT + r, back) ? NAN : 0.f;
+#pragma unroll
+        for (int e = 0; e < NB; ++e)
+          if (s_odd[j & 1][4 * r + 4 / KD * e]) o[e] += add;
+      }
+    }
+  };
+  auto softmax = [&](int j) {
+    if (is_edge(j)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[kb][i] = w.sees((w.tile0 + j) * KT + 32 * kb + c_row(i, half), back) ? sc[kb][i] : -INFINITY;
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kb][i]);
+    top = other_half_max(top);
+    // the reference of a row moves when one of its logits is 2^8 times beyond it: seldom after the first tiles
+    if (const bool beyond = top > m + a.near; __any(beyond)) {
+      const float to = beyond ? top : m, keep = exp2_fast((m - to) * a.scale);
+      m = to;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < NB; ++e) o[e] *= keep;
+    }
+    float off = m * a.scale;
+    // s scale - off in one operation is off by the rounding of `off`: far from 0 the difference is taken first, each row for itself
+    if (const bool far = fabsf(off) > kQ4FarLogit; __any(far)) {
+      const float from = far ? m : 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) sc[kb] -= from;
+      off = far ? 0.f : off;
+    }
+    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = exp2_fast(fmaf(sc[kb][i], a.scale, -off)), y = exp2_fast(fmaf(sc[kb][i + 1], a.scale, -off));
+        l0 += x; l1 += y;
+        p[2 * kb + i / 8][i % 8] = (__bf16)x; p[2 * kb + i / 8][i % 8 + 1] = (__bf16)y;
+      }
+    l += l0 + l1;
+  };
+
+  const int n = w.tile1 - w.tile0;
+  Codes kc, vc;
+  {
+    const int64_t at = row_of(0);
+    put_keys(fetch(L.K, L.K_scale, at), 0);
+    vc = fetch(L.V, L.V_scale, at);
+    kc = fetch(L.K, L.K_scale, row_of(min(1, n - 1)));
+  }
+  __syncthreads();
+  for (int j = 0; j < n; ++j) {
+    __builtin_amdgcn_s_setprio(1);                   // the wave that has products to give goes first
+    keys(j);
+    if (j > 0) values(j - 1);
+    __builtin_amdgcn_s_setprio(0);
+    softmax(j);
+    put_keys(kc, j + 1);
+    put_values(vc, j);
+    kc = fetch(L.K, L.K_scale, row_of(min(j + 2, n - 1)));           // (the last one again where there are no more)
+    vc = fetch(L.V, L.V_scale, row_of(min(j + 1, n - 1)));
+    __syncthreads();
+  }
+  values(n - 1);
+  __syncthreads();
+
+  // ---- sums to LDS as rows
+  l = other_half_sum(l);
+  if (half == 0) { s_m[0][32 * wave + col] = m; s_l[0][32 * wave + col] = l; }
+  float4* const mine = reinterpret_cast<float4*>(s_stage) + (32 * wave + col) * (D / 4);
+#pragma unroll
+  for (int e = 0; e < NB; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) mine[(8 * e + c_row(i, half) / 4) ^ (col & 15)] = make_float4(o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]);
+  __syncthreads();
+  w.template finish<1>(a, s_stage, s_m, s_l, &s_word, s_flags, bad);
+}
+
+struct Q4Plan { int waves, rows, tiles, splits; };   // waves and rows of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
+static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_pos, int32_t capacity, bool uniform) {
   Q4Plan p;
-  const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity;
-  p.tiles = (T * (Hq / Hkv) + 15) / 16;
-  const int64_t items = (int64_t)B * Hkv * p.tiles;
-  // A join through the workspace costs 5 us, one inside a workgroup 1: units are shared out among waves before workgroups, and among these
-  // only until every CU has one.  (256 units of 1000 slots: 8 waves 12.2 us, 4 with 3 workgroups a unit 14.0; 8 units of 30000: 32
-  // workgroups of 8 waves each 19.2, 64 22.8, 64 of 4 waves 24.6; 512 units of 1000: 4 waves 18.7, 8 20.0; 2048 of 571: 2 waves 31.2, 4 36.5, 8 44.)
-  p.waves = items >= 1024 ? 2 : (items >= 512 ? 4 : 8);
-  int64_t s = 256 / items;
-  s = std::min(s, slots / 256);                     // (8 tiles at least: a wave each)
+  const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity, rows = (int64_t)T * (Hq / Hkv);
+  const int64_t units = (int64_t)B * Hkv, wide = units * ((rows + 127) / 128);
+  int64_t s;
+  // 128 rows a workgroup where they fill the chip, or nearly do over many slots (a join of 128 rows costs what some hundred slots do).  32 heads over
+  // 8, us with 16 and with 128 rows: 8 x 128 tokens after 2000 (256 workgroups) 76 and 52, 8 x 64 45 and 38, 8 x 32 26 and 31; 16 x 64 after 500 28
+  // and 22, 16 x 32 17 and 21; 1 x 256 after 4000 45 and 42, 1 x 128 28 and 56; 1 x 128 after 30000 144 and 117, 1 x 64 80 and 98.
+  if (dt == SQA_BF16 && rows >= kQ4WideRows && (wide >= 256 || (wide >= 32 && wide * slots >= 250000))) {
+    p.rows = 128; p.waves = 4;
+    p.tiles = (int)((rows + 127) / 128);
+    s = std::min(512 / wide, slots / 1024);         // (two workgroups per CU; 64 of them over 4256 slots: 4 a unit 42 us, 8 67)
+  } else {
+    p.rows = 16;
+    p.tiles = (int)((rows + 15) / 16);
+    const int64_t items = units * p.tiles;
+    // A join through the workspace costs 5 us, one inside a workgroup 1: units are shared out among waves before workgroups, and among these
+    // only until every CU has one.  (256 units of 1000 slots: 8 waves 12.2 us, 4 with 3 workgroups a unit 14.0; 8 units of 30000: 32
+    // workgroups of 8 waves each 19.2, 64 22.8, 64 of 4 waves 24.6; 512 units of 1000: 4 waves 18.7, 8 20.0; 2048 of 571: 2 waves 31.2, 4 36.5, 8 44.)
+    p.waves = items >= 1024 ? 2 : (items >= 512 ? 4 : 8);
+    s = std::min(256 / items, slots / 256);         // (8 tiles at least: a wave each)
+  }
   s = std::min<int64_t>(s, kQ4Splits);
   p.splits = s < 1 ? 1 : (int)s;
   return p;
 }
+// rows of sums that may be joined: no more workgroups than the plan shares out slots to
+static size_t q4_records(int T, int Hq, int Hkv) { return (int64_t)T * (Hq / Hkv) >= kQ4WideRows ? 512 * 128 : 256 * 16; }
 
-template <typename T, int D, int NW> static sqa_status start_q4(const Q4AttentionArgs& a, hipStream_t st) {
-  auto fn = q4_attention_kernel<T, D, NW>;
-  using C = Q4Tile<T, D>;
-  size_t lds = NW * C::VB;
-  if (a.a.L.block_table) lds += (size_t)(a.a.L.blocks_per_unit + 3) / 4 * 16 + 16;
+static sqa_status start_q4(void (*fn)(Q4AttentionArgs), int threads, size_t lds, const Q4AttentionArgs& a, hipStream_t st) {
+  if (a.a.L.block_table) lds += (size_t)(a.a.L.blocks_per_unit + 3) / 4 * 16 + 16;       // (whole tiles of block numbers)
   SQA_HIP_CHECK(allow_dynamic_lds(reinterpret_cast<const void*>(fn), lds));
   const int64_t work = (int64_t)a.a.c.B * a.a.c.Hkv * a.tiles * a.splits;
-  fn<<<(unsigned)xcd_grid(work), 64 * NW, lds, st>>>(a);
+  fn<<<(unsigned)xcd_grid(work), threads, lds, st>>>(a);
   SQA_HIP_CHECK(hipGetLastError());
   return SQA_OK;
 }
-template <typename T, int D> static sqa_status launch_q4(int waves, const Q4AttentionArgs& a, hipStream_t st) {
-  if (waves == 2) return start_q4<T, D, 2>(a, st);
-  return waves == 8 ? start_q4<T, D, 8>(a, st) : start_q4<T, D, 4>(a, st);
+template <typename T, int D> static sqa_status launch_q4(const Q4Plan& p, const Q4AttentionArgs& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (p.rows == 128) return start_q4(q4_attention_wide_kernel<D>, 256, Q4Wide<D>::STAGE, a, st);
+  const size_t lds = (size_t)p.waves * Q4Tile<T, D>::VB;
+  if (p.waves == 2) return start_q4(q4_attention_kernel<T, D, 2>, 128, lds, a, st);
+  return p.waves == 8 ? start_q4(q4_attention_kernel<T, D, 8>, 512, lds, a, st) : start_q4(q4_attention_kernel<T, D, 4>, 256, lds, a, st);
 }
 
 }  // namespace sqa
@@ -535,7 +804,7 @@ template <typename T, int D> static sqa_status launch_q4(int waves, const Q4Atte
 extern "C" size_t sqa_q4_workspace_bytes(const sqa_q4_cache* layer, int B, int T, int Hq, int Hkv, int D) {
   sqa_status why;
   if (!layer || sqa::bad_q4(*layer, D, &why) || sqa::bad_chunk_shape(B, T, Hq, Hkv, D, 0, nullptr)) return 0;
-  return sqa::kChunkCounterBytes + (size_t)sqa::kQ4Records * (D / 4 + 1) * 16;
+  return sqa::kChunkCounterBytes + sqa::q4_records(T, Hq, Hkv) * (D / 4 + 1) * 16;
 }
 
 extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
@@ -553,7 +822,7 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   if (uniform && (int64_t)new_pos + T > layer->capacity && T > layer->capacity - layer->n_sink) return SQA_ERR_CAPACITY;
   const size_t es = dt == SQA_F32 ? 4 : 2, qb = (size_t)B * Hq * T * D * es, lb = (size_t)B * Hq * T * sizeof(float);
   if (overlap(q, qb, out, qb) || (lse && (overlap(lse, lb, q, qb) || overlap(lse, lb, out, qb)))) return SQA_ERR_SHAPE;
-  const Q4Plan p = q4_plan(B, T, Hq, Hkv, new_pos, layer->capacity, uniform);
+  const Q4Plan p = q4_plan(dt, B, T, Hq, Hkv, new_pos, layer->capacity, uniform);
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   Q4AttentionArgs a{};
   a.a = q4_args(layer, B, T, Hq, Hkv, new_pos, opts);
@@ -566,6 +835,17 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   a.group_m = reciprocal(a.a.c.g); a.heads_m = reciprocal(Hkv); a.tiles_m = reciprocal(p.tiles); a.splits_m = reciprocal(p.splits);
   a.tiles = p.tiles; a.splits = p.splits;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dt == SQA_F32) return D == 64 ? launch_q4<float, 64>(p.waves, a, st) : launch_q4<float, 128>(p.waves, a, st);
-  return D == 64 ? launch_q4<bf16_t, 64>(p.waves, a, st) : launch_q4<bf16_t, 128>(p.waves, a, st);
+  if (dt == SQA_F32) return D == 64 ? launch_q4<float, 64>(p, a, st) : launch_q4<float, 128>(p, a, st);
+  return D == 64 ? launch_q4<bf16_t, 64>(p, a, st) : launch_q4<bf16_t, 128>(p, a, st);
+}
+
+extern "C" sqa_status sqa_q4_plan(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
+                                  const sqa_batch_opts* opts, sqa_q4_plan_info* info) {
+  if (!layer || !info) return SQA_ERR_NULL;
+  if (dt != SQA_F32 && dt != SQA_BF16) return SQA_ERR_DTYPE;
+  if (sqa::bad_chunk_shape(B, T, Hq, Hkv, D, new_pos, opts)) return SQA_ERR_SHAPE;
+  if (layer->capacity < 1 || layer->capacity > sqa::kQ4MostSlots) return SQA_ERR_CAPACITY;
+  const sqa::Q4Plan p = sqa::q4_plan(dt, B, T, Hq, Hkv, new_pos, layer->capacity, !(opts && (opts->prompt_len || opts->new_pos_seq)));
+  info->rows = p.rows; info->waves = p.waves; info->row_tiles = p.tiles; info->slot_splits = p.splits; info->rounded_probs = p.rows == 128;
+  return SQA_OK;
 }

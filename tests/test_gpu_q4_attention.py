@@ -44,12 +44,15 @@ def unit(c, name, u):
     return x[c.block_table[0][u].long()].flatten(0, 1)[:cap] if c.blocked else x.view(-1, cap, x.shape[-1])[u]
 
 
-def hp_of(dtype, rows):
-    """(128 rows and more of a unit may have their probabilities rounded to bf16)"""
-    return 0.0 if dtype == torch.float32 else (2.0 ** -15 if rows < 128 else 2.0 ** -8)
+def hp_of(sqa, c, q, ragged, before=0):
+    """How far probabilities may be off for the product with V: by the form that the call takes."""
+    B, Hq, T, D = q.shape
+    if q.dtype == torch.float32:
+        return 0.0
+    return 2.0 ** -8 if sqa.q4_plan(c.capacities[0], B, T, Hq, c.Hkv, D, "bf16", before, ragged)["rounded_probs"] else 2.0 ** -15
 
 
-def check(c, q, out, lse, before, new, cap, sink, what):
+def check(hp, c, q, out, lse, before, new, cap, sink, what):
     """Every unit against the definition; before and new per sequence, cap their slots."""
     B, Hq, T, D = q.shape
     g = Hq // c.Hkv
@@ -63,7 +66,7 @@ def check(c, q, out, lse, before, new, cap, sink, what):
         for h in range(c.Hkv):
             u = b * c.Hkv + h
             K, V = (Q.values(unit(c, x, u)[:len(at)], unit(c, x + "_scale", u)[:len(at)]) for x in ("K", "V"))
-            want, want_lse, bound, lse_bound = Q.attention(q[b, h * g:(h + 1) * g, :n], K, V, seen, q.dtype, hp_of(q.dtype, T * g))
+            want, want_lse, bound, lse_bound = Q.attention(q[b, h * g:(h + 1) * g, :n], K, V, seen, q.dtype, hp)
             got = out[b, :n, h * g:(h + 1) * g].transpose(0, 1).double()
             assert bool(((got - want).abs() <= bound).all()), (what, b, h, float(((got - want).abs() / bound).max()))
             off = (lse[b, h * g:(h + 1) * g, :n].double() - want_lse).abs()
@@ -86,7 +89,29 @@ def test_attention(sqa, dtype, D, blocked):
         c = filled(sqa, B, Hkv, D, cap, 0, blocked, gen)
         q = (torch.randn(B, Hq, T, D, generator=gen, device=DEV) * 1.5).to(dt)
         out, lse = sqa.q4_attention(q, before, c)
-        check(c, q, out, lse, [before] * B, [T] * B, [cap] * B, 0, (B, T, before, Hq, Hkv))
+        check(hp_of(sqa, c, q, False, before), c, q, out, lse, [before] * B, [T] * B, [cap] * B, 0, (B, T, before, Hq, Hkv))
+        again = sqa.q4_attention(q, before, c)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+WIDE = [  # B, T, before, Hq, Hkv, capacity (0: room for all), sinks -> slot splits: chunks whose workgroups have 128 rows
+    (4, 520, 70, 16, 8, 0, 0, 1), (8, 300, 0, 32, 8, 0, 0, 1), (16, 129, 63, 16, 16, 0, 0, 1), (1, 128, 8000, 32, 4, 0, 0, 7), (2, 257, 7000, 16, 8, 0, 0, 6),
+    (8, 130, 400, 32, 8, 200, 4, 1), (16, 128, 190, 16, 16, 300, 7, 1)]
+
+
+@pytest.mark.parametrize("blocked", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows(sqa, D, blocked):
+    """Sums joined over workgroups, tiles of slots that end inside a block, rows behind the last, chunks that turn a ring."""
+    for i, (B, T, before, Hq, Hkv, cap, sink, splits) in enumerate(WIDE):
+        gen = generator(200 + i)
+        cap = cap or before + T + 2
+        c = filled(sqa, B, Hkv, D, cap, sink, blocked, gen)
+        q = (torch.randn(B, Hq, T, D, generator=gen, device=DEV) * 1.5).bfloat16()
+        plan = sqa.q4_plan(cap, B, T, Hq, Hkv, D, "bf16", before)
+        assert plan["rows"] == 128 and plan["slot_splits"] == splits
+        out, lse = sqa.q4_attention(q, before, c)
+        check(2.0 ** -8, c, q, out, lse, [before] * B, [T] * B, [cap] * B, sink, (B, T, before, Hq, Hkv))
         again = sqa.q4_attention(q, before, c)
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
@@ -110,14 +135,14 @@ def test_rings(sqa, dtype, D, blocked):
             # (what a slot holds depends on the position modulo the ring: long histories by a shorter one that ends the same way)
             ring = cap - sink
             short = before if before < 4 * cap + 200 else sink + ring + (before - sink) % ring + ring
-            check(c, q, out, lse, [short] * B, [T] * B, [cap] * B, sink, (cap, sink, T, before))
+            check(hp_of(sqa, c, q, False, before), c, q, out, lse, [short] * B, [T] * B, [cap] * B, sink, (cap, sink, T, before))
 
 
 def test_ragged(sqa):
     """Own lengths, positions and budgets; padding and sequences that take no part stay as they were."""
     for dtype, D, T in (("bf16", 128, 9), ("f32", 64, 9), ("bf16", 64, 70), ("bf16", 128, 300)):
         dt, gen = R.DT[dtype], generator(17)
-        B, Hq, Hkv, cap, sink = 6, 6, 2, 700, 4
+        B, Hq, Hkv, cap, sink = 6, 24 if T == 300 else 6, 8 if T == 300 else 2, 700, 4
         new = [T, 1, 0, T // 2, T, 1]
         before = [0, 650, 5, 100, -1, 3000]
         budget = [700, 300, 700, 505, 700, 64]
@@ -129,7 +154,7 @@ def test_ragged(sqa):
             opts = sqa.batch_opts(prompt_len=ints(new), new_pos_seq=ints(before), budget_seq=ints(budget), status=status)
             sqa.q4_attention(q, 0, c, out=out, lse=lse, opts=opts)
             part = [n if p >= 0 else 0 for n, p in zip(new, before)]
-            check(c, q, out, lse, before, part, budget, sink, (dtype, D, T))
+            check(hp_of(sqa, c, q, True), c, q, out, lse, before, part, budget, sink, (dtype, D, T))
             assert int(status) == 0
             for b, n in enumerate(part):
                 assert bool((out[b, n:] == 5).all()) and bool((lse[b, :, n:] == 6).all())
@@ -140,7 +165,10 @@ def test_what_is_not_seen_changes_nothing(sqa):
     for dtype, D in (("bf16", 128), ("bf16", 64), ("f32", 128)):
         dt = R.DT[dtype]
         for B, T, before, Hq, Hkv, cap, sink in ((2, 1, 45, 4, 2, 100, 0), (1, 7, 20, 6, 2, 60, 0), (1, 40, 200, 8, 4, 1000, 0), (1, 20, 95, 4, 2, 64, 4),
-                                                 (1, 300, 10, 8, 2, 400, 0)):
+                                                 (1, 300, 10, 8, 2, 400, 0),
+                                                 (8, 300, 50, 32, 8, 400, 0), (8, 130, 400, 32, 8, 200, 4)):
+            if dt == torch.float32 and B * T > 1000:
+                continue
             gen = generator(23)
             c = filled(sqa, B, Hkv, D, cap, sink, False, gen)
             q = torch.randn(B, Hq, T, D, generator=gen, device=DEV).to(dt)
@@ -177,7 +205,7 @@ def test_extreme_logits_and_queries(sqa):
         q[0, 4] = -Q.values(c.K[0][0, 0, 299], c.K_scale[0][0, 0, 299]).float() * 30
         q = q.to(dt)
         out, lse = sqa.q4_attention(q, 299, c)
-        check(c, q, out, lse, [299], [1], [300], 0, dtype)
+        check(hp_of(sqa, c, q, False, 299), c, q, out, lse, [299], [1], [300], 0, dtype)
         q2 = q.clone()
         q2[0, 5, 0, 3], q2[0, 2, 0, 0] = math.nan, math.inf
         got = sqa.q4_attention(q2, 299, c)
@@ -188,9 +216,9 @@ def test_extreme_logits_and_queries(sqa):
 
 def test_blocks_that_are_not_there(sqa):
     """A unit with a block outside the pools, and a sequence that overwrote its own tokens: zeros, -inf, reported; the others as they were."""
-    for T, before, cap in ((1, 40, 100), (1, 5000, 6000), (30, 60, 100), (200, 50, 300)):
+    for T, before, cap, Hq, Hkv in ((1, 40, 100, 4, 2), (1, 5000, 6000, 4, 2), (30, 60, 100, 4, 2), (200, 50, 300, 4, 2), (300, 20, 400, 64, 32), (128, 7900, 8100, 32, 4)):
         gen = generator(31)
-        B, Hq, Hkv, D = 2, 4, 2, 128
+        B, D, g = 2, 128, Hq // Hkv
         c = filled(sqa, B, Hkv, D, cap, 0, True, gen)
         q = torch.randn(B, Hq, T, D, generator=gen, device=DEV).bfloat16()
         clean = sqa.q4_attention(q, before, c)
@@ -203,8 +231,8 @@ def test_blocks_that_are_not_there(sqa):
                 assert int(status) == 2
                 # (rows that see no slot of the block may be there all the same: a chunk's first ones)
                 sees = torch.arange(before, before + T, device=DEV) >= entry * 16
-                assert bool((out[0, sees, 2:] == 0).all()) and bool((lse[0, 2:, sees] == -math.inf).all())
-                assert torch.equal(out[0, :, :2], clean[0][0, :, :2]) and torch.equal(out[1], clean[0][1]) and torch.equal(lse[1], clean[1][1])
+                assert bool((out[0, sees, g:2 * g] == 0).all()) and bool((lse[0, g:2 * g, sees] == -math.inf).all())
+                assert torch.equal(out[0, :, :g], clean[0][0, :, :g]) and torch.equal(out[0, :, 2 * g:], clean[0][0, :, 2 * g:]) and torch.equal(out[1], clean[0][1]) and torch.equal(lse[1], clean[1][1])
                 c.block_table[0].copy_(was)
         c.block_table[0][:, (before + T + 15) // 16:] = -1                   # (entries behind the last token are not read)
         assert all(torch.equal(a, b) for a, b in zip(clean, sqa.q4_attention(q, before, c)))
@@ -314,7 +342,7 @@ def test_a_serving_loop(sqa, dtype):
         # (units of sequences without blocks have -1 in their tables: looked at only where there are tokens)
         table = c.block_table[0].clone()
         c.block_table[0].clamp_(min=0)
-        check(c, q, out, lse, length, safe, [cap] * B, sink, step)
+        check(hp_of(sqa, c, q, True), c, q, out, lse, length, safe, [cap] * B, sink, step)
         c.block_table[0].copy_(table)
         got = sqa.q4_read(c, 0, cap, torch.float32, opts=sqa.batch_opts(prompt_len=ints([min(p + n, cap) if n else 0 for p, n in zip(length, new)])))
         for b, n in enumerate(new):

@@ -134,6 +134,40 @@ def test_map_refusals(change, code):
     assert lib.sqa_slot_map(*a.values()) == code
 
 
+FORMS = [  # capacity, B, T, Hq, Hkv, new_pos, dtype -> rows, waves, row tiles, slot splits
+    (100, 1, 1, 8, 2, 99, "bf16", (16, 8, 1, 1)), (30001, 1, 1, 64, 8, 30000, "bf16", (16, 8, 1, 32)), (571, 64, 1, 32, 32, 1500, "bf16", (16, 2, 1, 1)),
+    (1001, 64, 1, 32, 8, 1000, "bf16", (16, 4, 1, 1)), (4095, 16, 5, 32, 8, 4090, "bf16", (16, 8, 2, 1)), (5000, 2, 1, 12, 4, 4990, "f32", (16, 8, 1, 19)),
+    (4000, 1, 128, 32, 8, 3000, "bf16", (16, 8, 32, 1)), (600, 4, 520, 16, 8, 70, "bf16", (128, 4, 9, 1)), (8192, 4, 300, 64, 8, 7800, "bf16", (128, 4, 19, 1)),
+    (8200, 1, 128, 32, 4, 8000, "bf16", (128, 4, 8, 7)), (8200, 1, 128, 32, 4, 8000, "f32", (16, 8, 64, 1)), (1 << 30, 1, 1, 1, 1, 5, "bf16", (16, 8, 1, 1))]
+
+
+@pytest.mark.parametrize("capacity,B,T,Hq,Hkv,new_pos,dtype,want", FORMS)
+def test_plan(capacity, B, T, Hq, Hkv, new_pos, dtype, want):
+    got = sqa.q4_plan(capacity, B, T, Hq, Hkv, 128, dtype, new_pos)
+    assert (got["rows"], got["waves"], got["row_tiles"], got["slot_splits"]) == want and got["rounded_probs"] == (want[0] == 128)
+    assert got == sqa.q4_plan(min(capacity, new_pos + T), B, T, Hq, Hkv, 128, dtype, ragged=True)         # (a ragged batch: by the room there is)
+
+
+def test_plans_fit_their_workspace():
+    # no more records than the workspace has rows for, of any length up to the one that it was made for, and no more than a wave's lanes
+    for dtype in ("bf16", "f32"):
+        for B, Hq, Hkv in ((1, 1, 1), (1, 8, 1), (1, 64, 8), (3, 12, 4), (40, 32, 32)):
+            for T in (1, 2, 5, 15, 16, 17, 31, 64, 127, 128, 129, 500, 4000):
+                for cap in (1, 300, 5000, 100000, 1 << 30):
+                    p = sqa.q4_plan(cap, B, T, Hq, Hkv, 64, dtype, ragged=True)
+                    records = B * Hkv * p["row_tiles"] * p["slot_splits"] * p["rows"]
+                    room = lib.sqa_q4_workspace_bytes(layer(cap=cap), B, T, Hq, Hkv, 64) - 4096
+                    assert p["slot_splits"] <= 64 and (p["slot_splits"] == 1 or (records * 17 * 16 <= room and B * Hkv * p["row_tiles"] <= 1024))
+
+
+@pytest.mark.parametrize("change,code", [(dict(layer=None), NULL), (dict(info=None), NULL), (dict(dt=2), DTYPE), (dict(T=0), SHAPE), (dict(D=32), SHAPE),
+                                         (dict(layer=layer(cap=0)), CAP)])
+def test_plan_refusals(change, code):
+    a = dict(layer=layer(), dt=1, B=2, T=4, Hq=4, Hkv=2, D=64, new_pos=10, opts=None, info=C.byref(sqa.Q4PlanInfo()))
+    a.update(change)
+    assert lib.sqa_q4_plan(*a.values()) == code
+
+
 def test_one_workspace_serves_every_shorter_chunk():
     need = lambda *shape: lib.sqa_q4_workspace_bytes(layer(cap=5000), *shape)
     for B, Hq, Hkv, D in ((1, 8, 8, 128), (3, 24, 8, 64), (16, 64, 8, 128), (2, 5, 1, 128)):
