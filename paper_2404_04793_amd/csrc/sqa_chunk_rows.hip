@@ -64,8 +64,8 @@ __device__ __forceinline__ int judge_unit(const ChunkArgs& a, const UnitAsked& k
   return bad ? SQA_ERR_STATE : (outside ? SQA_ERR_SHAPE : 0);
 }
 
-// AXES: rotated by positions on several axes
-template <typename T, int D, int U, bool AXES> __device__ __forceinline__ void rows_work(const RowsArgs& a) {
+template <typename T, int D, int U>
+__global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs a) {
   constexpr int E = Piece<T>::E, LPR = D / E, HPW = SQA_WAVE / LPR;
   const int lane = threadIdx.x & (SQA_WAVE - 1), c = lane % LPR;
   const int64_t item = (int64_t)blockIdx.x * (kRowsThreads / SQA_WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SQA_WAVE);
@@ -78,7 +78,7 @@ template <typename T, int D, int U, bool AXES> __device__ __forceinline__ void r
   const int t0 = tb * U;
   if (t0 >= s.n) return;
   const bool turn = a.prep.rope != nullptr;
-  if (!AXES && turn && s.pos + s.n > a.prep.n_pos) {
+  if (turn && s.pos + s.n > a.prep.n_pos) {
     if (group == 0 && tb == 0 && lane == 0 && a.c.status) *a.c.status = SQA_ERR_SHAPE;
     return;
   }
@@ -103,70 +103,55 @@ template <typename T, int D, int U, bool AXES> __device__ __forceinline__ void r
   if (kind == kKeyValue) asked = ask_unit(a.c, b, u, s, c);
 
   // ---- norm and rotation
-  const int e0 = c * E;
-  if constexpr (AXES) {
-    RowPrep<T, D, true> how(a.prep, kind == kQuery ? a.prep.q_weight : a.prep.k_weight, lane);
-    how.set_axes(a.axes);
+  const void* wp = kind == kQuery ? a.prep.q_weight : a.prep.k_weight;
+  float w[E];
+  if (wp) Piece<T>::open(ld16(static_cast<const T*>(wp) + c * E), w);
+  const int half = a.prep.rot_dim / 2, e0 = c * E, step = a.prep.interleaved ? 0 : half / E;
+  const bool mine = turn && e0 < a.prep.rot_dim, first = e0 < half;
+  const int partner = mine ? (first ? lane + step : lane - step) : lane;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      float y[E];
-      Piece<T>::open(x[i], y);
-      const AxisPos at = axes_of(a.axes, a.c, a.prep.n_pos, b, t0 + min(i, nt - 1), group == 0 && lane == 0);
-      how.normalise(y);
-      how.rotate(y, at);
-      x[i] = Piece<T>::close(y);
+  for (int i = 0; i < U; ++i) {
+    float y[E];
+    Piece<T>::open(x[i], y);
+    if (wp) {
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
+#pragma unroll
+      for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
+      const float r = 1.f / sqrtf(ss * (1.f / D) + a.prep.eps);
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
     }
-  } else {
-    const void* wp = kind == kQuery ? a.prep.q_weight : a.prep.k_weight;
-    float w[E];
-    if (wp) Piece<T>::open(ld16(static_cast<const T*>(wp) + c * E), w);
-    const int half = a.prep.rot_dim / 2, step = a.prep.interleaved ? 0 : half / E;
-    const bool mine = turn && e0 < a.prep.rot_dim, first = e0 < half;
-    const int partner = mine ? (first ? lane + step : lane - step) : lane;
+    if (turn) {
+      const float* row = a.prep.rope + (s.pos + t0 + min(i, nt - 1)) * a.prep.rot_dim;
+      if (a.prep.interleaved) {
+        if (mine) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      float y[E];
-      Piece<T>::open(x[i], y);
-      if (wp) {
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
-        const float r = 1.f / sqrtf(ss * (1.f / D) + a.prep.eps);
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
-      }
-      if (turn) {
-        const float* row = a.prep.rope + (s.pos + t0 + min(i, nt - 1)) * a.prep.rot_dim;
-        if (a.prep.interleaved) {
-          if (mine) {
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-              const float cs = row[(e0 + e) / 2], sn = row[half + (e0 + e) / 2];
-              const float p = y[e], q = y[e + 1];
-              y[e] = p * cs - q * sn;
-              y[e + 1] = q * cs + p * sn;
-            }
-          }
-        } else {
-          float cs[E], sn[E];
-          const float* from = row + (mine ? (first ? e0 : e0 - half) : 0);
-#pragma unroll
-          for (int e = 0; e < E; e += 4) {
-            *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
-            *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
-          }
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
-            const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
-            y[e] = mine ? z : y[e];
+          for (int e = 0; e < E; e += 2) {
+            const float cs = row[(e0 + e) / 2], sn = row[half + (e0 + e) / 2];
+            const float p = y[e], q = y[e + 1];
+            y[e] = p * cs - q * sn;
+            y[e + 1] = q * cs + p * sn;
           }
         }
+      } else {
+        float cs[E], sn[E];
+        const float* from = row + (mine ? (first ? e0 : e0 - half) : 0);
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
+          *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
+          const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
+          y[e] = mine ? z : y[e];
+        }
       }
-      if (wp || turn) x[i] = Piece<T>::close(y);
     }
+    if (wp || turn) x[i] = Piece<T>::close(y);
   }
 
   // ---- where they go
@@ -200,8 +185,74 @@ template <typename T, int D, int U, bool AXES> __device__ __forceinline__ void r
     *reinterpret_cast<int4*>(a.c.L.unit_state + (int64_t)u * SQA_ST_WORDS) = make_int4((int)(s.pos + s.n), 0, -2, 0);
 }
 
-template <typename T, int D, int U> __global__ __launch_bounds__(kRowsThreads) void chunk_rows_kernel(const RowsArgs a) { rows_work<T, D, U, false>(a); }
-template <typename T, int D, int U> __global__ __launch_bounds__(kRowsThreads) void axis_rows_kernel(const RowsArgs a) { rows_work<T, D, U, true>(a); }
+// The same with positions on several axes.  What a token's pairs turn by is gathered from several rows of the table, and is the same for all heads:
+// a wave takes one token and U groups of heads in place of U tokens.  (2 x 4500 tokens of 32 + 8 heads, a quarter of them padding, axes in turns, from
+// HBM: 47 us, 2.9 TB/s; with U tokens of one group 91.)
+template <typename T, int D, int U>
+__global__ __launch_bounds__(kRowsThreads) void axis_rows_kernel(const RowsArgs a) {
+  constexpr int E = Piece<T>::E, LPR = D / E, HPW = SQA_WAVE / LPR;
+  const int lane = threadIdx.x & (SQA_WAVE - 1), c = lane % LPR;
+  const int64_t item = (int64_t)blockIdx.x * (kRowsThreads / SQA_WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SQA_WAVE);
+  const int groups = a.q_groups + a.kv_groups, runs = (groups + U - 1) / U;
+  const int t = (int)(item % a.c.T);
+  const int64_t br = item / a.c.T;
+  const int b = (int)(br / runs), first = (int)(br % runs) * U;
+  if (b >= a.c.B) return;
+  const bool reports = first == 0 && lane == 0;
+  const ChunkSeq s = chunk_seq(a.c, b, reports && t == 0);
+  if (t >= s.n) return;
+  auto kind_of = [&](int group) { return group < a.q_groups ? kQuery : (a.k_out ? kKeyOut : kKeyValue); };
+  auto head_of = [&](int group) { return (group < a.q_groups ? group : group - a.q_groups) * HPW + lane / LPR; };
+  uint4 x[U], v[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int group = min(first + i, groups - 1), kind = kind_of(group);
+    const sqa_token_rows& src = kind == kQuery ? a.q : a.k;
+    const int h = min(head_of(group), (kind == kQuery ? a.c.Hq : a.c.Hkv) - 1);
+    const int64_t at = (int64_t)h * D + c * E;
+    x[i] = ld16(static_cast<const T*>(src.data) + (int64_t)b * src.seq_stride + (int64_t)t * src.row_stride + at);
+    if (kind == kKeyValue) v[i] = ld16(static_cast<const T*>(a.v.data) + (int64_t)b * a.v.seq_stride + (int64_t)t * a.v.row_stride + at);
+  }
+  __shared__ float s_angles[kRowsThreads / SQA_WAVE][128];
+  RowPrep<T, D> how(a.prep, lane);
+  float cs[E], sn[E];
+  how.angles_of(a.axes, axes_of(a.axes, a.c, a.prep.n_pos, b, t, reports), s_angles[threadIdx.x / SQA_WAVE], cs, sn);
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int group = first + i;
+    if (group >= groups) break;
+    const int kind = kind_of(group), heads = kind == kQuery ? a.c.Hq : a.c.Hkv, h = head_of(group);
+    const bool there = h < heads;
+    const int u = b * a.c.Hkv + min(h, heads - 1);
+    UnitAsked asked;
+    if (kind == kKeyValue) asked = ask_unit(a.c, b, u, s, c);
+    float y[E];
+    Piece<T>::open(x[i], y);
+    how.normalise(y, kind == kQuery ? a.prep.q_weight : a.prep.k_weight);
+    how.turn(y, cs, sn);
+    const uint4 w = Piece<T>::close(y);
+    if (kind != kKeyValue) {
+      if (there) st16(static_cast<T*>(kind == kQuery ? a.q_out : a.k_out) + (((int64_t)b * heads + h) * a.c.T + t) * D + c * E, w);
+      continue;
+    }
+    const int why = judge_unit<LPR>(a.c, asked, s, c);
+    if (!there) continue;
+    if (why) {
+      if (c == 0 && t == 0 && a.c.status) *a.c.status = why;
+      continue;
+    }
+    const ChunkUnit& unit = asked.x;
+    const int64_t slot = s.pos + t;
+    const int64_t row = unit.table ? (int64_t)unit.table[slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit.first + slot;
+    st16(static_cast<T*>(a.c.L.K) + row * D + c * E, w);
+    st16(static_cast<T*>(a.c.L.V) + row * D + c * E, v[i]);
+    if (c == 0) {
+      a.c.L.pos[unit.first + slot] = (int32_t)slot;
+      if (a.c.L.score_acc) a.c.L.score_acc[unit.first + slot] = 0.f;
+      if (t == 0) *reinterpret_cast<int4*>(a.c.L.unit_state + (int64_t)u * SQA_ST_WORDS) = make_int4((int)(s.pos + s.n), 0, -2, 0);
+    }
+  }
+}
 
 template <typename T, int D>
 static void launch_rows(RowsArgs& a, hipStream_t st) {
@@ -210,6 +261,18 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   a.kv_groups = (a.k_out || a.c.L.K) ? (a.c.Hkv + HPW - 1) / HPW : 0;
   const int64_t groups = (int64_t)a.c.B * (a.q_groups + a.kv_groups);
   constexpr int waves = kRowsThreads / SQA_WAVE;
+  if (a.axes.n) {
+    // four or five groups of heads a wave where that leaves every SIMD two waves, whichever comes out more evenly (10 groups: 51 us, 55 with four, 58
+    // with eight or two)
+    const int all = a.q_groups + a.kv_groups, U = (all + 4) / 5 * 5 < (all + 3) / 4 * 4 ? 5 : 4;
+    const bool many = (int64_t)a.c.B * a.c.T * ((all + U - 1) / U) >= 2048;
+    const int64_t items = (int64_t)a.c.B * a.c.T * (many ? (all + U - 1) / U : all);
+    const unsigned blocks = (unsigned)((items + waves - 1) / waves);
+    if (!many) axis_rows_kernel<T, D, 1><<<blocks, kRowsThreads, 0, st>>>(a);
+    else if (U == 5) axis_rows_kernel<T, D, 5><<<blocks, kRowsThreads, 0, st>>>(a);
+    else axis_rows_kernel<T, D, 4><<<blocks, kRowsThreads, 0, st>>>(a);
+    return;
+  }
   // two tokens per wave where that leaves every SIMD a wave, otherwise one.  (4 x 2048 tokens of 32 + 8 heads: 35.7 us with two, 39.1
   // with four, 42.3 with one; rows stored non-temporally 34.7, but what reads them next is slower by more.  From a quarter as many waves on or
   // only from four times as many on, in us against this rule: 64 tokens 4.8 and 4.1 against 4.9, 4 x 64 appended 6.7 and 6.1 against 6.7, 2 x 512
@@ -217,11 +280,6 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   const bool two = groups * ((a.c.T + 1) / 2) >= 1024;
   a.t_blocks = two ? (a.c.T + 1) / 2 : a.c.T;
   const int64_t blocks = (groups * a.t_blocks + waves - 1) / waves;
-  if (a.axes.n) {
-    if (two) axis_rows_kernel<T, D, 2><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
-    else axis_rows_kernel<T, D, 1><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
-    return;
-  }
   if (two) chunk_rows_kernel<T, D, 2><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
   else chunk_rows_kernel<T, D, 1><<<(unsigned)blocks, kRowsThreads, 0, st>>>(a);
 }

@@ -8,8 +8,6 @@
 
 namespace sqa {
 
-enum { kQ4Query = 0, kQ4KeyValue = 1 };
-
 struct Q4RowsArgs {
   Q4Args a;
   sqa_token_rows q, k, v;
@@ -18,7 +16,7 @@ struct Q4RowsArgs {
   AxesArgs axes;
   const int32_t* slot_map;
   int64_t rows;                                     // of the cache
-  int q_groups, kv_groups, t_blocks;                // items of a sequence: head groups x blocks of U tokens
+  int q_groups, kv_groups;                          // groups of heads, as many as a wave's lanes hold rows
 };
 
 // E numbers of a lane, LPG lanes of which are a group: codes in the low 4 E bits, and the group's byte
@@ -43,77 +41,76 @@ template <int E> __device__ __forceinline__ uint32_t q4_round(const float (&y)[E
   return w;
 }
 
+// A wave takes one token and U groups of heads: slots and angles are the same for all of them.
 template <typename T, int D, int U, bool AXES>
 __global__ __launch_bounds__(kRowsThreads) void q4_rows_kernel(const Q4RowsArgs a) {
   constexpr int E = Piece<T>::E, LPR = D / E, HPW = SQA_WAVE / LPR, LPG = kGroup / E;
   const int lane = threadIdx.x & (SQA_WAVE - 1), c = lane % LPR;
   const int64_t item = (int64_t)blockIdx.x * (kRowsThreads / SQA_WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SQA_WAVE);
-  const int groups = a.q_groups + a.kv_groups;
-  const int tb = (int)(item % a.t_blocks);
-  const int64_t bg = item / a.t_blocks;
-  const int b = (int)(bg / groups), group = (int)(bg % groups);
+  const int groups = a.q_groups + a.kv_groups, runs = (groups + U - 1) / U, T_ = a.a.c.T;
+  const int t = (int)(item % T_);
+  const int64_t br = item / T_;
+  const int b = (int)(br / runs), first = (int)(br % runs) * U;
   if (b >= a.a.c.B) return;
-  const bool reports = group == groups - 1 && tb == 0 && lane == 0;
-  const Q4Seq s = q4_seq(a.a, b, reports);
-  const int t0 = tb * U;
-  if (t0 >= s.n) return;
+  const bool reports = first == 0 && lane == 0;
+  const Q4Seq s = q4_seq(a.a, b, reports && t == 0);
+  if (t >= s.n) return;
   const bool turn = a.prep.rope != nullptr;
   if (!AXES && turn && s.pos + s.n > a.prep.n_pos) {
-    if (reports && a.a.c.status) *a.a.c.status = SQA_ERR_SHAPE;
+    if (reports && t == 0 && a.a.c.status) *a.a.c.status = SQA_ERR_SHAPE;
     return;
   }
-  const int kind = group < a.q_groups ? kQ4Query : kQ4KeyValue;
-  if (kind == kQ4KeyValue && s.why && !a.slot_map) {
-    if (reports && a.a.c.status) *a.a.c.status = s.why;
-    return;
-  }
-  const int heads = kind == kQ4Query ? a.a.c.Hq : a.a.c.Hkv;
-  const int h = (kind == kQ4Query ? group : group - a.q_groups) * HPW + lane / LPR;
-  const bool there = h < heads;
-  const int nt = min(U, s.n - t0);
+  const bool stores = a.slot_map || !s.why;         // (queries are written all the same)
+  if (!stores && reports && t == 0 && a.a.c.status) *a.a.c.status = s.why;
+  const int slot = stores && !a.slot_map ? s.slot(s.pos + t) : 0;
 
-  const sqa_token_rows& src = kind == kQ4Query ? a.q : a.k;
-  const int64_t at = (int64_t)b * src.seq_stride + (int64_t)t0 * src.row_stride + (int64_t)(there ? h : 0) * D + c * E;
+  auto head_of = [&](int group) { return (group < a.q_groups ? group : group - a.q_groups) * HPW + lane / LPR; };
   uint4 x[U], v[U];
-#pragma unroll
-  for (int i = 0; i < U; ++i) x[i] = ld16(static_cast<const T*>(src.data) + at + min(i, nt - 1) * src.row_stride);
   int64_t row[U];                                   // of the cache
-  if (kind == kQ4KeyValue) {
-    const int64_t vat = (int64_t)b * a.v.seq_stride + (int64_t)t0 * a.v.row_stride + (int64_t)(there ? h : 0) * D + c * E;
-#pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = ld16(static_cast<const T*>(a.v.data) + vat + min(i, nt - 1) * a.v.row_stride);
-    const int64_t u = (int64_t)b * heads + min(h, heads - 1);
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int t = t0 + min(i, nt - 1);
-      if (a.slot_map) {
-        row[i] = a.slot_map[u * a.a.c.T + t];
-      } else {
-        const int slot = s.slot(s.pos + t);
-        row[i] = a.a.L.block_table ? (int64_t)a.a.L.block_table[u * a.a.L.blocks_per_unit + slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS
-                                   : u * a.a.L.capacity + slot;
-      }
-    }
-  }
-
-  RowPrep<T, D, AXES> how(a.prep, kind == kQ4Query ? a.prep.q_weight : a.prep.k_weight, lane);
-  if constexpr (AXES) how.set_axes(a.axes);
 #pragma unroll
   for (int i = 0; i < U; ++i) {
+    const int group = min(first + i, groups - 1);
+    const bool query = group < a.q_groups;
+    const sqa_token_rows& src = query ? a.q : a.k;
+    const int h = min(head_of(group), (query ? a.a.c.Hq : a.a.c.Hkv) - 1);
+    const int64_t at = (int64_t)h * D + c * E;
+    x[i] = ld16(static_cast<const T*>(src.data) + (int64_t)b * src.seq_stride + (int64_t)t * src.row_stride + at);
+    if (!query) {
+      v[i] = ld16(static_cast<const T*>(a.v.data) + (int64_t)b * a.v.seq_stride + (int64_t)t * a.v.row_stride + at);
+      const int64_t u = (int64_t)b * a.a.c.Hkv + h;
+      row[i] = a.slot_map ? a.slot_map[u * T_ + t]
+             : a.a.L.block_table ? (int64_t)a.a.L.block_table[u * a.a.L.blocks_per_unit + slot / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS
+                                 : u * a.a.L.capacity + slot;
+    }
+  }
+  RowPrep<T, D> how(a.prep, lane);
+  float cs[E], sn[E];
+  if constexpr (AXES) {
+    __shared__ float s_angles[kRowsThreads / SQA_WAVE][128];
+    how.angles_of(a.axes, axes_of(a.axes, a.a.c, a.prep.n_pos, b, t, reports), s_angles[threadIdx.x / SQA_WAVE], cs, sn);
+  } else if (turn) {
+    how.angles_of(s.pos + t, cs, sn);
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int group = first + i;
+    if (group >= groups) break;
+    const bool query = group < a.q_groups;
+    const int h = head_of(group);
+    const bool there = h < (query ? a.a.c.Hq : a.a.c.Hkv);
     float y[E];
-    const int t = t0 + min(i, nt - 1);
     Piece<T>::open(x[i], y);
-    how.normalise(y);
-    if constexpr (AXES) how.rotate(y, axes_of(a.axes, a.a.c, a.prep.n_pos, b, t, group == groups - 1 && lane == 0));
-    else if (turn) how.rotate(y, s.pos + t);
-    if (kind == kQ4Query) {
+    how.normalise(y, query ? a.prep.q_weight : a.prep.k_weight);
+    if (turn) how.turn(y, cs, sn);
+    if (query) {
       const uint4 w = Piece<T>::close(y);
-      if (there && i < nt) st16(static_cast<T*>(a.q_out) + (((int64_t)b * heads + h) * a.a.c.T + t) * D + c * E, w);
+      if (there) st16(static_cast<T*>(a.q_out) + (((int64_t)b * a.a.c.Hq + h) * T_ + t) * D + c * E, w);
       continue;
     }
+    if (!stores) continue;
     const bool inside = (uint64_t)row[i] < (uint64_t)a.rows;
-    if (there && i < nt && c == 0 && !inside && !(a.slot_map && row[i] == -1) && a.a.c.status) *a.a.c.status = SQA_ERR_SHAPE;
-    const bool put = there && i < nt && inside;
+    if (there && c == 0 && !inside && !(a.slot_map && row[i] == -1) && a.a.c.status) *a.a.c.status = SQA_ERR_SHAPE;
+    const bool put = there && inside;
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
       if (kv) Piece<T>::open(v[i], y);
@@ -186,12 +183,12 @@ template <typename T, int D> static void launch_q4_rows(Q4RowsArgs& a, hipStream
   constexpr int HPW = SQA_WAVE / (D / Piece<T>::E), waves = kRowsThreads / SQA_WAVE;
   a.q_groups = a.q_out ? (a.a.c.Hq + HPW - 1) / HPW : 0;
   a.kv_groups = (a.a.c.Hkv + HPW - 1) / HPW;
-  const int64_t groups = (int64_t)a.a.c.B * (a.q_groups + a.kv_groups);
-  const bool two = groups * ((a.a.c.T + 1) / 2) >= 1024;            // (as in sqa_chunk_rows.hip)
-  a.t_blocks = two ? (a.a.c.T + 1) / 2 : a.a.c.T;
-  const unsigned blocks = (unsigned)((groups * a.t_blocks + waves - 1) / waves);
-  if (a.axes.n) two ? q4_rows_kernel<T, D, 2, true><<<blocks, kRowsThreads, 0, st>>>(a) : q4_rows_kernel<T, D, 1, true><<<blocks, kRowsThreads, 0, st>>>(a);
-  else two ? q4_rows_kernel<T, D, 2, false><<<blocks, kRowsThreads, 0, st>>>(a) : q4_rows_kernel<T, D, 1, false><<<blocks, kRowsThreads, 0, st>>>(a);
+  const int groups = a.q_groups + a.kv_groups;
+  const bool four = (int64_t)a.a.c.B * a.a.c.T * ((groups + 3) / 4) >= 2048;        // (two waves per SIMD)
+  const int64_t items = (int64_t)a.a.c.B * a.a.c.T * (four ? (groups + 3) / 4 : groups);
+  const unsigned blocks = (unsigned)((items + waves - 1) / waves);
+  if (a.axes.n) four ? q4_rows_kernel<T, D, 4, true><<<blocks, kRowsThreads, 0, st>>>(a) : q4_rows_kernel<T, D, 1, true><<<blocks, kRowsThreads, 0, st>>>(a);
+  else four ? q4_rows_kernel<T, D, 4, false><<<blocks, kRowsThreads, 0, st>>>(a) : q4_rows_kernel<T, D, 1, false><<<blocks, kRowsThreads, 0, st>>>(a);
 }
 
 }  // namespace sqa

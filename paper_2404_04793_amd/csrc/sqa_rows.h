@@ -48,132 +48,96 @@ struct AxesArgs {
 
 struct AxisPos { int x, y, z, w; };
 
-// What is done to each row of a head (sqa_head_prep), for lane `lane` of a wave whose rows are LPR lanes each.  AXES: a token has a
-// position on each of several axes, and each pair goes by one of them.
-template <typename T, int D, bool AXES> struct RowPrep {
+// What is done to each row of a head (sqa_head_prep), for lane `lane` of a wave whose rows are LPR lanes each.
+template <typename T, int D> struct RowPrep {
   static constexpr int E = Piece<T>::E, LPR = D / E;
   const sqa_head_prep& prep;
-  bool norm, turn, mine, first;
+  bool mine, first;
   int half, e0, step, partner;
-  float w[E];
-  uint32_t axes, other_axes;                        // AXES: of this lane's pairs, two bits each; where they differ from the first one's
-
-  __device__ __forceinline__ RowPrep(const sqa_head_prep& p, const void* weight, int lane) : prep(p) {
-    const int c = lane % LPR;
-    norm = weight != nullptr;
-    turn = p.rope != nullptr;
-    if (norm) Piece<T>::open(ld16(static_cast<const T*>(weight) + c * E), w);
-    half = p.rot_dim / 2; e0 = c * E; step = p.interleaved ? 0 : half / E;
-    mine = turn && e0 < p.rot_dim; first = e0 < half;
+  __device__ __forceinline__ RowPrep(const sqa_head_prep& p, int lane) : prep(p) {
+    half = p.rot_dim / 2; e0 = lane % LPR * E; step = p.interleaved ? 0 : half / E;
+    mine = p.rope != nullptr && e0 < p.rot_dim; first = e0 < half;
     partner = mine ? (first ? lane + step : lane - step) : lane;
   }
   __device__ __forceinline__ int first_pair() const { return mine ? (prep.interleaved ? e0 / 2 : (first ? e0 : e0 - half)) : 0; }
-  __device__ __forceinline__ void set_axes(const AxesArgs& a) {
-    const int p0 = first_pair(), word = p0 / 16, n = prep.interleaved ? E / 2 : E;
-    uint32_t v = a.axis[0];
-    if (word == 1) v = a.axis[1];
-    if (word == 2) v = a.axis[2];
-    if (word == 3) v = a.axis[3];
-    v >>= 2 * (p0 % 16);
-    axes = v & ((1u << 2 * n) - 1);
-    other_axes = mine ? axes ^ ((axes & 3) * 0x5555u & ((1u << 2 * n) - 1)) : 0;
+  // n cosines and sines of neighbouring pairs of one row of the table
+  template <int N> __device__ __forceinline__ void neighbours(const float* from, float (&cs)[E], float (&sn)[E]) const {
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
+        *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
+      }
+    } else {
+      *reinterpret_cast<float2*>(cs) = *reinterpret_cast<const float2*>(from);
+      *reinterpret_cast<float2*>(sn) = *reinterpret_cast<const float2*>(from + half);
+    }
   }
-  __device__ __forceinline__ const float* row(AxisPos at, uint32_t axis) const {
+  // What the lane's pairs turn by (E of them where pairs lie half a head apart, E / 2 where they are neighbours): from the table's row of the
+  // token's position,
+  __device__ __forceinline__ void angles_of(int64_t pos, float (&cs)[E], float (&sn)[E]) const {
+    const float* from = prep.rope + pos * prep.rot_dim + first_pair();
+    if (prep.interleaved) neighbours<E / 2>(from, cs, sn);
+    else neighbours<E>(from, cs, sn);
+  }
+  // or of its positions on the axes: a lane of the wave fetches one pair's, and they are handed out through LDS (s_wave: 128 numbers of this wave).
+  // (Fetched by each lane that needs them, one pair at a time: 58 us where this takes 50, 2 x 4500 tokens of 40 heads.)
+  __device__ __forceinline__ void angles_of(const AxesArgs& a, AxisPos at, float* s_wave, float (&cs)[E], float (&sn)[E]) const {
+    const int lane = threadIdx.x & (SQA_WAVE - 1), word = lane / 16;
+    uint32_t axis = a.axis[0];
+    if (word == 1) axis = a.axis[1];
+    if (word == 2) axis = a.axis[2];
+    if (word == 3) axis = a.axis[3];
+    axis = axis >> 2 * (lane % 16) & 3;
     int p = at.x;
     if (axis == 1) p = at.y;
     if (axis == 2) p = at.z;
     if (axis == 3) p = at.w;
-    return prep.rope + (int64_t)p * prep.rot_dim;
-  }
-  // N cosines and sines of pairs p0 ..: neighbouring numbers of one row of the table where every lane's pairs go by one axis each, else
-  // one by one
-  template <int N> __device__ __forceinline__ void angles(AxisPos at, float (&cs)[N], float (&sn)[N]) const {
-    const int p0 = first_pair();
-    if (!__any(other_axes)) {
-      const float* from = row(at, axes & 3) + p0;
-      if constexpr (N >= 4) {
-#pragma unroll
-        for (int e = 0; e < N; e += 4) {
-          *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
-          *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
-        }
-      } else {
-        *reinterpret_cast<float2*>(cs) = *reinterpret_cast<const float2*>(from);
-        *reinterpret_cast<float2*>(sn) = *reinterpret_cast<const float2*>(from + half);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float* from = row(at, axes >> 2 * e & 3) + p0 + e;
-        cs[e] = from[0]; sn[e] = from[half];
-      }
+    if (lane < half) {
+      const float* from = prep.rope + (int64_t)p * prep.rot_dim + lane;
+      s_wave[lane] = from[0];
+      s_wave[64 + lane] = from[half];
     }
+    asm volatile("" ::: "memory");                  // (a wave's LDS accesses are done in order)
+    const int p0 = first_pair();
+    const int n = prep.interleaved ? E / 2 : E;
+#pragma unroll
+    for (int e = 0; e < E; e += 2)
+      if (e < n) {
+        *reinterpret_cast<float2*>(cs + e) = *reinterpret_cast<const float2*>(s_wave + p0 + e);
+        *reinterpret_cast<float2*>(sn + e) = *reinterpret_cast<const float2*>(s_wave + 64 + p0 + e);
+      }
   }
 
-  __device__ __forceinline__ void normalise(float (&y)[E]) const {
-    if (norm) {
-      float ss = 0.f;
+  __device__ __forceinline__ void normalise(float (&y)[E], const void* weight) const {
+    if (!weight) return;
+    float w[E], ss = 0.f;
+    Piece<T>::open(ld16(static_cast<const T*>(weight) + e0), w);
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
+    for (int e = 0; e < E; ++e) ss = fmaf(y[e], y[e], ss);
 #pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
-      const float r = 1.f / sqrtf(ss * (1.f / D) + prep.eps);
+    for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, LPR);
+    const float r = 1.f / sqrtf(ss * (1.f / D) + prep.eps);
 #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
-    }
+    for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
   }
-  __device__ __forceinline__ void turn_pairs(float (&y)[E], const float* cs, const float* sn) const {           // neighbours
-    if (mine) {
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float p = y[e], q = y[e + 1];
-        y[e] = p * cs[e / 2] - q * sn[e / 2];
-        y[e + 1] = q * cs[e / 2] + p * sn[e / 2];
-      }
-    }
-  }
-  __device__ __forceinline__ void turn_halves(float (&y)[E], const float* cs, const float* sn) const {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
-      const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
-      y[e] = mine ? z : y[e];
-    }
-  }
-  // by the table's row of the token's position
-  __device__ __forceinline__ void rotate(float (&y)[E], int64_t pos) const {
-    const float* row = prep.rope + pos * prep.rot_dim;
+  __device__ __forceinline__ void turn(float (&y)[E], const float (&cs)[E], const float (&sn)[E]) const {
     if (prep.interleaved) {
       if (mine) {
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
-          const float cs = row[(e0 + e) / 2], sn = row[half + (e0 + e) / 2];
           const float p = y[e], q = y[e + 1];
-          y[e] = p * cs - q * sn;
-          y[e + 1] = q * cs + p * sn;
+          y[e] = p * cs[e / 2] - q * sn[e / 2];
+          y[e + 1] = q * cs[e / 2] + p * sn[e / 2];
         }
       }
     } else {
-      float cs[E], sn[E];
-      const float* from = row + (mine ? (first ? e0 : e0 - half) : 0);
 #pragma unroll
-      for (int e = 0; e < E; e += 4) {
-        *reinterpret_cast<float4*>(cs + e) = *reinterpret_cast<const float4*>(from + e);
-        *reinterpret_cast<float4*>(sn + e) = *reinterpret_cast<const float4*>(from + half + e);
+      for (int e = 0; e < E; ++e) {
+        const float other = step == LPR / 2 ? half_row_away<LPR>(y[e]) : __shfl(y[e], partner);
+        const float z = fmaf(y[e], cs[e], first ? -other * sn[e] : other * sn[e]);
+        y[e] = mine ? z : y[e];
       }
-      turn_halves(y, cs, sn);
-    }
-  }
-  // by its positions on the axes
-  __device__ __forceinline__ void rotate(float (&y)[E], AxisPos at) const {
-    if (prep.interleaved) {
-      float cs[E / 2], sn[E / 2];
-      angles(at, cs, sn);
-      turn_pairs(y, cs, sn);
-    } else {
-      float cs[E], sn[E];
-      angles(at, cs, sn);
-      turn_halves(y, cs, sn);
     }
   }
 };
