@@ -780,10 +780,13 @@ def _layer_at(caches: "LayerCaches", layer: int, dtype: torch.dtype, B: int, Hkv
     return C.addressof(caches.table) + layer * _LC_BYTES
 
 
-def _append(where: str, call, k: torch.Tensor, v: torch.Tensor, new_pos: int, at: int, pool: torch.Tensor, prep, q, q_out, opts, axes,
-            more: tuple) -> Optional[torch.Tensor]:
+_append_rows = _lib.sqa_chunk_append_ex
+
+
+def _append(where: str, call, shape, k: torch.Tensor, v: torch.Tensor, new_pos: int, at: int, pool: torch.Tensor, prep, q, q_out, opts, axes,
+            *more) -> Optional[torch.Tensor]:
     """chunk_append and q4_append: to the layer at address `at`, whose keys are `pool`; `more`: the call's last arguments."""
-    B, T, Hkv, D = k.shape
+    B, T, Hkv, D = shape
     dtype, dev, Hq, q_to = k.dtype, k.get_device(), Hkv, None
     if v.shape != k.shape or v.dtype != dtype:
         raise TypeError("keys and values of one shape and dtype")
@@ -827,9 +830,9 @@ def chunk_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: "LayerC
                  opts: Optional[BatchOptsStruct] = None, axes: Optional[RopeAxesStruct] = None) -> Optional[torch.Tensor]:
     """k, v [B, T, Hkv, D] at positions new_pos .. -> slots new_pos .. of the caches' layer, keys normalised and rotated on the
     way (by positions on several axes: rope_axes); with q [B, T, Hq, D] the queries too -> [B, Hq, T, D]."""
-    B, T, Hkv, D = k.shape
+    B, _, Hkv, D = shape = k.shape
     at = _layer_at(caches, layer, k.dtype, B, Hkv, D)
-    return _append("sqa_chunk_append", _lib.sqa_chunk_append_ex, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes, ())
+    return _append("sqa_chunk_append", _append_rows, shape, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes)
 
 
 def chunk_workspace(caches: "LayerCaches", Hq: int, T: int, layer: int = 0) -> torch.Tensor:
@@ -958,13 +961,13 @@ def q4_append(k: torch.Tensor, v: torch.Tensor, new_pos: int, caches: Q4Caches, 
               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, opts: Optional[BatchOptsStruct] = None,
               axes: Optional[RopeAxesStruct] = None, slot_map: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """chunk_append into a cache in 4 bits.  slot_map int32 [B, Hkv, T] (sqa_slot_map): the row that each token goes to."""
-    B, T, Hkv, D = k.shape
+    B, T, Hkv, D = shape = k.shape
     at, rows = _q4_at(caches, layer, B, Hkv, D), None
     if slot_map is not None:
         _check_out(slot_map, (B, Hkv, T), torch.int32)
         _check_device([slot_map.get_device()])
         rows = slot_map.data_ptr()
-    return _append("sqa_q4_append", _lib.sqa_q4_append, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes, (rows,))
+    return _append("sqa_q4_append", _lib.sqa_q4_append, shape, k, v, new_pos, at, caches.K[layer], prep, q, q_out, opts, axes, rows)
 
 
 def q4_read(caches: Q4Caches, first_slot: int, n: int, dtype: torch.dtype, layer: int = 0, k_out: Optional[torch.Tensor] = None,
