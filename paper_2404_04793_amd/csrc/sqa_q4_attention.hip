@@ -462,8 +462,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
       uint4 w = now.v[y];
       uint32_t power = now.vp[y];
       if (edge) {
-        odd[y] = __ballot(power > 252u);
-        if (power > 252u) { w = make_uint4(0, 0, 0, 0); power = 127; }
+        const bool left_out = power > 252u;
+        odd[y] = __ballot(left_out);
+        w.x = left_out ? 0u : w.x; w.y = left_out ? 0u : w.y; w.z = left_out ? 0u : w.z; w.w = left_out ? 0u : w.w;
+        power = left_out ? 127u : power;
       }
       const float vs = __uint_as_float(power << 23);
       const uint32_t c[4] = {w.x, w.y, w.z, w.w};
