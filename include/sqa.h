@@ -629,7 +629,7 @@ sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, i
 /* How sqa_q4_attention would lay a chunk out on the chip (host arithmetic, no GPU call).  Of `layer` only capacity is read, of opts
  * whether prompt_len and new_pos_seq are NULL. */
 typedef struct sqa_q4_plan_info {
-  int32_t rows;             /* query rows (tokens x query heads of a KV head) of a workgroup: 16 or 128              */
+  int32_t rows;             /* query rows (tokens x query heads of a KV head) of a workgroup: 16, 32 or 128          */
   int32_t waves;            /* waves of 64 threads of a workgroup; with 16 rows they share out its slots             */
   int32_t row_tiles;        /* workgroups that the rows of a unit take                                               */
   int32_t slot_splits;      /* k > 1: k workgroups share out the slots of the same rows, and the last one joins them */

@@ -339,14 +339,14 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
   }
 };
 
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_kernel(const Q4AttentionArgs a) {
+template <typename T, int D, int NW, int R>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_attention_kernel(const Q4AttentionArgs a) {
   using C = Q4Tile<T, D>;
-  constexpr int M = 16, NE = C::NE, NL = C::NL, NP = C::NP, NV = C::NV, KD = C::KD, PP = D / 4, NT = 64 * NW;
+  constexpr int M = 16 * R, NE = C::NE, NL = C::NL, NP = C::NP, NV = C::NV, KD = C::KD, PP = D / 4, NT = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) char s_stage[];   // V tiles of the waves, at the end their sums; then the table
   __shared__ float s_m[NW][M], s_l[NW][M];
   __shared__ int s_word, s_flags[NW];
-  int* const s_table = reinterpret_cast<int*>(s_stage + NW * C::VB);
+  int* const s_table = reinterpret_cast<int*>(s_stage + R * NW * C::VB);
   const sqa_q4_cache& L = a.a.L;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i = lane & 15, j = lane >> 4;
@@ -354,17 +354,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
   Q4Work<T, D, NT, M, kQ4Slots> w;
   if (!w.locate(a)) return;
   const int tile0 = w.tile0, tile1 = w.tile1, end = w.end;
-  // ---- this lane's query row
-  int t, head;
-  w.place(min(w.row0 + i, w.last_row), t, head);
-  const int back = w.s.n - 1 - t;                   // tokens of the chunk behind it
+  // ---- this lane's query rows: i of each 16
+  int back[R];                                      // tokens of the chunk behind its token
   // its elements 8 KD j .. of step x: 8 (KD j + x) ..
-  uint4 qp[NP][KD];
-  {
+  uint4 qp[R][NP][KD];
+#pragma unroll
+  for (int n = 0; n < R; ++n) {
+    int t, head;
+    w.place(min(w.row0 + 16 * n + i, w.last_row), t, head);
+    back[n] = w.s.n - 1 - t;
     const T* src = static_cast<const T*>(a.q) + (((int64_t)w.b * a.a.c.Hq + head) * a.a.c.T + t) * D + 8 * KD * j;
 #pragma unroll
     for (int x = 0; x < KD; ++x) {
-      if constexpr (sizeof(T) == 2) qp[0][x] = ld16(src + 8 * x);
+      if constexpr (sizeof(T) == 2) qp[n][0][x] = ld16(src + 8 * x);
       else {
         const uint4 lo = ld16(src + 8 * x), hi = ld16(src + 8 * x + 4);
         const uint32_t v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
@@ -372,7 +374,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
 #pragma unroll
         for (int y = 0; y < 4; ++y) split16<NP>(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1]), w[y]);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) qp[p][x] = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
+        for (int p = 0; p < NP; ++p) qp[n][p][x] = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
       }
     }
   }
@@ -422,10 +424,14 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
     }
   };
 
-  f32x4_t o[NE];
+  f32x4_t o[R][NE];
+  float m[R], l[R];
 #pragma unroll
-  for (int e = 0; e < NE; ++e) o[e] = f32x4_t{};
-  float m = -FLT_MAX, l = 0.f;
+  for (int n = 0; n < R; ++n) {
+#pragma unroll
+    for (int e = 0; e < NE; ++e) o[n][e] = f32x4_t{};
+    m[n] = -FLT_MAX; l[n] = 0.f;
+  }
   // the lane's places in the wave's tile of V: of its first row's pieces (the others by exclusive or), of its column's rows
   const int put_row = D == 128 ? lane >> 2 : lane >> 1, put_piece = D == 128 ? 4 * (lane & 3) : 4 * (lane & 1), get_row = 4 * j + i / 4;
   const uint32_t tile_at = lds_at(s_stage) + wave * C::VB;
@@ -442,15 +448,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
     asm volatile("" : "+v"(put), "+v"(get));        // (their exclusive ors take an instruction each, not registers of their own)
     // (the last one again where there are no more: a load under a condition would have the compiler wait for all loads before the next use)
     const At ahead = locate(tl + NW < tile1 ? tl + NW : tl);
-    // ---- s[kb][r]: slot 32 tl + 16 kb + 4 j + r of row i
-    f32x4_t sc[2] = {f32x4_t{}, f32x4_t{}};
+    // ---- sc[n][kb][r]: slot 32 tl + 16 kb + 4 j + r of row 16 n + i
+    f32x4_t sc[R][2];
+#pragma unroll
+    for (int n = 0; n < R; ++n) sc[n][0] = sc[n][1] = f32x4_t{};
 #pragma unroll
     for (int x = 0; x < KD; ++x) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         const bf16x8_t k = __builtin_bit_cast(bf16x8_t, q4_open(now.k[kb][x], __uint_as_float(now.kp[kb] << 23)));
 #pragma unroll
-        for (int p = 0; p < NP; ++p) sc[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8_t, qp[p][x]), sc[kb], 0, 0, 0);
+        for (int n = 0; n < R; ++n)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) sc[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8_t, qp[n][p][x]), sc[n][kb], 0, 0, 0);
       }
     }
     fetch_keys(ahead, now);               // (into registers that have just been used)
@@ -476,34 +486,38 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
     fetch_values(ahead, now);
     asm volatile("" ::: "memory");                  // (a wave's LDS accesses are done in order)
     // ---- softmax
-    if (edge) {
+    uint32_t pw[R][NV][4];
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+      f32x4_t (&s)[2] = sc[n];
+      if (edge) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[kb][r] = w.sees(tl * kQ4Slots + 16 * kb + 4 * j + r, back[n]) ? s[kb][r] : -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      if (__any(top > m[n] + a.near)) {             // the reference of a row moves when one of its logits is 2^8 times beyond it
+        top = lanes16_max(top);
+        const float to = top > m[n] + a.near ? top : m[n], keep = exp2_fast((m[n] - to) * a.scale);
+        m[n] = to;
+        l[n] *= keep;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) o[n][e] *= keep;
+      }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          sc[kb][r] = w.sees(tl * kQ4Slots + 16 * kb + 4 * j + r, back) ? sc[kb][r] : -INFINITY;
+        for (int r = 0; r < 4; r += 2) {
+          const float x = exp2_fast((s[kb][r] - m[n]) * a.scale), y = exp2_fast((s[kb][r + 1] - m[n]) * a.scale);
+          l[n] += x + y;
+          uint32_t w[NV];
+          split16<NV>(x, y, w);
+#pragma unroll
+          for (int k = 0; k < NV; ++k) pw[n][k][2 * kb + r / 2] = w[k];
+        }
     }
-    float top = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-    if (__any(top > m + a.near)) {                  // the reference of a row moves when one of its logits is 2^8 times beyond it
-      top = lanes16_max(top);
-      const float to = top > m + a.near ? top : m, keep = exp2_fast((m - to) * a.scale);
-      m = to;
-      l *= keep;
-#pragma unroll
-      for (int e = 0; e < NE; ++e) o[e] *= keep;
-    }
-    uint32_t pw[NV][4];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int r = 0; r < 4; r += 2) {
-        const float x = exp2_fast((sc[kb][r] - m) * a.scale), y = exp2_fast((sc[kb][r + 1] - m) * a.scale);
-        l += x + y;
-        uint32_t w[NV];
-        split16<NV>(x, y, w);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) pw[k][2 * kb + r / 2] = w[k];
-      }
     // ---- O^T += V^T.P^T, four blocks of 16 elements at a time
 #pragma unroll
     for (int e0 = 0; e0 < NE; e0 += 4) {
@@ -516,11 +530,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
         v[e] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
       }
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const bf16x8_t pk = __builtin_bit_cast(bf16x8_t, make_uint4(pw[k][0], pw[k][1], pw[k][2], pw[k][3]));
+      for (int n = 0; n < R; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e], pk, o[e0 + e], 0, 0, 0);
-      }
+        for (int k = 0; k < NV; ++k) {
+          const bf16x8_t pk = __builtin_bit_cast(bf16x8_t, make_uint4(pw[n][k][0], pw[n][k][1], pw[n][k][2], pw[n][k][3]));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[n][e0 + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e], pk, o[n][e0 + e], 0, 0, 0);
+        }
     }
     // the groups that are not finite, to the rows that see them
 #pragma unroll
@@ -529,29 +545,38 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2) void q4_attention_
         const int from = __builtin_ctzll(odd[y]);
         odd[y] &= odd[y] - 1;
         const int slot = tl * kQ4Slots + (D == 128 ? 16 * y + (from >> 2) : from >> 1), group = D == 128 ? from & 3 : from & 1;
-        const float add = w.sees(slot, back) ? NAN : 0.f;
 #pragma unroll
-        for (int e = 0; e < NE; ++e) o[e] += e / 2 == group ? add : 0.f;
+        for (int n = 0; n < R; ++n) {
+          const float add = w.sees(slot, back[n]) ? NAN : 0.f;
+#pragma unroll
+          for (int e = 0; e < NE; ++e) o[n][e] += e / 2 == group ? add : 0.f;
+        }
       }
     asm volatile("" ::: "memory");
   }
 
   // ---- the waves' sums joined, each row's pieces of 16 bytes in an order without bank conflicts
-  l = lanes16_sum(l);
-  if (j == 0) { s_m[wave][i] = m; s_l[wave][i] = l; }
-  __syncthreads();
-  float top = s_m[0][i];
-#pragma unroll 2
-  for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][i]);
-  const float keep = exp2_fast((m - top) * a.scale);
-  float4* const mine = reinterpret_cast<float4*>(s_stage) + (wave * M + i) * PP;
 #pragma unroll
-  for (int e = 0; e < NE; ++e) mine[(4 * e + j) ^ i] = make_float4(o[e][0] * keep, o[e][1] * keep, o[e][2] * keep, o[e][3] * keep);
+  for (int n = 0; n < R; ++n) {
+    l[n] = lanes16_sum(l[n]);
+    if (j == 0) { s_m[wave][16 * n + i] = m[n]; s_l[wave][16 * n + i] = l[n]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < R; ++n) {
+    float top = s_m[0][16 * n + i];
+#pragma unroll 2
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][16 * n + i]);
+    const float keep = exp2_fast((m[n] - top) * a.scale);
+    float4* const mine = reinterpret_cast<float4*>(s_stage) + (wave * M + 16 * n + i) * PP;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) mine[(4 * e + j) ^ i] = make_float4(o[n][e][0] * keep, o[n][e][1] * keep, o[n][e][2] * keep, o[n][e][3] * keep);
+  }
   __syncthreads();
   w.template finish<NW>(a, s_stage, s_m, s_l, &s_word, s_flags, bad);
 }
 
-// The same for many rows in bf16: 128 rows and tiles of 64 slots, two workgroups per CU.  A tile is opened once for all four waves: K and V of the
+// The same for many more rows in bf16: 128 rows and tiles of 64 slots, two workgroups per CU.  A tile is opened once for all four waves: K and V of the
 // next ones are on their way in 4 bits in registers (16 bytes of each a thread) and go to LDS as bf16 between a tile's products and
 // the barrier.  V^T.P^T of a tile follows K.Q^T of the next one.  Probabilities are rounded to one bf16, as in sqa_chunk_attention's form for many
 // rows: the products bound these calls.
@@ -755,7 +780,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   w.template finish<1>(a, s_stage, s_m, s_l, &s_word, s_flags, bad);
 }
 
-struct Q4Plan { int waves, rows, tiles, splits; };   // waves and rows of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
+struct Q4Plan { int waves, rows, tiles, splits; };   // waves and rows (16, 32, 128) of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
 static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_pos, int32_t capacity, bool uniform) {
   Q4Plan p;
   const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity, rows = (int64_t)T * (Hq / Hkv);
@@ -769,8 +794,11 @@ static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_p
     p.tiles = (int)((rows + 127) / 128);
     s = std::min(512 / wide, slots / 1024);         // (two workgroups per CU; 64 of them over 4256 slots: 4 a unit 42 us, 8 67)
   } else {
-    p.rows = 16;
-    p.tiles = (int)((rows + 15) / 16);
+    // 32 rows a workgroup (codes are opened once for both 16s, and half as many waves fit) where there is work enough for it: 32 heads over 8, us with
+    // 16 and with 32 rows: 16 x 5 tokens after 4000 29.1 and 27.1, 16 x 16 49.4 and 40.2, 64 x 5 after 1000 28.2 and 25.3, 64 x 16 47.3 and 40.6, 1 x 128
+    // after 4000 26.6 and 24.9; 16 x 5 after 500 9.7 and 12.2, 4 x 16 after 2000 14.4 and 15.7, 1 x 5 after 30000 23.5 and 27.4.
+    p.rows = dt == SQA_BF16 && rows > 16 && units * ((rows + 31) / 32) * slots >= 400000 ? 32 : 16;
+    p.tiles = (int)((rows + p.rows - 1) / p.rows);
     const int64_t items = units * p.tiles;
     // A join through the workspace costs 5 us, one inside a workgroup 1: units are shared out among waves before workgroups, and among these
     // only until every CU has one.  (256 units of 1000 slots: 8 waves 12.2 us, 4 with 3 workgroups a unit 14.0; 8 units of 30000: 32
@@ -783,7 +811,10 @@ static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_p
   return p;
 }
 // rows of sums that may be joined: no more workgroups than the plan shares out slots to
-static size_t q4_records(int T, int Hq, int Hkv) { return (int64_t)T * (Hq / Hkv) >= kQ4WideRows ? 512 * 128 : 256 * 16; }
+static size_t q4_records(int T, int Hq, int Hkv) {
+  const int64_t rows = (int64_t)T * (Hq / Hkv);
+  return rows >= kQ4WideRows ? 512 * 128 : rows > 16 ? 256 * 32 : 256 * 16;
+}
 
 static sqa_status start_q4(void (*fn)(Q4AttentionArgs), int threads, size_t lds, const Q4AttentionArgs& a, hipStream_t st) {
   if (a.a.L.block_table) lds += (size_t)(a.a.L.blocks_per_unit + 3) / 4 * 16 + 16;       // (whole tiles of block numbers)
@@ -796,9 +827,14 @@ static sqa_status start_q4(void (*fn)(Q4AttentionArgs), int threads, size_t lds,
 template <typename T, int D> static sqa_status launch_q4(const Q4Plan& p, const Q4AttentionArgs& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
     if (p.rows == 128) return start_q4(q4_attention_wide_kernel<D>, 256, Q4Wide<D>::STAGE, a, st);
-  const size_t lds = (size_t)p.waves * Q4Tile<T, D>::VB;
-  if (p.waves == 2) return start_q4(q4_attention_kernel<T, D, 2>, 128, lds, a, st);
-  return p.waves == 8 ? start_q4(q4_attention_kernel<T, D, 8>, 512, lds, a, st) : start_q4(q4_attention_kernel<T, D, 4>, 256, lds, a, st);
+  const size_t lds = (size_t)p.waves * (p.rows / 16) * Q4Tile<T, D>::VB;
+  if constexpr (sizeof(T) == 2)
+    if (p.rows == 32) {
+      if (p.waves == 2) return start_q4(q4_attention_kernel<T, D, 2, 2>, 128, lds, a, st);
+      return p.waves == 8 ? start_q4(q4_attention_kernel<T, D, 8, 2>, 512, lds, a, st) : start_q4(q4_attention_kernel<T, D, 4, 2>, 256, lds, a, st);
+    }
+  if (p.waves == 2) return start_q4(q4_attention_kernel<T, D, 2, 1>, 128, lds, a, st);
+  return p.waves == 8 ? start_q4(q4_attention_kernel<T, D, 8, 1>, 512, lds, a, st) : start_q4(q4_attention_kernel<T, D, 4, 1>, 256, lds, a, st);
 }
 
 }  // namespace sqa

@@ -116,6 +116,28 @@ def test_many_rows(sqa, D, blocked):
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
+MIDDLE = [  # B, T, before, Hq, Hkv, capacity (0: room for all), sinks -> waves, slot splits: chunks whose workgroups have 32 rows
+    (8, 9, 3200, 32, 16, 0, 0, 8, 2), (2, 127, 7000, 8, 8, 0, 0, 8, 4), (16, 20, 2500, 32, 16, 900, 4, 4, 1), (32, 9, 500, 64, 32, 0, 0, 2, 1),
+    (1, 33, 13000, 16, 16, 0, 0, 8, 8), (16, 31, 1650, 16, 16, 1600, 0, 8, 1)]
+
+
+@pytest.mark.parametrize("blocked", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_two_tiles_of_rows(sqa, D, blocked):
+    """32 rows a workgroup: every number of waves, sums joined, a second tile with one row or none but the first's last again, rings that turn."""
+    for i, (B, T, before, Hq, Hkv, cap, sink, waves, splits) in enumerate(MIDDLE):
+        gen = generator(250 + i)
+        cap = cap or before + T + 2
+        c = filled(sqa, B, Hkv, D, cap, sink, blocked, gen)
+        q = (torch.randn(B, Hq, T, D, generator=gen, device=DEV) * 1.5).bfloat16()
+        plan = sqa.q4_plan(cap, B, T, Hq, Hkv, D, "bf16", before)
+        assert (plan["rows"], plan["waves"], plan["slot_splits"]) == (32, waves, splits)
+        out, lse = sqa.q4_attention(q, before, c)
+        check(2.0 ** -15, c, q, out, lse, [before] * B, [T] * B, [cap] * B, sink, (B, T, before, Hq, Hkv))
+        again = sqa.q4_attention(q, before, c)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 RINGS = [  # capacity, sinks, T, before
     (40, 0, 1, 39), (40, 0, 1, 40), (40, 4, 1, 41), (571, 4, 1, 1500), (16, 15, 1, 90), (1, 0, 1, 7), (33, 1, 5, 31), (100, 4, 96, 400), (64, 0, 64, 64),
     (70, 6, 20, 55), (300, 2, 130, 250), (2000, 4, 3, 100000), (5000, 0, 1, 2 ** 31 - 3)]
@@ -140,9 +162,10 @@ def test_rings(sqa, dtype, D, blocked):
 
 def test_ragged(sqa):
     """Own lengths, positions and budgets; padding and sequences that take no part stay as they were."""
-    for dtype, D, T in (("bf16", 128, 9), ("f32", 64, 9), ("bf16", 64, 70), ("bf16", 128, 300)):
+    for dtype, D, T in (("bf16", 128, 9), ("f32", 64, 9), ("bf16", 64, 70), ("bf16", 128, 300), ("bf16", 64, 12), ("bf16", 128, 12)):
         dt, gen = R.DT[dtype], generator(17)
-        B, Hq, Hkv, cap, sink = 6, 24 if T == 300 else 6, 8 if T == 300 else 2, 700, 4
+        B, cap, sink = 6, 700, 4
+        Hq, Hkv = {300: (24, 8), 12: (192, 64)}.get(T, (6, 2))             # (128, 32 and 16 rows a workgroup)
         new = [T, 1, 0, T // 2, T, 1]
         before = [0, 650, 5, 100, -1, 3000]
         budget = [700, 300, 700, 505, 700, 64]
@@ -165,7 +188,7 @@ def test_what_is_not_seen_changes_nothing(sqa):
     for dtype, D in (("bf16", 128), ("bf16", 64), ("f32", 128)):
         dt = R.DT[dtype]
         for B, T, before, Hq, Hkv, cap, sink in ((2, 1, 45, 4, 2, 100, 0), (1, 7, 20, 6, 2, 60, 0), (1, 40, 200, 8, 4, 1000, 0), (1, 20, 95, 4, 2, 64, 4),
-                                                 (1, 300, 10, 8, 2, 400, 0),
+                                                 (1, 300, 10, 8, 2, 400, 0), (16, 9, 850, 64, 32, 1000, 0), (16, 9, 900, 64, 32, 850, 4),
                                                  (8, 300, 50, 32, 8, 400, 0), (8, 130, 400, 32, 8, 200, 4)):
             if dt == torch.float32 and B * T > 1000:
                 continue
@@ -216,7 +239,7 @@ def test_extreme_logits_and_queries(sqa):
 
 def test_blocks_that_are_not_there(sqa):
     """A unit with a block outside the pools, and a sequence that overwrote its own tokens: zeros, -inf, reported; the others as they were."""
-    for T, before, cap, Hq, Hkv in ((1, 40, 100, 4, 2), (1, 5000, 6000, 4, 2), (30, 60, 100, 4, 2), (200, 50, 300, 4, 2), (300, 20, 400, 64, 32), (128, 7900, 8100, 32, 4)):
+    for T, before, cap, Hq, Hkv in ((1, 40, 100, 4, 2), (1, 5000, 6000, 4, 2), (30, 60, 100, 4, 2), (200, 50, 300, 4, 2), (300, 20, 400, 64, 32), (9, 1700, 1800, 256, 64), (128, 7900, 8100, 32, 4)):
         gen = generator(31)
         B, D, g = 2, 128, Hq // Hkv
         c = filled(sqa, B, Hkv, D, cap, 0, True, gen)
