@@ -19,6 +19,10 @@
  *   Between a model's projections and these calls: sqa_qk_norm_rope, and for prompts
  *   that come in chunks (or drafts of a few tokens) sqa_chunk_append,
  *   sqa_chunk_attention and sqa_chunk_scores (sqa_chunk_plan: how they would be launched).
+ *   With positions on several axes (images and frames among the text): the *_ex forms of the first two.
+ *   The same tokens in 4 bits, kept by position alone (every token, or the sliding and
+ *   StreamingLLM policies): sqa_q4_append, sqa_q4_read, sqa_q4_attention (sqa_q4_plan).
+ *   Block tables kept on the GPU: sqa_block_assign, sqa_slot_map.
  *
  * Conventions
  *   - "DEVICE" pointers are HIP device memory owned by the caller and borrowed
@@ -592,7 +596,8 @@ typedef struct sqa_q4_cache {
 
 /* A chunk into the cache: sqa_chunk_append for 4 bits.  Keys are normalised and rotated in fp32 and rounded once, to 4 bits.
  *   slot_map : DEVICE int32 [B][Hkv][T] or NULL: the row (of the pools, or of all units' rows) that each token goes to, -1 = nowhere,
- *              as sqa_slot_map makes it once for the layers that share a table; positions then only say how tokens are rotated
+ *              as sqa_slot_map makes it once for the layers that share a table; positions then only say how tokens are rotated (a row
+ *              that two tokens are given holds parts of either)
  *   axes     : HOST or NULL: positions on several axes (sqa_rope_axes)
  * A sequence that brings more than capacity - n_sink tokens past its capacity would overwrite its own: its keys and values are left
  * out, status SQA_ERR_CAPACITY.  Tokens whose block lies outside the pools (or whose row outside the cache) are left out, status
@@ -605,7 +610,8 @@ sqa_status sqa_q4_append(const sqa_token_rows* q, const sqa_token_rows* k, const
 /* Slots first_slot .. first_slot + T - 1 of every unit as the numbers they stand for (exact in either type).  With opts, new_pos_seq is
  * the sequence's first slot and prompt_len how many are wanted.
  *   k_out, v_out : DEVICE [B][Hkv][T][D], dtype dt; either may be NULL.  Rows of slots that the unit does not have are left as they
- *                  were, status SQA_ERR_CAPACITY (a block outside the pools: SQA_ERR_SHAPE) */
+ *                  were, status SQA_ERR_CAPACITY (a block outside the pools: SQA_ERR_SHAPE).  They share no memory with each
+ *                  other or with the cache */
 sqa_status sqa_q4_read(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, int Hkv, int D, int32_t first_slot,
                        void* k_out, void* v_out, void* stream, const sqa_batch_opts* opts);
 
@@ -630,7 +636,7 @@ sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, i
  * whether prompt_len and new_pos_seq are NULL. */
 typedef struct sqa_q4_plan_info {
   int32_t rows;             /* query rows (tokens x query heads of a KV head) of a workgroup: 16, 32 or 128          */
-  int32_t waves;            /* waves of 64 threads of a workgroup; with 16 rows they share out its slots             */
+  int32_t waves;            /* waves of 64 threads of a workgroup; with 16 or 32 rows they share out its slots       */
   int32_t row_tiles;        /* workgroups that the rows of a unit take                                               */
   int32_t slot_splits;      /* k > 1: k workgroups share out the slots of the same rows, and the last one joins them */
   int32_t rounded_probs;    /* 1: probabilities are rounded to bf16 for the product with V                            */
@@ -651,7 +657,7 @@ sqa_status sqa_q4_plan(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, in
  * entry; the entries become -1 --, then the others take what they lack from the end of the list, in the same order.  A sequence that
  * the list is too short for gets nothing, and none behind it does: held stays, status SQA_ERR_CAPACITY.  held outside
  * 0 .. blocks_per_unit: that sequence is left alone, status SQA_ERR_STATE; a list with more blocks than it has room for: nothing is
- * done, status SQA_ERR_STATE.  One workgroup; B <= SQA_MAX_ASSIGN. */
+ * done, status SQA_ERR_STATE.  B <= SQA_MAX_ASSIGN.  Nothing is kept between calls, and the result does not depend on how threads run. */
 enum { SQA_MAX_ASSIGN = 8192 };
 sqa_status sqa_block_assign(int32_t* block_table, int B, int Hkv, int32_t blocks_per_unit, int32_t capacity, const int32_t* tokens,
                             int32_t* held, int32_t* free_ids, int32_t* free_count, int32_t n_blocks, int32_t* status, void* stream);

@@ -916,6 +916,8 @@ class Q4Caches:
         """capacities[l]: slots of a unit of layer l, its budget (every token: the longest length).  blocked: K and V are pools of
         16-row blocks, dealt out to the units in a seeded random order (block_seed; None = in order) with a few to spare; with
         n_blocks the pools have that many and the tables are empty (-1): block_assign fills them."""
+        for n in (n_sink, *capacities):
+            _check_position(n, "sqa_q4_cache")
         self.L, self.B, self.Hkv, self.D, self.n_sink, self.blocked = len(capacities), B, Hkv, D, n_sink, blocked
         self.capacities = list(capacities)
         self.K, self.V, self.K_scale, self.V_scale = [], [], [], []
@@ -1004,7 +1006,8 @@ def q4_workspace(caches: Q4Caches, Hq: int, T: int, layer: int = 0) -> torch.Ten
 def q4_plan(capacity: int, B: int, T: int, Hq: int, Hkv: int, D: int, dtype: str, new_pos: int = 0, ragged: bool = False) -> dict:
     """sqa_q4_plan: how q4_attention would lay a chunk out (host arithmetic, no GPU).  dtype: "bf16" or "f32"; ragged: with prompt_len or
     new_pos_seq."""
-    _check_position(new_pos, "sqa_q4_plan")
+    for n in (new_pos, capacity):
+        _check_position(n, "sqa_q4_plan")
     layer, opts, info = Q4CacheStruct(capacity=capacity), BatchOptsStruct(prompt_len=0x1000 if ragged else None), Q4PlanInfo()
     _check(_lib.sqa_q4_plan(C.addressof(layer), {"f32": 0, "bf16": 1}[dtype], B, T, Hq, Hkv, D, new_pos, C.addressof(opts), C.addressof(info)), "sqa_q4_plan")
     return {f: int(getattr(info, f)) for f, _ in Q4PlanInfo._fields_}
@@ -1054,6 +1057,7 @@ def block_assign(block_table: torch.Tensor, tokens: torch.Tensor, held: torch.Te
     if B < 1 or units % B or held.numel() != B or free_count.numel() != 1:
         raise TypeError("block_table [B * Hkv, blocks_per_unit], tokens and held [B], free_count [1]")
     _check_device([t.get_device() for t in (block_table, tokens, held, free_ids, free_count)] + ([] if status is None else [status.get_device()]))
+    _check_position(capacity, "sqa_block_assign")
     code = _lib.sqa_block_assign(block_table.data_ptr(), B, units // B, per, capacity, tokens.data_ptr(), held.data_ptr(), free_ids.data_ptr(),
                                  free_count.data_ptr(), free_ids.numel(), _ptr(status), _stream())
     if code != SQA_OK:
@@ -1081,7 +1085,8 @@ def slot_map(block_table: Optional[torch.Tensor], capacity: int, T: int, new_pos
         devices.append(block_table.get_device())
     extra = _opts_at(opts, B, devices[0])
     _check_device(devices)
-    _check_position(new_pos, "sqa_slot_map")
+    for n in (new_pos, capacity, n_sink):
+        _check_position(n, "sqa_slot_map")
     code = _lib.sqa_slot_map(_ptr(block_table), B, T, Hkv, per, capacity, n_sink, new_pos, out.data_ptr(), _stream(), extra)
     if code != SQA_OK:
         raise SqaError(code, "sqa_slot_map")

@@ -203,7 +203,7 @@ extern "C" sqa_status sqa_q4_append(const sqa_token_rows* q, const sqa_token_row
   sqa_status why;
   if (bad_q4(*layer, D, &why)) return why;
   const size_t es = dt == SQA_F32 ? 4 : 2;
-  if ((q && bad_rows(*q, B, T, es)) || bad_rows(*k, B, T, es) || bad_rows(*v, B, T, es) || !aligned16(q_out)) return SQA_ERR_SHAPE;
+  if ((q && bad_rows(*q, B, T, es)) || bad_rows(*k, B, T, es) || bad_rows(*v, B, T, es) || !aligned16(q_out) || (reinterpret_cast<uintptr_t>(slot_map) & 3u)) return SQA_ERR_SHAPE;
   Q4RowsArgs a{};
   if (prep) {
     if ((why = check_prep(*prep, D, axes, new_pos, T, opts))) return why;
@@ -240,6 +240,12 @@ extern "C" sqa_status sqa_q4_read(const sqa_q4_cache* layer, sqa_dtype dt, int B
   sqa_status why;
   if (bad_q4(*layer, D, &why)) return why;
   if (!(opts && (opts->prompt_len || opts->new_pos_seq || opts->budget_seq)) && (int64_t)first_slot + T > layer->capacity) return SQA_ERR_CAPACITY;
+  const size_t out_bytes = (size_t)B * Hkv * T * D * (dt == SQA_F32 ? 4 : 2), c_bytes = (size_t)q4_rows(*layer, B, Hkv) * D / 2;
+  if (k_out && v_out && overlap(k_out, out_bytes, v_out, out_bytes)) return SQA_ERR_SHAPE;
+  for (const void* out : {k_out, v_out})
+    if (out && (overlap(out, out_bytes, layer->K, c_bytes) || overlap(out, out_bytes, layer->V, c_bytes) ||
+                overlap(out, out_bytes, layer->K_scale, c_bytes / 16) || overlap(out, out_bytes, layer->V_scale, c_bytes / 16)))
+      return SQA_ERR_SHAPE;
   const int64_t threads = (int64_t)B * Hkv * T * (D / 8), blocks = (threads + kRowsThreads - 1) / kRowsThreads;
   if (blocks > INT32_MAX) return SQA_ERR_SHAPE;
   Q4ReadArgs a{q4_args(layer, B, T, Hkv, Hkv, first_slot, opts), k_out, v_out};

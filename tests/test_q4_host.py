@@ -82,7 +82,7 @@ def test_norm_rope_on_axes_refusals(change, code):
     (dict(dt=2), DTYPE), (dict(D=96), SHAPE), (dict(T=0), SHAPE), (dict(Hq=5), SHAPE), (dict(new_pos=-1), SHAPE), (dict(v=rows(0x300004)), SHAPE),
     (dict(layer=layer(cap=13)), "runs"), (dict(layer=layer(cap=13, sink=10)), CAP), (dict(layer=layer(cap=3)), CAP),
     (dict(k=rows(0x4000100)), SHAPE), (dict(v=rows(0x8000000)), SHAPE), (dict(q=rows(0x9000)), SHAPE), (dict(q_out=P(0x200000)), SHAPE),
-    (dict(prep=prep(n_pos=12)), SHAPE)])
+    (dict(prep=prep(n_pos=12)), SHAPE), (dict(slot_map=P(0xd002)), SHAPE)])
 def test_append_refusals(change, code):
     a = dict(q=rows(), k=rows(0x200000), v=rows(0x300000), dt=1, B=2, T=4, Hq=4, Hkv=2, D=64, prep=prep(), new_pos=10, q_out=P(0x2000000),
              layer=layer(), stream=None, opts=None, axes=None, slot_map=None)
@@ -94,7 +94,8 @@ def test_append_refusals(change, code):
 
 @pytest.mark.parametrize("change,code", [
     (dict(layer=None), NULL), (dict(k_out=None, v_out=None), NULL), (dict(layer=layer(V=None)), NULL), (dict(dt=3), DTYPE), (dict(B=0), SHAPE),
-    (dict(D=32), SHAPE), (dict(first=-1), SHAPE), (dict(first=61), CAP), (dict(k_out=P(0x100008)), SHAPE), (dict(layer=layer(sink=70)), BUDGET)])
+    (dict(D=32), SHAPE), (dict(first=-1), SHAPE), (dict(first=61), CAP), (dict(k_out=P(0x100008)), SHAPE), (dict(layer=layer(sink=70)), BUDGET),
+    (dict(v_out=P(0x100400)), SHAPE), (dict(k_out=P(0x4000100)), SHAPE), (dict(v_out=P(0x8000f00), k_out=None), SHAPE), (dict(k_out=P(0x9100), v_out=None), SHAPE)])
 def test_read_refusals(change, code):
     a = dict(layer=layer(), dt=1, B=2, T=4, Hkv=2, D=64, first=10, k_out=P(0x100000), v_out=P(0x200000), stream=None, opts=None)
     a.update(change)
@@ -205,3 +206,18 @@ def test_binding_refuses_what_it_cannot_describe():
                  lambda: sqa.slot_map(i32(4, 4), 64, 1, out=i32(2, 2, 1))):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_numbers_that_ctypes_would_cut_off():
+    one = torch.zeros(1, dtype=torch.int32)
+    for bad in (1 << 32, (1 << 32) + 5, -(1 << 31) - 1):
+        with pytest.raises(sqa.SqaError):
+            sqa.q4_plan(bad, 1, 1, 1, 1, 64, "bf16")
+        with pytest.raises(sqa.SqaError):
+            sqa.Q4Caches([16], 1, 1, 64, "cpu", n_sink=bad)
+        with pytest.raises(sqa.SqaError):
+            sqa.rope_axes(one.view(1, 1, 1), [bad])
+        with pytest.raises((sqa.SqaError, ValueError)):              # (without a GPU the tensors' device is refused first)
+            sqa.slot_map(one.view(1, 1), bad, 1, B=1, Hkv=1)
+        with pytest.raises((sqa.SqaError, ValueError)):
+            sqa.block_assign(one.view(1, 1), one, one, one, one, bad)
