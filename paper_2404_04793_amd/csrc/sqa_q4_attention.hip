@@ -33,8 +33,9 @@ struct Q4AttentionArgs {
   float4* part;                                     // [items][splits][rows][D / 4 + 1]: sums, then (m, l, bad)
   float scale;                                      // log2(e) / sqrt(D)
   float near;                                       // 8 / scale: logits that close to a row's reference do not move it
-  uint32_t group_m, heads_m, tiles_m, splits_m;     // 2^32 / g, / Hkv, / tiles, / splits: for divisions by them
+  uint32_t group_m, heads_m, tiles_m, splits_m;     // 2^32 / g, / Hkv, / tiles, / splits: for divisions by them (tiles_m: / B Hkv where tile_major)
   int tiles, splits;
+  int tile_major;                                   // all units' longest row tiles first, in place of one run of units per XCD
 };
 
 // q = x / d and what is left, for 0 <= x < 2^31 and m = 2^32 / d rounded up: the high product is one too large at most
@@ -103,18 +104,19 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
   Q4Seq s;
   int item, split, u, b, h, g, row0, last_row, parts, tile0, tile1;
   int len, end, whole;                              // slots that hold tokens, that the workgroup's rows see, that all of its rows see lie before them
-  int newest, fixed, ring;
+  int newest, fixed, ring, back_most;               // back_most: tokens of the chunk behind the first row's
   bool turned;
   uint32_t group_m;
 
   // false: there is nothing to do.  (All of it the same in all lanes.)
   __device__ __forceinline__ bool locate(const Q4AttentionArgs& a) {
     const uint32_t total = (uint32_t)(a.a.c.B * a.a.c.Hkv) * (uint32_t)(a.tiles * a.splits);
-    const uint32_t per8 = (total + 7) / 8, work = (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);                // (one run of items per XCD, see xcd_item)
+    const uint32_t per8 = (total + 7) / 8, work = a.tile_major ? blockIdx.x : (blockIdx.x & 7) * per8 + (blockIdx.x >> 3);    // (one run of items per XCD, see xcd_item)
     if (blockIdx.x >> 3 >= per8 || work >= total) return false;
     int tile;
     divide((int)work, a.splits, a.splits_m, item, split);
-    divide(item, a.tiles, a.tiles_m, u, tile);
+    if (a.tile_major) divide(item, a.a.c.B * a.a.c.Hkv, a.tiles_m, tile, u);
+    else divide(item, a.tiles, a.tiles_m, u, tile);
     tile = a.tiles - 1 - tile;                      // (the longest first)
     divide(u, a.a.c.Hkv, a.heads_m, b, h);
     g = a.a.c.g; group_m = a.group_m;
@@ -132,7 +134,8 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     turned = s.end() > s.slots;
     len = s.why ? 1 : s.len();
     end = turned ? len : min((int)s.pos + t_last + 1, len);
-    whole = turned ? (s.n == 1 ? len : 0) : min((int)s.pos + t_first + 1, len);
+    whole = min((int)s.pos + t_first + 1, len);
+    back_most = scalar(s.n - 1 - t_first);
     newest = s.why ? 0 : scalar(s.slot(s.end() - 1));
     fixed = turned ? s.sink : 0; ring = turned ? s.slots - s.sink : 0;
     const int nt = (int)((uint32_t)(end + KT - 1) / KT);
@@ -163,6 +166,16 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     int behind = newest - slot;
     behind += behind < 0 ? ring : 0;
     return (bool)((int)(slot < len) & ((int)(slot < fixed) | (int)(behind >= back)));
+  }
+  // Does some row not see some slot of tile tl?  (The same in all lanes.)  In a ring that has turned: by how far its newest slot lies behind the newest.
+  __device__ __forceinline__ bool is_edge(int tl) const {
+    const int from = tl * KT, to = from + KT;
+    if (!turned) return to > whole;
+    const int hi = min(to, len) - 1, lo = max(from, fixed);
+    int behind = newest - hi;
+    behind += behind < 0 ? ring : 0;
+    behind = (int)(lo <= newest) & (int)(newest <= hi) ? 0 : behind;
+    return (bool)((int)(to > len) | ((int)(lo <= hi) & (int)(behind < back_most)));
   }
   // block numbers of this workgroup's slots to LDS; does one of them lie outside the pools?
   __device__ __forceinline__ bool stage_blocks(const sqa_q4_cache& L, int* s_table, int* s_flags) const {
@@ -466,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
     }
     fetch_keys(ahead, now);               // (into registers that have just been used)
     // ---- V to LDS as bf16
-    const bool edge = (tl + 1) * kQ4Slots > w.whole;
+    const bool edge = w.is_edge(tl);
     uint64_t odd[NL] = {};                          // (lanes whose group is not finite, where not every row sees it)
 #pragma unroll
     for (int y = 0; y < NL; ++y) {
@@ -640,7 +653,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
     for (int p = 0; p < KD; ++p)
       *(lds_v4u_t*)(uintptr_t)(lds0 + tile + row * R::RB + (((KD * part + p) ^ swizzle) << 4)) = __builtin_bit_cast(v4u_t, q4_open(x.c[p], power));
   };
-  auto is_edge = [&](int j) { return (w.tile0 + j + 1) * KT > w.whole; };                // not all rows of the workgroup see all of the tile
+  auto is_edge = [&](int j) { return w.is_edge(w.tile0 + j); };
   auto put_keys = [&](const Codes& x, int j) { put(x, (j & 1) * TILE, R::k_swizzle(row)); };
   auto put_values = [&](Codes x, int j) {
     if (is_edge(j)) {                               // a slot that a row does not see has probability 0, but 0 x NaN is NaN: see values()
@@ -782,7 +795,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   w.template finish<1>(a, s_stage, s_m, s_l, &s_word, s_flags, bad);
 }
 
-struct Q4Plan { int waves, rows, tiles, splits; };   // waves and rows (16, 32, 128) of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
+struct Q4Plan { int waves, rows, tiles, splits; bool tile_major; };   // waves and rows (16, 32, 128) of a workgroup, row tiles of a unit, workgroups that share out the slots of the same rows
 static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_pos, int32_t capacity, bool uniform) {
   Q4Plan p;
   const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity, rows = (int64_t)T * (Hq / Hkv);
@@ -795,10 +808,15 @@ static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_p
     p.rows = 128; p.waves = 4;
     p.tiles = (int)((rows + 127) / 128);
     s = std::min(512 / wide, slots / 1024);         // (two workgroups per CU; 64 of them over 4256 slots: 4 a unit 42 us, 8 67)
+    // The longest row tiles of all units first, where a chunk's rows differ much in what they see: an XCD's units in turn leave some XCDs with the long ones.
+    // (us, units in turn and the longest first: 8 x 2048 tokens of 32 heads 371 and 338, 34 x up to 936 of 16 over 4 156 and 139, 13 x up to 1019 of 6 over 2 45
+    // and 36, 4 x up to 1067 after 254 49 and 43; 2048 after 6144 482 and 481; 40 x up to 417 of 5 over 1 after 9155 384 and 400, units' tiles meeting in L2.)
+    p.tile_major = (int64_t)T * 4 >= slots;
   } else {
     // 32 rows a workgroup (codes are opened once for both 16s, and half as many waves fit) where there is work enough for it: 32 heads over 8, us with
     // 16 and with 32 rows: 16 x 5 tokens after 4000 29.1 and 27.1, 16 x 16 49.4 and 40.2, 64 x 5 after 1000 28.2 and 25.3, 64 x 16 47.3 and 40.6, 1 x 128
     // after 4000 26.6 and 24.9; 16 x 5 after 500 9.7 and 12.2, 4 x 16 after 2000 14.4 and 15.7, 1 x 5 after 30000 23.5 and 27.4.
+    p.tile_major = false;
     p.rows = dt == SQA_BF16 && rows > 16 && units * ((rows + 31) / 32) * slots >= 400000 ? 32 : 16;
     p.tiles = (int)((rows + p.rows - 1) / p.rows);
     const int64_t items = units * p.tiles;
@@ -872,8 +890,8 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   a.scale = (float)(1.4426950408889634 / sqrt((double)D));
   a.near = 8.f / a.scale;
   auto reciprocal = [](int d) { return 0xffffffffu / (uint32_t)d + 1; };
-  a.group_m = reciprocal(a.a.c.g); a.heads_m = reciprocal(Hkv); a.tiles_m = reciprocal(p.tiles); a.splits_m = reciprocal(p.splits);
-  a.tiles = p.tiles; a.splits = p.splits;
+  a.group_m = reciprocal(a.a.c.g); a.heads_m = reciprocal(Hkv); a.tiles_m = reciprocal(p.tile_major ? B * Hkv : p.tiles); a.splits_m = reciprocal(p.splits);
+  a.tiles = p.tiles; a.splits = p.splits; a.tile_major = p.tile_major;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dt == SQA_F32) return D == 64 ? launch_q4<float, 64>(p, a, st) : launch_q4<float, 128>(p, a, st);
   return D == 64 ? launch_q4<bf16_t, 64>(p, a, st) : launch_q4<bf16_t, 128>(p, a, st);
