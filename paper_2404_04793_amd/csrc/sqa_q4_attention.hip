@@ -591,9 +591,11 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
 }
 
 // The same for many more rows in bf16: 128 rows and tiles of 64 slots, two workgroups per CU.  A tile is opened once for all four waves: K and V of the
-// next ones are on their way in 4 bits in registers (16 bytes of each a thread) and go to LDS as bf16 between a tile's products and
-// the barrier.  V^T.P^T of a tile follows K.Q^T of the next one.  Probabilities are rounded to one bf16, as in sqa_chunk_attention's form for many
-// rows: the products bound these calls.
+// next ones are on their way in 4 bits in registers (16 bytes of each a thread) and are opened into LDS as bf16 between the products K.Q^T of a
+// tile; the exponentials of a tile stand between the products V^T.P^T of the one before.  (Step by step, as the order is written: left to itself, or told by
+// groups, the compiler gathers products and vector instructions.  2048 tokens of 64 heads over 8 after 6144 482 -> 463 us, 4 x up to 1067 of 12 over 3 44 ->
+// 40; with priority for either part 461 and 40, but 8 x 233 of 256 over 32 104 -> 108.)  Probabilities are rounded to one bf16, as in
+// sqa_chunk_attention's form for many rows: the products bound these calls.
 template <int D> struct Q4Wide {
   using R = TileRows<bf16_t, D>;
   static constexpr int Slots = 64, Rows = 128, TILE = Slots * R::RB;
@@ -630,7 +632,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   }
   const bool bad = w.stage_blocks(L, s_table, s_flags);
 
-  // ---- a thread's part of a tile: 8 KD numbers of row tid / 4
+  // ---- a thread's part of a tile: 8 KD numbers of a row, a wave the same part of all 64
   const int row = lane, part = wave;
   const int64_t unit_row = (int64_t)w.u * L.capacity;
   auto row_of = [&](int j) {                        // (slots behind the last one: that one again)
@@ -647,23 +649,16 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
     return x;
   };
   const uint32_t lds0 = lds_at(s_stage);
-  auto put = [&](const Codes& x, uint32_t tile, int swizzle) {
-    const float power = __uint_as_float(x.power << 23);
-#pragma unroll
-    for (int p = 0; p < KD; ++p)
-      *(lds_v4u_t*)(uintptr_t)(lds0 + tile + row * R::RB + (((KD * part + p) ^ swizzle) << 4)) = __builtin_bit_cast(v4u_t, q4_open(x.c[p], power));
+  auto put_piece = [&](const Codes& x, int p, uint32_t tile, int swizzle) {
+    *(lds_v4u_t*)(uintptr_t)(lds0 + tile + row * R::RB + (((KD * part + p) ^ swizzle) << 4)) = __builtin_bit_cast(v4u_t, q4_open(x.c[p], __uint_as_float(x.power << 23)));
   };
   auto is_edge = [&](int j) { return w.is_edge(w.tile0 + j); };
-  auto put_keys = [&](const Codes& x, int j) { put(x, (j & 1) * TILE, R::k_swizzle(row)); };
-  auto put_values = [&](Codes x, int j) {
-    if (is_edge(j)) {                               // a slot that a row does not see has probability 0, but 0 x NaN is NaN: see values()
-      const bool odd = x.power > 252u;
-      s_odd[j & 1][4 * row + part] = odd;
+  auto leave_out = [&](Codes& x, int j) {           // a slot that a row does not see has probability 0, but 0 x NaN is NaN: see odd_values()
+    const bool odd = x.power > 252u;
+    s_odd[j & 1][4 * row + part] = odd;
 #pragma unroll
-      for (int p = 0; p < KD; ++p) x.c[p] = odd ? 0u : x.c[p];
-      x.power = odd ? 127u : x.power;
-    }
-    put(x, (2 + (j & 1)) * TILE, C::v_swizzle(row));
+    for (int p = 0; p < KD; ++p) x.c[p] = odd ? 0u : x.c[p];
+    x.power = odd ? 127u : x.power;
   };
 
   // ---- the lane's places in a tile of K and of V
@@ -682,16 +677,28 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   for (int e = 0; e < NB; ++e) o[e] = f32x16_t{};
   float m = -FLT_MAX, l = 0.f;                       // m: a reference that a row's largest logit is near, not always that logit
 
-  auto keys = [&](int j) {                           // sc = K.Q^T of tile j
+  Codes kc, vc;
+  // sc = K.Q^T of tile j, and between the products V of tile j and K of the next one opened into LDS
+  auto keys = [&](int j) {
+    if (is_edge(j)) leave_out(vc, j);
     const char* const Kt = s_stage + (j & 1) * TILE;
+    constexpr int N = 2 * NS, AHEAD = 3;
+    uint4 k[AHEAD + 1];
+    auto fetch_k = [&](int n) { k[n % (AHEAD + 1)] = *reinterpret_cast<const uint4*>(Kt + k_at[n / 2] + 32 * (n % 2) * R::RB); };
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      uint4 k[NS];
+    for (int n = 0; n < AHEAD; ++n) fetch_k(n);
+    sc[0] = sc[1] = f32x16_t{};
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < NS; ++x) k[x] = *reinterpret_cast<const uint4*>(Kt + k_at[x] + 32 * kb * R::RB);
-      sc[kb] = f32x16_t{};
-#pragma unroll
-      for (int x = 0; x < NS; ++x) mma_piece<T>(k[x], q.p[x], sc[kb]);
+    for (int n = 0; n < N; ++n) {
+      if (n + AHEAD < N) fetch_k(n + AHEAD);
+      mma_piece<T>(k[n % (AHEAD + 1)], q.p[n / 2], sc[n % 2]);
+      if (n % 2) {
+        const int p = n / 2;
+        if (p < KD) put_piece(vc, p, (2 + (j & 1)) * TILE, C::v_swizzle(row));
+        else put_piece(kc, p - KD, ((j + 1) & 1) * TILE, R::k_swizzle(row));
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   auto values = [&](int j) {                         // o += V^T.P^T of tile j
@@ -706,6 +713,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
         const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[ks], o[e], 0, 0, 0);
       }
+  };
+  auto odd_values = [&](int j) {
     if (is_edge(j)) {                               // the groups that are not finite, to the rows that see them
       uint64_t odd = __ballot(reinterpret_cast<const uint32_t*>(s_odd[j & 1])[lane] != 0);            // (a lane per slot)
       while (odd) {
@@ -718,7 +727,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
       }
     }
   };
-  auto softmax = [&](int j) {
+  auto softmax = [&](int j, bool before) {           // p of tile j; before: and o += V^T.P^T of the tile before it
     if (is_edge(j)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -733,6 +742,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
     top = other_half_max(top);
     // the reference of a row moves when one of its logits is 2^8 times beyond it: seldom after the first tiles
     if (const bool beyond = top > m + a.near; __any(beyond)) {
+      if (before) { values(j - 1); odd_values(j - 1); }
+      before = false;
       const float to = beyond ? top : m, keep = exp2_fast((m - to) * a.scale);
       m = to;
       l *= keep;
@@ -748,39 +759,69 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
       off = far ? 0.f : off;
     }
     float l0 = 0.f, l1 = 0.f;
+    if (!before) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
+        for (int i = 0; i < 16; i += 2) {
+          const float x = exp2_fast(fmaf(sc[kb][i], a.scale, -off)), y = exp2_fast(fmaf(sc[kb][i + 1], a.scale, -off));
+          l0 += x; l1 += y;
+          p[2 * kb + i / 8][i % 8] = (__bf16)x; p[2 * kb + i / 8][i % 8 + 1] = (__bf16)y;
+        }
+    } else {
+      bf16x8_t pn[4];
+      const char* const Vt = s_stage + (2 + ((j - 1) & 1)) * TILE;
+      constexpr int N = 4 * NB, AHEAD = 3;           // products; fragments of V on their way
+      s16x4_t vlo[AHEAD + 1], vhi[AHEAD + 1];
+      auto fetch_v = [&](int n) {
+        const char* at = Vt + v_at[n % NB] + 16 * (n / NB) * R::RB;
+        vlo[n % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at));
+        vhi[n % (AHEAD + 1)] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 8 * R::RB));
+      };
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) fetch_v(n);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        if (n < N) {
+          if (n + AHEAD < N) fetch_v(n + AHEAD);
+          const bf16x8_t v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(vlo[n % (AHEAD + 1)], vhi[n % (AHEAD + 1)], 0, 1, 2, 3, 4, 5, 6, 7));
+          o[n % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[n / NB], o[n % NB], 0, 0, 0);
+        }
+        const int kb = n / 8, i = 2 * n % 16;
         const float x = exp2_fast(fmaf(sc[kb][i], a.scale, -off)), y = exp2_fast(fmaf(sc[kb][i + 1], a.scale, -off));
         l0 += x; l1 += y;
-        p[2 * kb + i / 8][i % 8] = (__bf16)x; p[2 * kb + i / 8][i % 8 + 1] = (__bf16)y;
+        pn[2 * kb + i / 8][i % 8] = (__bf16)x; pn[2 * kb + i / 8][i % 8 + 1] = (__bf16)y;
+        __builtin_amdgcn_sched_barrier(0);
       }
+      // (without it the compiler takes these exponentials out again, to be one with those of the other branch)
+      asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(pn[2]), "+v"(pn[3]), "+v"(l0), "+v"(l1));
+#pragma unroll
+      for (int x = 0; x < 4; ++x) p[x] = pn[x];
+      odd_values(j - 1);
+    }
     l += l0 + l1;
   };
 
   const int n = w.tile1 - w.tile0;
-  Codes kc, vc;
   {
     const int64_t at = row_of(0);
-    put_keys(fetch(L.K, L.K_scale, at), 0);
+    kc = fetch(L.K, L.K_scale, at);
+#pragma unroll
+    for (int p = 0; p < KD; ++p) put_piece(kc, p, 0, R::k_swizzle(row));
     vc = fetch(L.V, L.V_scale, at);
     kc = fetch(L.K, L.K_scale, row_of(min(1, n - 1)));
   }
   __syncthreads();
   for (int j = 0; j < n; ++j) {
-    __builtin_amdgcn_s_setprio(1);                   // the wave that has products to give goes first
     keys(j);
-    if (j > 0) values(j - 1);
-    __builtin_amdgcn_s_setprio(0);
-    softmax(j);
-    put_keys(kc, j + 1);
-    put_values(vc, j);
     kc = fetch(L.K, L.K_scale, row_of(min(j + 2, n - 1)));           // (the last one again where there are no more)
     vc = fetch(L.V, L.V_scale, row_of(min(j + 1, n - 1)));
+    softmax(j, j > 0);
     __syncthreads();
   }
   values(n - 1);
+  odd_values(n - 1);
   __syncthreads();
 
   // ---- sums to LDS as rows
