@@ -22,7 +22,7 @@ typedef __attribute__((address_space(1))) const uint8_t g_u8_t;
 typedef __attribute__((address_space(3))) v4u_t lds_v4u_t;
 
 constexpr int kQ4Splits = 64;                       // workgroups that share out a unit's slots: a lane each when they are joined
-constexpr int kQ4WideRows = 128;                    // rows of a unit from which on a workgroup may take 128 of them (bf16)
+constexpr int kQ4WideRows = 65;                     // rows of a unit from which on a workgroup may take 128 of them (bf16)
 
 struct Q4AttentionArgs {
   Q4Args a;
@@ -842,10 +842,11 @@ static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_p
   const int64_t slots = uniform ? std::min<int64_t>((int64_t)new_pos + T, capacity) : capacity, rows = (int64_t)T * (Hq / Hkv);
   const int64_t units = (int64_t)B * Hkv, wide = units * ((rows + 127) / 128);
   int64_t s;
-  // 128 rows a workgroup where they fill the chip, or nearly do over many slots (a join of 128 rows costs what some hundred slots do).  32 heads over
-  // 8, us with 16 and with 128 rows: 8 x 128 tokens after 2000 (256 workgroups) 76 and 52, 8 x 64 45 and 38, 8 x 32 26 and 31; 16 x 64 after 500 28
-  // and 22, 16 x 32 17 and 21; 1 x 256 after 4000 45 and 42, 1 x 128 28 and 56; 1 x 128 after 30000 144 and 117, 1 x 64 80 and 98.
-  if (dt == SQA_BF16 && rows >= kQ4WideRows && (wide >= 256 || (wide >= 32 && wide * slots >= 250000))) {
+  // 128 rows a workgroup where they fill the chip, or nearly do over many slots (a join of 128 rows costs what some hundred slots do), and half of them or more
+  // are there.  32 heads over 8, us with 16, 32 and 128 rows: 16 x 24 tokens after 4000 65, 75 and 60, 64 x 24 after 1000 75, 73 and 51 (64 x 33 with 32 rows
+  // 105, 64 x 48 with 128 94), 16 x 64 after 500 29, 26 and 23, 8 x 64 after 2000 48, 40 and 38, 1 x 256 after 30000 288, 214 and 172; 64 x 16 after 1000 47, 41 and 45, 16 x 32 after 500 17, 17 and 20, 1 x 256 after
+  // 4000 48, 38 and 41, 1 x 128 after 30000 150, 116 and 126.
+  if (dt == SQA_BF16 && rows >= kQ4WideRows && (wide >= 256 || (wide >= 64 && wide * slots >= 300000))) {
     p.rows = 128; p.waves = 4;
     p.tiles = (int)((rows + 127) / 128);
     s = std::min(512 / wide, slots / 1024);         // (two workgroups per CU; 64 of them over 4256 slots: 4 a unit 42 us, 8 67)

@@ -95,7 +95,7 @@ def test_attention(sqa, dtype, D, blocked):
 
 
 WIDE = [  # B, T, before, Hq, Hkv, capacity (0: room for all), sinks -> slot splits: chunks whose workgroups have 128 rows
-    (4, 520, 70, 16, 8, 0, 0, 1), (8, 300, 0, 32, 8, 0, 0, 1), (16, 129, 63, 16, 16, 0, 0, 1), (1, 128, 8000, 32, 4, 0, 0, 7), (2, 257, 7000, 16, 8, 0, 0, 6),
+    (4, 520, 70, 16, 8, 0, 0, 1), (8, 300, 0, 32, 8, 0, 0, 1), (16, 129, 63, 16, 16, 0, 0, 1), (32, 96, 63, 16, 16, 0, 0, 1), (1, 128, 8000, 64, 8, 0, 0, 7), (2, 257, 7000, 16, 8, 0, 0, 6),
     (8, 130, 400, 32, 8, 200, 4, 1), (16, 128, 190, 16, 16, 300, 7, 1)]
 
 

@@ -141,7 +141,9 @@ FORMS = [  # capacity, B, T, Hq, Hkv, new_pos, dtype -> rows, waves, row tiles, 
     (4000, 1, 128, 32, 8, 3000, "bf16", (32, 8, 16, 2)), (4000, 1, 128, 32, 8, 2900, "bf16", (16, 8, 32, 1)),
     (4095, 16, 5, 32, 8, 4090, "f32", (16, 8, 2, 1)), (4095, 16, 4, 32, 8, 4090, "bf16", (16, 8, 1, 2)), (900, 16, 20, 32, 16, 2500, "bf16", (32, 4, 2, 1)),
     (510, 32, 9, 64, 32, 500, "bf16", (32, 2, 1, 1)), (600, 4, 520, 16, 8, 70, "bf16", (128, 4, 9, 1)), (8192, 4, 300, 64, 8, 7800, "bf16", (128, 4, 19, 1)),
-    (8200, 1, 128, 32, 4, 8000, "bf16", (128, 4, 8, 7)), (8200, 1, 128, 32, 4, 8000, "f32", (16, 8, 64, 1)), (1 << 30, 1, 1, 1, 1, 5, "bf16", (16, 8, 1, 1))]
+    (8200, 1, 128, 64, 8, 8000, "bf16", (128, 4, 8, 7)), (8200, 1, 128, 32, 4, 8000, "bf16", (32, 8, 32, 2)),
+    (1100, 64, 24, 32, 8, 1000, "bf16", (128, 4, 1, 1)), (1100, 64, 16, 32, 8, 1000, "bf16", (32, 2, 2, 1)), (1100, 64, 33, 32, 8, 1000, "bf16", (128, 4, 2, 1)),
+    (300, 16, 129, 16, 16, 63, "bf16", (128, 4, 2, 1)), (300, 16, 129, 16, 16, 63, "f32", (16, 2, 9, 1)), (8200, 1, 128, 32, 4, 8000, "f32", (16, 8, 64, 1)), (1 << 30, 1, 1, 1, 1, 5, "bf16", (16, 8, 1, 1))]
 
 
 @pytest.mark.parametrize("capacity,B,T,Hq,Hkv,new_pos,dtype,want", FORMS)
