@@ -105,6 +105,7 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
   int item, split, u, b, h, g, row0, last_row, parts, tile0, tile1;
   int len, end, whole;                              // slots that hold tokens, that the workgroup's rows see, that all of its rows see lie before them
   int newest, fixed, ring, back_most;               // back_most: tokens of the chunk behind the first row's
+  int gap0, gap;                                    // tiles gap0 .. gap0 + gap - 1 no row of the workgroup sees: left out of the count
   bool turned;
   uint32_t group_m;
 
@@ -138,7 +139,21 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     back_most = scalar(s.n - 1 - t_first);
     newest = s.why ? 0 : scalar(s.slot(s.end() - 1));
     fixed = turned ? s.sink : 0; ring = turned ? s.slots - s.sink : 0;
-    const int nt = (int)((uint32_t)(end + KT - 1) / KT);
+    int nt = (int)((uint32_t)(end + KT - 1) / KT);
+    gap0 = gap = 0;
+    if (turned && !s.why) {
+      // the tokens behind the last row's, `hidden` of them: slots up to the newest, and where these begin at the ring's start its end too.  One run of
+      // whole tiles among them, the longer one.
+      const int hidden = scalar(s.n - 1 - t_last), low = min(hidden, newest + 1 - fixed), high = hidden - low;
+      auto leave = [&](int from, int to) {
+        const int x = (from + KT - 1) / KT, y = to == len ? nt : to / KT;
+        if (y - x > gap) { gap0 = x; gap = y - x; }
+      };
+      leave(newest + 1 - low, newest + 1);
+      if (high > 0) leave(len - high, len);
+      nt -= gap;
+    }
+    gap0 = scalar(gap0); gap = scalar(gap);
     int per = nt, rest;
     parts = 1;
     if (a.splits > 1) {
@@ -155,6 +170,8 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     }
     return true;
   }
+  // the i-th tile of those that some row sees
+  __device__ __forceinline__ int tile_of(int i) const { return i + (i >= gap0 ? gap : 0); }
   __device__ __forceinline__ void place(int r, int& t, int& head) const {
     int x;
     divide(r, g, group_m, t, x);
@@ -184,7 +201,7 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     const int32_t* table = L.block_table + (int64_t)u * L.blocks_per_unit;
     bool bad = false;
     for (int x = threadIdx.x; x < BPT * (tile1 - tile0); x += NT) {
-      const int e = BPT * tile0 + x;
+      const int e = BPT * tile_of(tile0 + x / BPT) + x % BPT;
       int blk = e * SQA_BLOCK_SLOTS < end ? table[e] : 0;
       if ((unsigned)blk >= (unsigned)L.n_blocks) { bad = true; blk = 0; }
       s_table[x] = blk;
@@ -396,17 +413,16 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
   const bool bad = w.stage_blocks(L, s_table, s_flags);
   // ---- rows of 16 neighbouring slots lie one after the other; slots behind the last one are read as that one again
   const int64_t unit_row = (int64_t)w.u * L.capacity;
-  auto row_of = [&](int slot) {                     // (the same in all lanes)
-    return L.block_table ? (int64_t)__builtin_amdgcn_readfirstlane(s_table[slot / SQA_BLOCK_SLOTS - 2 * tile0]) * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS
-                         : unit_row + slot;
+  auto row_of = [&](int tl, int slot, int k) {      // (the same in all lanes)
+    return L.block_table ? (int64_t)__builtin_amdgcn_readfirstlane(s_table[2 * (tl - tile0) + k]) * SQA_BLOCK_SLOTS : unit_row + slot + 16 * k;
   };
   struct At { int64_t row[2]; int last[2]; };       // of a tile's halves: the first row, and the last that there is behind it
   auto locate = [&](int tl) {
-    const int slot = tl * kQ4Slots;
+    const int slot = w.tile_of(tl) * kQ4Slots;
     At x;
-    x.row[0] = row_of(slot); x.last[0] = min(end - 1 - slot, 15);
+    x.row[0] = row_of(tl, slot, 0); x.last[0] = min(end - 1 - slot, 15);
     const bool two = end - slot > 16;               // (a half without a slot: the first half again)
-    x.row[1] = two ? row_of(slot + 16) : x.row[0]; x.last[1] = two ? min(end - 17 - slot, 15) : x.last[0];
+    x.row[1] = two ? row_of(tl, slot, 1) : x.row[0]; x.last[1] = two ? min(end - 17 - slot, 15) : x.last[0];
     return x;
   };
   struct Codes { uint32_t k[2][KD], kp[2], vp[NL]; uint4 v[NL]; } now;
@@ -462,7 +478,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
     asm volatile("" : "+v"(put), "+v"(get));        // (their exclusive ors take an instruction each, not registers of their own)
     // (the last one again where there are no more: a load under a condition would have the compiler wait for all loads before the next use)
     const At ahead = locate(tl + NW < tile1 ? tl + NW : tl);
-    // ---- sc[n][kb][r]: slot 32 tl + 16 kb + 4 j + r of row 16 n + i
+    // ---- sc[n][kb][r]: slot first + 16 kb + 4 j + r of row 16 n + i
     f32x4_t sc[R][2];
 #pragma unroll
     for (int n = 0; n < R; ++n) sc[n][0] = sc[n][1] = f32x4_t{};
@@ -479,7 +495,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
     }
     fetch_keys(ahead, now);               // (into registers that have just been used)
     // ---- V to LDS as bf16
-    const bool edge = w.is_edge(tl);
+    const int first = w.tile_of(tl) * kQ4Slots;
+    const bool edge = w.is_edge(w.tile_of(tl));
     uint64_t odd[NL] = {};                          // (lanes whose group is not finite, where not every row sees it)
 #pragma unroll
     for (int y = 0; y < NL; ++y) {
@@ -509,7 +526,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            s[kb][r] = w.sees(tl * kQ4Slots + 16 * kb + 4 * j + r, back[n]) ? s[kb][r] : -INFINITY;
+            s[kb][r] = w.sees(first + 16 * kb + 4 * j + r, back[n]) ? s[kb][r] : -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
       if (__any(top > m[n] + a.near)) {             // the reference of a row moves when one of its logits is 2^8 times beyond it
@@ -558,7 +575,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 && R == 1 ? 4 : 2) void q4_
       while (odd[y]) {
         const int from = __builtin_ctzll(odd[y]);
         odd[y] &= odd[y] - 1;
-        const int slot = tl * kQ4Slots + (D == 128 ? 16 * y + (from >> 2) : from >> 1), group = D == 128 ? from & 3 : from & 1;
+        const int slot = first + (D == 128 ? 16 * y + (from >> 2) : from >> 1), group = D == 128 ? from & 3 : from & 1;
 #pragma unroll
         for (int n = 0; n < R; ++n) {
           const float add = w.sees(slot, back[n]) ? NAN : 0.f;
@@ -636,8 +653,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   const int row = lane, part = wave;
   const int64_t unit_row = (int64_t)w.u * L.capacity;
   auto row_of = [&](int j) {                        // (slots behind the last one: that one again)
-    const int slot = min((w.tile0 + j) * KT + row, w.end - 1);
-    return L.block_table ? (int64_t)s_table[slot / SQA_BLOCK_SLOTS - KT / SQA_BLOCK_SLOTS * w.tile0] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit_row + slot;
+    const int from = w.tile_of(w.tile0 + j) * KT, at = min(row, w.end - 1 - from), slot = from + at;
+    return L.block_table ? (int64_t)s_table[KT / SQA_BLOCK_SLOTS * j + at / SQA_BLOCK_SLOTS] * SQA_BLOCK_SLOTS + slot % SQA_BLOCK_SLOTS : unit_row + slot;
   };
   struct Codes { uint32_t c[KD], power; };
   auto fetch = [&](const void* codes, const uint8_t* powers, int64_t at) {
@@ -652,7 +669,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   auto put_piece = [&](const Codes& x, int p, uint32_t tile, int swizzle) {
     *(lds_v4u_t*)(uintptr_t)(lds0 + tile + row * R::RB + (((KD * part + p) ^ swizzle) << 4)) = __builtin_bit_cast(v4u_t, q4_open(x.c[p], __uint_as_float(x.power << 23)));
   };
-  auto is_edge = [&](int j) { return w.is_edge(w.tile0 + j); };
+  auto is_edge = [&](int j) { return w.is_edge(w.tile_of(w.tile0 + j)); };
   auto leave_out = [&](Codes& x, int j) {           // a slot that a row does not see has probability 0, but 0 x NaN is NaN: see odd_values()
     const bool odd = x.power > 252u;
     s_odd[j & 1][4 * row + part] = odd;
@@ -720,7 +737,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
       while (odd) {
         const int r = __builtin_ctzll(odd);
         odd &= odd - 1;
-        const float add = w.sees((w.tile0 + j) * KT + r, back) ? NAN : 0.f;
+        const float add = w.sees(w.tile_of(w.tile0 + j) * KT + r, back) ? NAN : 0.f;
 #pragma unroll
         for (int e = 0; e < NB; ++e)
           if (s_odd[j & 1][4 * r + 4 / KD * e]) o[e] += add;
@@ -729,10 +746,11 @@ template <int D> __global__ __launch_bounds__(256, 2) void q4_attention_wide_ker
   };
   auto softmax = [&](int j, bool before) {           // p of tile j; before: and o += V^T.P^T of the tile before it
     if (is_edge(j)) {
+      const int first = w.tile_of(w.tile0 + j) * KT;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[kb][i] = w.sees((w.tile0 + j) * KT + 32 * kb + c_row(i, half), back) ? sc[kb][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) sc[kb][i] = w.sees(first + 32 * kb + c_row(i, half), back) ? sc[kb][i] : -INFINITY;
     }
     float top = sc[0][0];
 #pragma unroll

@@ -96,7 +96,7 @@ def test_attention(sqa, dtype, D, blocked):
 
 WIDE = [  # B, T, before, Hq, Hkv, capacity (0: room for all), sinks -> slot splits: chunks whose workgroups have 128 rows
     (4, 520, 70, 16, 8, 0, 0, 1), (8, 300, 0, 32, 8, 0, 0, 1), (16, 129, 63, 16, 16, 0, 0, 1), (32, 96, 63, 16, 16, 0, 0, 1), (1, 128, 8000, 64, 8, 0, 0, 7), (2, 257, 7000, 16, 8, 0, 0, 6),
-    (8, 130, 400, 32, 8, 200, 4, 1), (16, 128, 190, 16, 16, 300, 7, 1)]
+    (8, 130, 400, 32, 8, 200, 4, 1), (4, 900, 1500, 16, 4, 1000, 4, 1), (3, 1000, 600, 12, 12, 1000, 0, 1), (16, 128, 190, 16, 16, 300, 7, 1)]
 
 
 @pytest.mark.parametrize("blocked", [False, True])
@@ -140,7 +140,9 @@ def test_two_tiles_of_rows(sqa, D, blocked):
 
 RINGS = [  # capacity, sinks, T, before
     (40, 0, 1, 39), (40, 0, 1, 40), (40, 4, 1, 41), (571, 4, 1, 1500), (16, 15, 1, 90), (1, 0, 1, 7), (33, 1, 5, 31), (100, 4, 96, 400), (64, 0, 64, 64),
-    (70, 6, 20, 55), (300, 2, 130, 250), (2000, 4, 3, 100000), (5000, 0, 1, 2 ** 31 - 3)]
+    (70, 6, 20, 55), (300, 2, 130, 250), (2000, 4, 3, 100000), (5000, 0, 1, 2 ** 31 - 3),
+    # (chunks that hide whole tiles of the ring from their first rows: in the middle, at both ends, behind sinks)
+    (300, 0, 300, 400), (300, 0, 250, 640), (320, 40, 280, 330), (520, 3, 400, 1500), (520, 100, 420, 700), (257, 0, 200, 315)]
 
 
 @pytest.mark.parametrize("blocked", [False, True])
