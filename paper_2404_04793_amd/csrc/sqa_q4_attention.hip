@@ -178,7 +178,8 @@ template <typename T, int D, int NT, int M, int KT> struct Q4Work {
     head = h * g + x;
   }
   // Does a row whose token is `back` tokens before the newest see a slot?  The newest lies at `newest`, the others of the ring before it.
-  // (Without branches: where a value was set to -inf behind && and || some lanes have been seen to keep theirs.)
+  // (Without branches.  `if (!(a && (b || c))) s[0] = -INFINITY` for the first register of a product's result was compiled to -inf where !a and to an
+  // empty region for the lanes where only b || c is false: these kept their logit.  tests/test_no_empty_branches.py finds such regions; no kernel has one.)
   __device__ __forceinline__ bool sees(int slot, int back) const {
     int behind = newest - slot;
     behind += behind < 0 ? ring : 0;
