@@ -601,7 +601,7 @@ typedef struct sqa_q4_cache {
  *   axes     : HOST or NULL: positions on several axes (sqa_rope_axes)
  * A sequence that brings more than capacity - n_sink tokens past its capacity would overwrite its own: its keys and values are left
  * out, status SQA_ERR_CAPACITY.  Tokens whose block lies outside the pools (or whose row outside the cache) are left out, status
- * SQA_ERR_SHAPE. */
+ * SQA_ERR_SHAPE.  q_out and the cache's four pools share no memory with each other, with the inputs or with slot_map. */
 sqa_status sqa_q4_append(const sqa_token_rows* q, const sqa_token_rows* k, const sqa_token_rows* v, sqa_dtype dt,
                          int B, int T, int Hq, int Hkv, int D, const sqa_head_prep* prep, int32_t new_pos, void* q_out,
                          const sqa_q4_cache* layer, void* stream, const sqa_batch_opts* opts, const sqa_rope_axes* axes,
@@ -622,7 +622,8 @@ size_t sqa_q4_workspace_bytes(const sqa_q4_cache* layer, int B, int T, int Hq, i
 /* Causal attention of a chunk that has been appended (T = 1: a decode step) over the tokens that the cache still holds:
  *   out[b][t][h] = sum_j softmax_j(q . K_j / sqrt(D)) V_j  over the slots j whose token's position is at most new_pos + t
  *   q   : DEVICE [B][Hq][T][D], dtype dt
- *   out : DEVICE [B][T][Hq][D], dtype dt;  lse : DEVICE float [B][Hq][T] or NULL, as for sqa_chunk_attention
+ *   out : DEVICE [B][T][Hq][D], dtype dt;  lse : DEVICE float [B][Hq][T] or NULL, as for sqa_chunk_attention.  They and the
+ *         workspace share no memory with each other, with q or with the cache
  * With the positions, lengths and budgets of the append.  A token whose own slot was taken again by the chunk's later ones cannot be (see
  * sqa_q4_append): such a sequence gets rows of zeros and lse -inf, status SQA_ERR_CAPACITY; so does a unit one of whose blocks lies
  * outside the pools, status SQA_ERR_SHAPE (tokens that see nothing of that block may have their rows all the same).  Queries, probabilities and sums keep fp32's precision (bf16: queries exactly, probabilities

@@ -68,5 +68,11 @@ inline Q4Args q4_args(const sqa_q4_cache* layer, int B, int T, int Hq, int Hkv, 
 inline int64_t q4_rows(const sqa_q4_cache& c, int B, int Hkv) {
   return c.block_table ? (int64_t)c.n_blocks * SQA_BLOCK_SLOTS : (int64_t)B * Hkv * c.capacity;
 }
+// Does memory that a call writes (n bytes at p, or NULL) lie in the cache or its table?
+inline bool in_q4(const sqa_q4_cache& c, int B, int Hkv, int D, const void* p, size_t n) {
+  const size_t codes = (size_t)q4_rows(c, B, Hkv) * D / 2, powers = codes / (kGroup / 2);
+  return p && (overlap(p, n, c.K, codes) || overlap(p, n, c.V, codes) || overlap(p, n, c.K_scale, powers) || overlap(p, n, c.V_scale, powers) ||
+               (c.block_table && overlap(p, n, c.block_table, (size_t)B * Hkv * c.blocks_per_unit * sizeof(int32_t))));
+}
 
 }  // namespace sqa

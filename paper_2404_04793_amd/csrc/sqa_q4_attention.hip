@@ -936,11 +936,15 @@ extern "C" sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T
   sqa_status why;
   if (bad_q4(*layer, D, &why)) return why;
   if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return SQA_ERR_SHAPE;
-  if (ws_bytes < sqa_q4_workspace_bytes(layer, B, T, Hq, Hkv, D)) return SQA_ERR_CAPACITY;
+  const size_t need = sqa_q4_workspace_bytes(layer, B, T, Hq, Hkv, D);
+  if (ws_bytes < need) return SQA_ERR_CAPACITY;
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
   if (uniform && (int64_t)new_pos + T > layer->capacity && T > layer->capacity - layer->n_sink) return SQA_ERR_CAPACITY;
   const size_t es = dt == SQA_F32 ? 4 : 2, qb = (size_t)B * Hq * T * D * es, lb = (size_t)B * Hq * T * sizeof(float);
   if (overlap(q, qb, out, qb) || (lse && (overlap(lse, lb, q, qb) || overlap(lse, lb, out, qb)))) return SQA_ERR_SHAPE;
+  // (workgroups that still read these would see what others have stored)
+  if (overlap(workspace, need, q, qb) || overlap(workspace, need, out, qb) || (lse && overlap(workspace, need, lse, lb)) || in_q4(*layer, B, Hkv, D, out, qb) ||
+      in_q4(*layer, B, Hkv, D, lse, lb) || in_q4(*layer, B, Hkv, D, workspace, need)) return SQA_ERR_SHAPE;
   const Q4Plan p = q4_plan(dt, B, T, Hq, Hkv, new_pos, layer->capacity, uniform);
   if ((int64_t)B * Hkv * p.tiles * p.splits > INT32_MAX - 8) return SQA_ERR_SHAPE;
   Q4AttentionArgs a{};

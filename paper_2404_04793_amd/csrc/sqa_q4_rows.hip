@@ -220,6 +220,13 @@ extern "C" sqa_status sqa_q4_append(const sqa_token_rows* q, const sqa_token_row
   };
   if (hits(q_out, q_bytes) || hits(layer->K, c_bytes) || hits(layer->V, c_bytes) || hits(layer->K_scale, p_bytes) || hits(layer->V_scale, p_bytes))
     return SQA_ERR_SHAPE;
+  if (in_q4(*layer, B, Hkv, D, q_out, q_bytes)) return SQA_ERR_SHAPE;
+  // (keys and values are written at once; a call that only reads may be given one pool for both)
+  if (overlap(layer->K, c_bytes, layer->V, c_bytes) || overlap(layer->K_scale, p_bytes, layer->V_scale, p_bytes)) return SQA_ERR_SHAPE;
+  for (const void* codes : {layer->K, layer->V})
+    if (overlap(codes, c_bytes, layer->K_scale, p_bytes) || overlap(codes, c_bytes, layer->V_scale, p_bytes)) return SQA_ERR_SHAPE;
+  const size_t m_bytes = (size_t)B * Hkv * T * sizeof(int32_t);
+  if (slot_map && (in_q4(*layer, B, Hkv, D, slot_map, m_bytes) || (q_out && overlap(slot_map, m_bytes, q_out, q_bytes)))) return SQA_ERR_SHAPE;
   if ((int64_t)B * T * ((Hq + 1) / 2 + (Hkv + 1) / 2) > (int64_t)INT32_MAX) return SQA_ERR_SHAPE;
   a.a = q4_args(layer, B, T, Hq, Hkv, new_pos, opts);
   if (q) a.q = *q;
@@ -240,12 +247,9 @@ extern "C" sqa_status sqa_q4_read(const sqa_q4_cache* layer, sqa_dtype dt, int B
   sqa_status why;
   if (bad_q4(*layer, D, &why)) return why;
   if (!(opts && (opts->prompt_len || opts->new_pos_seq || opts->budget_seq)) && (int64_t)first_slot + T > layer->capacity) return SQA_ERR_CAPACITY;
-  const size_t out_bytes = (size_t)B * Hkv * T * D * (dt == SQA_F32 ? 4 : 2), c_bytes = (size_t)q4_rows(*layer, B, Hkv) * D / 2;
+  const size_t out_bytes = (size_t)B * Hkv * T * D * (dt == SQA_F32 ? 4 : 2);
   if (k_out && v_out && overlap(k_out, out_bytes, v_out, out_bytes)) return SQA_ERR_SHAPE;
-  for (const void* out : {k_out, v_out})
-    if (out && (overlap(out, out_bytes, layer->K, c_bytes) || overlap(out, out_bytes, layer->V, c_bytes) ||
-                overlap(out, out_bytes, layer->K_scale, c_bytes / 16) || overlap(out, out_bytes, layer->V_scale, c_bytes / 16)))
-      return SQA_ERR_SHAPE;
+  if (in_q4(*layer, B, Hkv, D, k_out, out_bytes) || in_q4(*layer, B, Hkv, D, v_out, out_bytes)) return SQA_ERR_SHAPE;
   const int64_t threads = (int64_t)B * Hkv * T * (D / 8), blocks = (threads + kRowsThreads - 1) / kRowsThreads;
   if (blocks > INT32_MAX) return SQA_ERR_SHAPE;
   Q4ReadArgs a{q4_args(layer, B, T, Hkv, Hkv, first_slot, opts), k_out, v_out};
