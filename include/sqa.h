@@ -494,7 +494,7 @@ sqa_status sqa_qk_norm_rope_ex(const sqa_token_rows* q, const sqa_token_rows* k,
  *   q, q_out : the chunk's queries, prepared by the same launch as in sqa_qk_norm_rope; or both NULL
  *   k, v     : HOST structs
  *   layer    : HOST struct with DEVICE pointers, any of the three layouts; score_acc may be NULL.  Units as
- *              sqa_prefill_compress or decode leave them, or empty ones ({0, 0, -2, 0})
+ *              sqa_prefill_compress or decode leave them, or empty ones ({0, 0, -2, 0}).  K, V, the inputs and q_out share no memory
  * A unit takes a chunk while it still holds every token of its sequence (slot = position, as it is until the
  * first eviction).  One that does not is left untouched, and so is one with too few tokens, status SQA_ERR_STATE; one
  * whose budget or slots would be exceeded: SQA_ERR_CAPACITY; a budget_seq entry out of range: SQA_ERR_BUDGET;
@@ -517,7 +517,8 @@ size_t sqa_chunk_workspace_bytes(const sqa_layer_cache* layer, int B, int T, int
 /* Causal attention of a chunk over all that the cache holds up to each of its tokens (the chunk has been appended):
  *   out[b][t][h] = sum_{j <= new_pos + t} softmax_j(q . K_j / sqrt(D)) V_j
  *   q   : DEVICE [B][Hq][T][D], dtype dt
- *   out : DEVICE [B][T][Hq][D], dtype dt (what an output projection takes)
+ *   out : DEVICE [B][T][Hq][D], dtype dt (what an output projection takes).  out, lse and the workspace share no memory with each
+ *         other, with q or with the cache
  *   lse : DEVICE float [B][Hq][T] or NULL: ln sum_{j <= new_pos + t} exp(q . K_j / sqrt(D)), the row_lse of
  *         sqa_prefill_scores_lse and sqa_chunk_scores
  * The softmax is in fp32.  In bf16 the product with V takes probabilities that are right to 2^-15 of each; where a workgroup
@@ -536,7 +537,8 @@ sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, int T, int Hq
  *                   exp(q . K_j / sqrt(D) - lse[b][h][t])
  * After the last chunk of a prompt score_acc is what sqa_prefill_scores gives for the whole prompt (to rounding), and K, V and
  * score_acc of a dense layer are the inputs of sqa_prefill_compress (P = capacity, opts->prompt_len).
- *   q, lse : as for sqa_chunk_attention; layer->score_acc required.  A wrong lse gives wrong scores, not an error
+ *   q, lse : as for sqa_chunk_attention; layer->score_acc required.  A wrong lse gives wrong scores, not an error; they share no memory
+ *            with score_acc or the workspace
  * What a token has given stays: an append at a smaller position takes its slot back, not its share of earlier slots'
  * scores.  So a draft is scored once it is known which of its tokens stay (opts->prompt_len).
  * A unit that does not hold the chunk is left untouched, status as above.  Results are the same from run to run. */

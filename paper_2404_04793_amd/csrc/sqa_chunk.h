@@ -97,6 +97,17 @@ inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
 }
+// Does memory that a call writes beside the cache (n bytes at p, or NULL) lie in a layer's?  (What packed units take is known to the device alone.)
+inline bool in_layer(const sqa_layer_cache& c, int B, int Hkv, int D, size_t es, const void* p, size_t n) {
+  if (!p) return false;
+  const size_t units = (size_t)B * Hkv, slots = units * c.capacity;
+  if (overlap(p, n, c.unit_state, units * SQA_ST_WORDS * sizeof(int32_t))) return true;
+  if (c.unit_offset) return overlap(p, n, c.unit_offset, (units + 1) * sizeof(*c.unit_offset));
+  const size_t bytes = (c.block_table ? (size_t)c.n_blocks * SQA_BLOCK_SLOTS : slots) * D * es;
+  return overlap(p, n, c.K, bytes) || overlap(p, n, c.V, bytes) || overlap(p, n, c.pos, slots * sizeof(int32_t)) ||
+         (c.score_acc && overlap(p, n, c.score_acc, slots * sizeof(float))) ||
+         (c.block_table && overlap(p, n, c.block_table, units * c.blocks_per_unit * sizeof(int32_t)));
+}
 
 // Data that one workgroup hands to another inside a launch: stored through to and loaded from where every XCD sees it (no
 // cache is flushed), 16 bytes at a time by buffer instructions with the agent-scope bits set, or 8 by atomics.

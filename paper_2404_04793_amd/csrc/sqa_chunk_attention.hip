@@ -812,10 +812,15 @@ extern "C" sqa_status sqa_chunk_attention(const void* q, sqa_dtype dt, int B, in
   if (sqa::bad_chunk_shape(B, T, Hq, Hkv, D, new_pos, opts)) return SQA_ERR_SHAPE;
   if (!sqa::aligned16(q) || !sqa::aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return SQA_ERR_SHAPE;
-  if (ws_bytes < sqa_chunk_workspace_bytes(layer, B, T, Hq, Hkv, D)) return SQA_ERR_CAPACITY;
+  const size_t need = sqa_chunk_workspace_bytes(layer, B, T, Hq, Hkv, D);
+  if (ws_bytes < need) return SQA_ERR_CAPACITY;
   if (!(opts && (opts->prompt_len || opts->new_pos_seq)) && (int64_t)new_pos + T > layer->capacity) return SQA_ERR_CAPACITY;
   const size_t es = dt == SQA_F32 ? 4 : 2, qb = (size_t)B * Hq * T * D * es, lb = (size_t)B * Hq * T * sizeof(float);
   if (sqa::overlap(q, qb, out, qb) || (lse && (sqa::overlap(lse, lb, q, qb) || sqa::overlap(lse, lb, out, qb)))) return SQA_ERR_SHAPE;
+  // (workgroups that still read these would see what others have stored)
+  if (sqa::overlap(workspace, need, q, qb) || sqa::overlap(workspace, need, out, qb) || (lse && sqa::overlap(workspace, need, lse, lb)) ||
+      sqa::in_layer(*layer, B, Hkv, D, es, out, qb) || sqa::in_layer(*layer, B, Hkv, D, es, lse, lb) || sqa::in_layer(*layer, B, Hkv, D, es, workspace, need))
+    return SQA_ERR_SHAPE;
   sqa::AttentionArgs a{};
   a.c = sqa::chunk_args(layer, B, T, Hq, Hkv, new_pos, opts);
   a.q = q; a.out = out; a.lse = lse;

@@ -312,8 +312,9 @@ static sqa_status rows_call(const sqa_token_rows* q, const sqa_token_rows* k, co
   if (hits(q_out, q_bytes) || hits(k_out, k_bytes) || (q_out && k_out && overlap(q_out, q_bytes, k_out, k_bytes))) return SQA_ERR_SHAPE;
   if (layer && !layer->unit_offset) {
     const size_t c_bytes = (layer->block_table ? (size_t)layer->n_blocks * SQA_BLOCK_SLOTS : (size_t)B * Hkv * layer->capacity) * D * es;
-    if (hits(layer->K, c_bytes) || hits(layer->V, c_bytes)) return SQA_ERR_SHAPE;
+    if (hits(layer->K, c_bytes) || hits(layer->V, c_bytes) || overlap(layer->K, c_bytes, layer->V, c_bytes)) return SQA_ERR_SHAPE;
   }
+  if (layer && in_layer(*layer, B, Hkv, D, es, q_out, q_bytes)) return SQA_ERR_SHAPE;
   a.c = chunk_args(layer, B, T, Hq, Hkv, new_pos, opts);
   if (q) a.q = *q;
   if (k) a.k = *k;

@@ -330,9 +330,15 @@ extern "C" sqa_status sqa_chunk_scores(const void* q, const float* lse, sqa_dtyp
   if (dt != SQA_F32 && dt != SQA_BF16) return SQA_ERR_DTYPE;
   if (sqa::bad_chunk_shape(B, T, Hq, Hkv, D, new_pos, opts)) return SQA_ERR_SHAPE;
   if (!sqa::aligned16(q) || (reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return SQA_ERR_SHAPE;
-  if (ws_bytes < sqa_chunk_workspace_bytes(layer, B, T, Hq, Hkv, D)) return SQA_ERR_CAPACITY;
+  const size_t need = sqa_chunk_workspace_bytes(layer, B, T, Hq, Hkv, D);
+  if (ws_bytes < need) return SQA_ERR_CAPACITY;
   const bool uniform = !(opts && (opts->prompt_len || opts->new_pos_seq));
   if (uniform && (int64_t)new_pos + T > layer->capacity) return SQA_ERR_CAPACITY;
+  // what the call writes (the scores and the workspace) and what it reads
+  const size_t es = dt == SQA_F32 ? 4 : 2, qb = (size_t)B * Hq * T * D * es, lb = (size_t)B * Hq * T * sizeof(float);
+  if (sqa::overlap(workspace, need, q, qb) || sqa::overlap(workspace, need, lse, lb) || sqa::in_layer(*layer, B, Hkv, D, es, workspace, need)) return SQA_ERR_SHAPE;
+  const size_t sb = (size_t)B * Hkv * layer->capacity * sizeof(float);
+  if (!layer->unit_offset && (sqa::overlap(layer->score_acc, sb, q, qb) || sqa::overlap(layer->score_acc, sb, lse, lb))) return SQA_ERR_SHAPE;
   sqa::ScoresArgs a{};
   a.c = sqa::chunk_args(layer, B, T, Hq, Hkv, new_pos, opts);
   a.q = q; a.lse = lse;
