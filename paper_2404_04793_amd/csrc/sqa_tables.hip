@@ -88,16 +88,23 @@ template <bool MOVE, bool UPDATE> __global__ __launch_bounds__(kAssignThreads) v
       const int b = owner(lacks, a.B, i), k = i - lacks[b], each = (lacks[b + 1] - lacks[b]) / a.Hkv;
       return a.table + ((int64_t)b * a.Hkv + k / each) * a.per + needs[b] - each + k % each;
     };
+    // (what changes hands is a block's number, or reported: whether it is a number that nothing else holds cannot be seen from here)
+    auto look = [&](int block) { if ((unsigned)block >= (unsigned)a.n_blocks && a.status) *a.status = SQA_ERR_STATE; };
     const int at = blockIdx.x * kAssignThreads + tid, all = gridDim.x * kAssignThreads;
     for (int i = at; i < given; i += all) {         // a block that comes back, to the list's end, and from there on where it is taken at once
       const int b = owner(gives, a.B, i), k = i - gives[b], each = (gives[b + 1] - gives[b]) / a.Hkv;
       int32_t* const entry = a.table + ((int64_t)b * a.Hkv + k / each) * a.per + needs[b] + k % each;
       const int block = *entry;
+      look(block);
       *entry = -1;
       a.free_ids[count + i] = block;
       if (given - 1 - i < taken) *entry_of(given - 1 - i) = block;
     }
-    for (int i = given + at; i < taken; i += all) *entry_of(i) = a.free_ids[there - 1 - i];       // (what the list held before)
+    for (int i = given + at; i < taken; i += all) { // (what the list held before)
+      const int block = a.free_ids[there - 1 - i];
+      look(block);
+      *entry_of(i) = block;
+    }
   }
   if constexpr (UPDATE) {
     if (MOVE) __syncthreads();
