@@ -662,7 +662,7 @@ sqa_status sqa_q4_plan(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, in
  * 0 .. blocks_per_unit: that sequence is left alone, status SQA_ERR_STATE; a list with more blocks than it has room for: nothing is
  * done, status SQA_ERR_STATE.  An entry that changes hands and is no block of the pools (0 .. n_blocks - 1) goes where it would
  * go, status SQA_ERR_STATE: whoever gets it is left out by the calls on the cache.  A number that is held twice is not noticed.
- * B <= SQA_MAX_ASSIGN.  Nothing is kept between calls, and the result does not depend on how threads run. */
+ * B <= SQA_MAX_ASSIGN; at most 2^31 - 1 - 2^16 entries in all.  Nothing is kept between calls, and the result does not depend on how threads run. */
 enum { SQA_MAX_ASSIGN = 8192 };
 sqa_status sqa_block_assign(int32_t* block_table, int B, int Hkv, int32_t blocks_per_unit, int32_t capacity, const int32_t* tokens,
                             int32_t* held, int32_t* free_ids, int32_t* free_count, int32_t n_blocks, int32_t* status, void* stream);

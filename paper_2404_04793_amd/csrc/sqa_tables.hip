@@ -10,6 +10,8 @@ namespace sqa {
 
 constexpr int kAssignThreads = 1024;
 constexpr int kOneAssign = 4096;                    // entries of all tables that one workgroup sees to
+constexpr int kMostAssign = 64;                     // workgroups of a launch
+constexpr int kMostEntries = INT32_MAX - kMostAssign * kAssignThreads;                   // (a thread's next entry, past the last, is a 32-bit number too)
 
 struct AssignArgs {
   int32_t* table;
@@ -152,7 +154,7 @@ extern "C" sqa_status sqa_block_assign(int32_t* block_table, int B, int Hkv, int
   if (!block_table || !tokens || !held || !free_ids || !free_count) return SQA_ERR_NULL;
   for (const void* p : {(const void*)block_table, (const void*)tokens, (const void*)held, (const void*)free_ids, (const void*)free_count, (const void*)status})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return SQA_ERR_SHAPE;
-  if (B < 1 || B > SQA_MAX_ASSIGN || Hkv < 1 || blocks_per_unit < 1 || n_blocks < 1 || (int64_t)B * Hkv > INT32_MAX / blocks_per_unit) return SQA_ERR_SHAPE;
+  if (B < 1 || B > SQA_MAX_ASSIGN || Hkv < 1 || blocks_per_unit < 1 || n_blocks < 1 || (int64_t)B * Hkv > sqa::kMostEntries / blocks_per_unit) return SQA_ERR_SHAPE;
   if (capacity < 1 || capacity > sqa::kQ4MostSlots || (int64_t)blocks_per_unit * SQA_BLOCK_SLOTS < capacity) return SQA_ERR_CAPACITY;
   sqa::AssignArgs a{block_table, tokens, held, free_ids, free_count, status, B, Hkv, blocks_per_unit, capacity, n_blocks};
   const size_t lds = (size_t)(3 * B + 2) * sizeof(int32_t);
@@ -164,7 +166,7 @@ extern "C" sqa_status sqa_block_assign(int32_t* block_table, int B, int Hkv, int
   };
   const int64_t entries = (int64_t)B * Hkv * blocks_per_unit;
   const bool ok = entries <= sqa::kOneAssign ? launch(sqa::block_assign_kernel<true, true>, 1)
-                                             : launch(sqa::block_assign_kernel<true, false>, (int)(entries / sqa::kOneAssign < 64 ? entries / sqa::kOneAssign + 1 : 64)) &&
+                                             : launch(sqa::block_assign_kernel<true, false>, (int)(entries / sqa::kOneAssign < sqa::kMostAssign ? entries / sqa::kOneAssign + 1 : sqa::kMostAssign)) &&
                                                    launch(sqa::block_assign_kernel<false, true>, 1);
   if (!ok) { (void)hipGetLastError(); return SQA_ERR_HIP; }
   return SQA_OK;

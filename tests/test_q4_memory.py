@@ -42,3 +42,10 @@ def test_read(change):
     a = dict(layer=host.layer(**TABLE), dt=1, B=2, T=4, Hkv=2, D=64, first=10, k_out=P(0x100000), v_out=P(0x200000), stream=None, opts=None)
     a.update(change)
     assert sqa._lib.sqa_q4_read(*a.values()) == SHAPE
+
+
+@pytest.mark.parametrize("B,Hkv,per", [(1, 1, 2 ** 31 - 1), (1, 1, 2 ** 31 - 65536), (2, 4, 2 ** 28 - 8191)])
+def test_tables_whose_entries_a_thread_could_not_count(B, Hkv, per):
+    """Threads step through what changes hands by 65536 at a time: past the last entry the number has to stay within 32 bits."""
+    at = [P(x << 34) for x in range(1, 7)]
+    assert sqa._lib.sqa_block_assign(at[0], B, Hkv, per, 64, at[1], at[2], at[3], at[4], 2 ** 31 - 1, at[5], None) == SHAPE
