@@ -626,11 +626,16 @@ size_t sqa_q4_workspace_bytes(const sqa_q4_cache* layer, int B, int T, int Hq, i
  *   q   : DEVICE [B][Hq][T][D], dtype dt
  *   out : DEVICE [B][T][Hq][D], dtype dt;  lse : DEVICE float [B][Hq][T] or NULL, as for sqa_chunk_attention.  They and the
  *         workspace share no memory with each other, with q or with the cache
- * With the positions, lengths and budgets of the append.  A token whose own slot was taken again by the chunk's later ones cannot be (see
- * sqa_q4_append): such a sequence gets rows of zeros and lse -inf, status SQA_ERR_CAPACITY; so does a unit one of whose blocks lies
- * outside the pools, status SQA_ERR_SHAPE (tokens that see nothing of that block may have their rows all the same).  Queries, probabilities and sums keep fp32's precision (bf16: queries exactly, probabilities
- * to 2^-15; where a workgroup has 128 rows (sqa_q4_plan) they are rounded to bf16 for the product with V).  A slot that a token may not see does not
- * change its row by a bit.  Results are the same from run to run. */
+ * With the positions, lengths and budgets of the append.  A token whose own slot was taken again by the chunk's later ones cannot be
+ * (see sqa_q4_append): such a sequence gets rows of zeros and lse -inf, status SQA_ERR_CAPACITY; so does a unit one of whose blocks lies
+ * outside the pools, status SQA_ERR_SHAPE (tokens that see nothing of that block may have their rows all the same).
+ * In a ring that has turned the chunk's later tokens have taken the slots of the oldest before its first row is worked out: the k-th token
+ * from its end sees k tokens fewer than the ring holds.  There rows depend on how a prompt is cut, a draft's rows are not those of
+ * its tokens one by one, and a draft cannot be taken back; single tokens (T = 1) have whole windows.
+ * Queries, sums and statistics keep fp32's precision (queries in bf16 are taken exactly).  For the product with V fp32 calls take
+ * probabilities to fp32's precision, bf16 calls to 2^-15 of each, but rounded to bf16 where a workgroup has 128 rows: which form a call has
+ * follows from B, T, heads and slots of the whole batch (sqa_q4_plan).  A slot that a token may not see does not change its row by
+ * a bit.  Results are the same from run to run. */
 sqa_status sqa_q4_attention(const void* q, sqa_dtype dt, int B, int T, int Hq, int Hkv, int D, int32_t new_pos,
                             const sqa_q4_cache* layer, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream,
                             const sqa_batch_opts* opts);
@@ -649,7 +654,8 @@ sqa_status sqa_q4_plan(const sqa_q4_cache* layer, sqa_dtype dt, int B, int T, in
 
 /* ---- block tables and slot maps on the GPU -----------------------------------
  * For loops whose lengths live on the GPU (or that are captured into a graph): tables of either kind of cache are brought up to
- * date from the sequences' lengths, blocks taken from and given back to a free list in device memory.
+ * date from the sequences' lengths, blocks taken from and given back to a free list in device memory.  Rows of these tables may be longer
+ * than SQA_MAX_BLOCKS_PER_UNIT, but the calls on a cache refuse one that names such a table.
  *   block_table : DEVICE [B*Hkv][blocks_per_unit], blocks_per_unit >= ceil(capacity / SQA_BLOCK_SLOTS)
  *   tokens      : DEVICE [B]: how many tokens each sequence is to have room for (those beyond capacity need none); 0: it has left,
  *                 < 0: it stays as it is

@@ -262,8 +262,10 @@ static void launch_rows(RowsArgs& a, hipStream_t st) {
   const int64_t groups = (int64_t)a.c.B * (a.q_groups + a.kv_groups);
   constexpr int waves = kRowsThreads / SQA_WAVE;
   if (a.axes.n) {
-    // four or five groups of heads a wave where that leaves every SIMD two waves, whichever comes out more evenly (10 groups: 51 us, 55 with four, 58
-    // with eight or two)
+    // four or five groups of heads a wave where that leaves every SIMD two waves, whichever comes out more evenly.  (10 groups: 51 us, 55 with four, 58
+    // with eight or two.  2 x 4500 tokens whose rows lie in HBM, with five, four, two and one: bf16 at D = 128 10 groups 57, 61, 64 and 69 us, 9 groups 51, 55,
+    // 58 and 59, 6 groups 40, 40, 39 and 41; at D = 64 10 groups 57, 61, 63 and 67, 5 groups 32, 35, 35 and 34; fp32 at D = 64 10 groups 51, 54, 57 and 60, at
+    // D = 128 half as many tokens of 20 groups 53, 52, 58 and 60.  Fewer than four groups are one wave's: 2 groups 26 us, with two a wave 22.)
     const int all = a.q_groups + a.kv_groups, U = (all + 4) / 5 * 5 < (all + 3) / 4 * 4 ? 5 : 4;
     const bool many = (int64_t)a.c.B * a.c.T * ((all + U - 1) / U) >= 2048;
     const int64_t items = (int64_t)a.c.B * a.c.T * (many ? (all + U - 1) / U : all);

@@ -885,7 +885,10 @@ static Q4Plan q4_plan(sqa_dtype dt, int B, int T, int Hq, int Hkv, int32_t new_p
     // only until every CU has one.  (256 units of 1000 slots: 8 waves 12.2 us, 4 with 3 workgroups a unit 14.0; 8 units of 30000: 32
     // workgroups of 8 waves each 19.2, 64 22.8, 64 of 4 waves 24.6; 512 units of 1000: 4 waves 18.7, 8 20.0; 2048 of 571: 2 waves 31.2, 4 36.5, 8 44.)
     p.waves = items >= 1024 ? 2 : (items >= 512 ? 4 : 8);
-    s = std::min(256 / items, slots / 256);         // (8 tiles at least: a wave each)
+    // (8 tiles at least, a wave each, of units as long as `slots`.  In a ragged batch that is the capacity, and shorter units are cut into as many shares.
+    // One token of 32 heads over 8 with no slot to spare and with room for 32768, us: 1 sequence of 500 tokens 9.1 and 12.1, of 2000 12.0 and 13.9, 8 of 500
+    // 8.5 and 9.8, 8 of 2000 12.3 and 12.0.)
+    s = std::min(256 / items, slots / 256);
   }
   s = std::min<int64_t>(s, kQ4Splits);
   p.splits = s < 1 ? 1 : (int)s;

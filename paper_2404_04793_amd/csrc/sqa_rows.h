@@ -1,5 +1,6 @@
-// Rows of heads as projections leave them, a lane holding 16 bytes of one: norm and rotation (what sqa_chunk_rows.hip and
-// sqa_q4_rows.hip share), and the checks of their arguments.
+// Rows of heads as projections leave them, a lane holding 16 bytes of one: norm and rotation for waves that take one token and several groups of
+// heads (axis_rows_kernel in sqa_chunk_rows.hip, q4_rows_kernel), and the checks of all such calls' arguments.  chunk_rows_kernel, whose waves take
+// several tokens of one group, has the same two steps in an order of its own.
 #pragma once
 #include "sqa_chunk.h"
 
@@ -37,7 +38,6 @@ template <int LPR> __device__ __forceinline__ float half_row_away(float v) {
   if constexpr (LPR == 16) return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true));      // row_ror:8
   else return __shfl_xor(v, LPR / 2, LPR);
 }
-
 
 // Positions on several axes (sqa_rope_axes): which axis a pair goes by, two bits each, as the host works it out.
 struct AxesArgs {
@@ -169,7 +169,6 @@ inline bool rows_overlap(const sqa_token_rows* r, int B, int T, int H, int D, si
   const int64_t last = (B > 1 ? (int64_t)(B - 1) * r->seq_stride : 0) + (T > 1 ? (int64_t)(T - 1) * r->row_stride : 0) + (int64_t)H * D;
   return overlap(r->data, (size_t)last * es, p, n);
 }
-
 
 // the library's view of a caller's axes; false: refused
 inline bool axes_args(const sqa_rope_axes* axes, const sqa_head_prep* prep, AxesArgs* out, sqa_status* why) {

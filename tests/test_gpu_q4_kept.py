@@ -196,3 +196,19 @@ def test_many_heads_and_few_rows_keep_their_probabilities(sqa):
             q = (torch.randn(B, Hq, T, D, generator=gen, device=DEV) * 1.5).bfloat16()
             out, lse = sqa.q4_attention(q, before, c)
             attention_test.check(2.0 ** -15, c, q, out, lse, [before] * B, [T] * B, [cap] * B, 0, (B, T, before, Hq, Hkv))
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+def test_how_much_a_chunk_sees_of_a_turned_ring(sqa, dtype, D):
+    """Keys of zeros: ln(slots seen) is what a row's normaliser says.  A chunk's k-th token from its end sees k slots fewer than the ring and the sinks
+    hold, a single token all of them."""
+    dt, cap, sink = R.DT[dtype], 64, 4
+    for T, before in ((1, 200), (10, 200), (60, 300), (7, 57), (7, 55)):
+        for B, g, Hkv in ((1, 3, 1), (2, 8, 4)):
+            c = sqa.Q4Caches([cap], B, Hkv, D, DEV, n_sink=sink)
+            out, lse = sqa.q4_attention(torch.randn(B, g * Hkv, T, D, device=DEV).to(dt), before, c)
+            turned = before + T > cap
+            seen = torch.tensor([cap - (T - 1 - t) if turned else before + t + 1 for t in range(T)], dtype=torch.float64, device=DEV)
+            want = seen.log().expand(lse.shape)
+            # (chunk_reference.py's bound with logits of 0: sums of `cap` terms, the exponential's and the logarithm's roundings)
+            assert bool(((lse.double() - want).abs() <= 4 * R.U + cap * R.U + 4 * R.U * (want + 1)).all()) and not bool(out.any()), (T, before)
